@@ -124,7 +124,8 @@ int specache_create(const specache_config* cfg, specache_ctx** out);
 int specache_destroy(specache_ctx* ctx);
 
 /* Message of the most recent failed call on ctx (never NULL; "" if none).
- * With ctx == NULL returns the message of the last failed specache_create. */
+ * With ctx == NULL returns the message of the calling thread's last failed specache_create or
+ * other call that takes no context. */
 const char* specache_last_error(const specache_ctx* ctx);
 
 /* Token counts of a layer: N tokens cached, of which the first Nq are quantised
@@ -431,6 +432,148 @@ int specache_timing(specache_ctx* ctx, int32_t enable, double* total_us, int64_t
  */
 int specache_measure_hbm_read(int64_t bytes, int32_t reps, double* gbs);
 int specache_measure_link(int64_t bytes, int32_t reps, double* memcpy_gbs, double* kernel_gbs);
+
+/*
+ * What stands around the cache's calls in a model's step: rotary positions, attention with a sliding window over 16-bit keys
+ * and values (a prompt's attention ahead of the bulk specache_quantize_append, and the step of a layer that keeps its 16-bit
+ * pairs), and the choice of the next tokens.  These calls take no context: they run on the current HIP device, whose memory
+ * every pointer but the host structures is, keep nothing between calls and may come from several threads.  They only enqueue
+ * work on `stream` (none allocates, synchronises or uses a stream or event of its own) and may be captured into a graph.
+ * specache_last_error(NULL) has the message of the calling thread's last failure.
+ */
+
+/* 16-bit rows of 128 channels: channel c of the row of (batch b, head h, token t) is element
+ * b * batch + h * head + t * token + c of data.  data is 16-byte aligned, the strides (in elements, not negative) are
+ * multiples of 8; a stride of 0 repeats rows (inputs only).  A projection's [B, n, heads * 128] and the cache's [B, heads, n, 128] are both such rows. */
+typedef struct specache_view {
+    void* data;
+    int64_t batch, head, token;
+} specache_view;
+
+enum { SPECACHE_ROTARY_HALF = 0, SPECACHE_ROTARY_INTERLEAVED = 1 };
+enum { SPECACHE_ROTARY_UNSCALED = 0, SPECACHE_ROTARY_LINEAR = 1, SPECACHE_ROTARY_BASE = 2, SPECACHE_ROTARY_BANDS = 3,
+       SPECACHE_ROTARY_RAMP = 4 };
+
+/*
+ * How positions turn channels.  With d = rotary_dim, pair i of the d / 2 pairs turns by f_i = base^(-2 i / d) per position;
+ * SPECACHE_ROTARY_HALF pairs channels (i, i + d / 2), SPECACHE_ROTARY_INTERLEAVED (2 i, 2 i + 1); channels from d on stay.
+ * scaling, for a context stretched by `factor` beyond `original_tokens` (both ignored where not named):
+ *   LINEAR  f_i / factor
+ *   BASE    base * factor^(d / (d - 2)) in the place of base
+ *   BANDS   with r = original_tokens * f_i / 2 pi (a pair's turns over the original length) and
+ *           g = clamp((r - low) / (high - low), 0, 1):  g f_i + (1 - g) f_i / factor
+ *   RAMP    the same with g = 1 - clamp((i - a) / max(b - a, 0.001), 0, 1), where a = max(0, floor(pair(high))) and
+ *           b = min(d - 1, ceil(pair(low))) for pair(t) = d ln(original_tokens / (2 pi t)) / (2 ln base), the pair that makes t turns
+ * gain multiplies cosine and sine; <= 0 selects 1, with RAMP 0.1 ln(factor) + 1.
+ */
+typedef struct specache_rotary_config {
+    int32_t rotary_dim;      /* a multiple of 16, 16 .. 128                                        */
+    int32_t layout;          /* SPECACHE_ROTARY_HALF or SPECACHE_ROTARY_INTERLEAVED                */
+    int32_t scaling;         /* SPECACHE_ROTARY_UNSCALED .. SPECACHE_ROTARY_RAMP                   */
+    int32_t original_tokens; /* BANDS, RAMP: >= 1                                                  */
+    double base;             /* > 1                                                                */
+    double factor;           /* LINEAR, BASE, BANDS, RAMP: >= 1                                    */
+    double low, high;        /* BANDS, RAMP: 0 < low < high                                        */
+    double gain;
+} specache_rotary_config;
+
+/* A worked-out configuration (host memory; plain data that may be copied).  turns[i] is pair i's turns per position as a
+ * fraction of 2^64: position times turns, modulo 2^64, is the angle without a rounding however far the position. */
+typedef struct specache_rotary {
+    uint64_t turns[64];
+    float gain;
+    int32_t rotary_dim, layout;
+} specache_rotary;
+
+/* Host only.  Errors: EINVAL (null pointer, a field out of its range). */
+int specache_rotary_plan(const specache_rotary_config* cfg, specache_rotary* out);
+
+/*
+ * Rotates q [batch, n_q_heads, tokens] and k [batch, n_kv_heads, tokens] and copies v [batch, n_kv_heads, tokens] as it is, each
+ * from its rows to those of the *_out view, in one launch: from a projection's output to what specache_quantize_append and
+ * the scoring calls take.  k, k_out and v, v_out may be NULL (both of a pair): that tensor is left out.  dtype: SPECACHE_FP16 or
+ * SPECACHE_BF16; the products and sums are binary32, rounded once.  An output view equals its input view (in place: same
+ * address and strides) or shares no memory with any input.
+ * positions: device int32 [batch, tokens], contiguous; any int32 (a negative one turns the other way).  NULL: token t of
+ * every sequence is at first_position + t.  first_position + tokens stays below 2^31.
+ * batch = 0, tokens = 0 or n_q_heads = 0 are allowed.
+ * Errors: EINVAL (null, misaligned or in-place-but-different views, counts, dtype, a plan that specache_rotary_plan did not write), EHIP.
+ */
+int specache_rotate(const specache_rotary* plan, int32_t dtype, int32_t batch, int32_t tokens, int32_t n_q_heads,
+                    const specache_view* q, const specache_view* q_out, int32_t n_kv_heads, const specache_view* k,
+                    const specache_view* k_out, const specache_view* v, const specache_view* v_out, const int32_t* positions,
+                    int32_t first_position, void* stream);
+
+/*
+ * Attention over 16-bit keys and values with a sliding window and sinks (first tokens that stay visible).  Of a sequence with
+ * n queries and N cached tokens, query row i stands at position p = N - n + i and sees the positions j <= p with
+ * j < sinks, or p - j < window, or any where window = 0:  out_i = sum_j softmax_j(sm_scale q_i . k_j) v_j.  A row that sees nothing
+ * (n > N) gives zeros.
+ */
+typedef struct specache_window_config {
+    int32_t batch;      /* >= 0                                                                        */
+    int32_t n_q_heads;  /* a multiple of n_kv_heads; Hq / Hkv <= 64                                    */
+    int32_t n_kv_heads; /* >= 1                                                                        */
+    int32_t head_dim;   /* must be 128                                                                 */
+    int32_t q_tokens;   /* rows of q and out per sequence and head, >= 0                               */
+    int32_t kv_tokens;  /* rows of k and v per sequence and head, >= 0; up to 2^30                     */
+    int32_t window;     /* positions seen, the row's own included; 0: all                              */
+    int32_t sinks;      /* first positions that stay visible behind the window, >= 0                   */
+    int32_t dtype;      /* SPECACHE_FP16 or SPECACHE_BF16: type of q, k, v and out                     */
+    float sm_scale;     /* logit scale; <= 0 selects 1/sqrt(head_dim)                                  */
+} specache_window_config;
+
+/* Host only: the bytes of scratch memory that specache_window_attend needs for cfg (0: none).  It depends on the counts, window
+ * and sinks alone.  Errors: EINVAL. */
+int specache_window_scratch(const specache_window_config* cfg, int64_t* bytes);
+
+/*
+ * q, out: [batch, n_q_heads, q_tokens] rows; k, v: [batch, n_kv_heads, kv_tokens] rows (q and out may have the same view).
+ * q_lengths, kv_lengths: device int32 [batch], the n and N of every sequence, held to 0 .. q_tokens and 0 .. kv_tokens;
+ * NULL: q_tokens and kv_tokens.  Rows of q and out from n on and rows of k and v from N on are neither read nor written.
+ * Scores, softmax and sums are binary32; the weights are rounded to dtype for their product with v, the output once.  A value
+ * that is not finite reaches the rows that see it and no others.  Without `window` and `sinks` this is a prompt's causal
+ * attention, with q_tokens = 1 or 2 a step's.  Results do not depend on what else runs, and are the same every time.
+ * scratch: device, 16-byte aligned, scratch_bytes >= specache_window_scratch; written before it is read.  Calls that may
+ * overlap need scratch memory of their own.  NULL where the size is 0.
+ * Errors: EINVAL (null or misaligned view, configuration, scratch), ECAPACITY (scratch too small; nothing is launched), EHIP.
+ */
+int specache_window_attend(const specache_window_config* cfg, const specache_view* q, const specache_view* k,
+                           const specache_view* v, const specache_view* out, const int32_t* q_lengths, const int32_t* kv_lengths,
+                           void* scratch, int64_t scratch_bytes, void* stream);
+
+/*
+ * Choice of a token per row of logits from given random numbers.  A row's tokens are ordered by logit, the largest first, the
+ * lower index first among equals; with weights w_i = exp((x_i - x_max) / temperature) the kept tokens are the
+ *   first top_k in that order (<= 0: all), of these
+ *   the fewest first ones whose weights sum to top_p of the sum so far kept (at least one; >= 1: all), and of these
+ *   those with w_i >= min_p (<= 0: all; at least one);
+ * the choice is the first kept token at which the running sum of the weights exceeds u times their sum (the last kept one where
+ * rounding leaves none).  temperature <= 0: the first token in the order, whatever else is asked for.  A logit of -infinity, or NaN, is a
+ * token that is not allowed: a row of nothing else gives -1.  Among logits of +infinity the weights are 1, of all others then 0.
+ */
+enum { SPECACHE_FP32 = 2 };   /* a type of logits only */
+
+typedef struct specache_sample_config {
+    int32_t rows;        /* >= 0                                                                        */
+    int32_t vocab;       /* 1 .. 2^24                                                                   */
+    int32_t dtype;       /* SPECACHE_FP16, SPECACHE_BF16 or SPECACHE_FP32: type of the logits           */
+    int64_t row_stride;  /* elements from a row to the next, >= 0 (0: every row is the first)           */
+} specache_sample_config;
+
+/* Host only: the bytes of scratch memory that specache_sample needs for cfg (0: none).  Errors: EINVAL. */
+int specache_sample_scratch(const specache_sample_config* cfg, int64_t* bytes);
+
+/*
+ * logits: device [rows] of vocab elements, row_stride apart, aligned to their type.  u: device float32 [rows], in [0, 1).  temperature, top_p, min_p: device
+ * float32 [rows]; top_k: device int32 [rows]; each NULL for 1, no limit, no limit, no limit in every row.  A NaN parameter is taken
+ * as that.  tokens: device int32 [rows].  The sums are in binary64 or in whole numbers, so that the choice is the same every time.
+ * scratch, scratch_bytes: as for specache_window_attend.
+ * Errors: EINVAL, ECAPACITY (scratch too small), EHIP.
+ */
+int specache_sample(const specache_sample_config* cfg, const void* logits, const float* u, const float* temperature,
+                    const int32_t* top_k, const float* top_p, const float* min_p, int32_t* tokens, void* scratch,
+                    int64_t scratch_bytes, void* stream);
 
 #ifdef __cplusplus
 }

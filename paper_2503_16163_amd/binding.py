@@ -19,7 +19,9 @@ EXPORTS = ["specache_create", "specache_destroy", "specache_last_error", "specac
            "specache_plan_append", "specache_quantize_append", "specache_score_topk", "specache_gather",
            "specache_score", "specache_select_gather", "specache_append_score",
            "specache_attend", "specache_score_attend", "specache_append_score_attend", "specache_decode_step", "specache_attend_static", "specache_debug_poison_slot", "specache_debug_fail_alloc", "specache_debug_scored_by_word", "specache_order_by_events", "specache_debug_kernel_choice", "specache_debug_merger_polls", "specache_export_quantized", "specache_export_rows", "specache_debug_logits",
-           "specache_timing", "specache_measure_hbm_read", "specache_measure_link"]
+           "specache_timing", "specache_measure_hbm_read", "specache_measure_link",
+           "specache_rotary_plan", "specache_rotate", "specache_window_scratch", "specache_window_attend",
+           "specache_sample_scratch", "specache_sample"]
 
 
 class Config(C.Structure):
@@ -27,6 +29,33 @@ class Config(C.Structure):
                                          "group", "residual", "max_seq", "topk", "dtype")] + [("sm_scale", C.c_float),
                                                                                  ("one_bit_form", C.c_int32), ("select_form", C.c_int32),
                                                                                  ("select_cache", C.c_int32), ("async_select", C.c_int32)]
+
+
+class View(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("batch", C.c_int64), ("head", C.c_int64), ("token", C.c_int64)]
+
+
+ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
+ROTARY_UNSCALED, ROTARY_LINEAR, ROTARY_BASE, ROTARY_BANDS, ROTARY_RAMP = range(5)
+FP32 = 2   # a type of logits only
+
+
+class RotaryConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rotary_dim", "layout", "scaling", "original_tokens")] + \
+               [(n, C.c_double) for n in ("base", "factor", "low", "high", "gain")]
+
+
+class Rotary(C.Structure):
+    _fields_ = [("turns", C.c_uint64 * 64), ("gain", C.c_float), ("rotary_dim", C.c_int32), ("layout", C.c_int32)]
+
+
+class WindowConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "n_q_heads", "n_kv_heads", "head_dim", "q_tokens", "kv_tokens", "window", "sinks",
+                                         "dtype")] + [("sm_scale", C.c_float)]
+
+
+class SampleConfig(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("vocab", C.c_int32), ("dtype", C.c_int32), ("row_stride", C.c_int64)]
 
 
 class SpeCacheError(RuntimeError):
@@ -80,6 +109,13 @@ def lib():
         L.specache_timing.argtypes = [vp, i32, vp, vp]
         L.specache_measure_hbm_read.argtypes = [C.c_int64, i32, C.POINTER(C.c_double)]
         L.specache_measure_link.argtypes = [C.c_int64, i32, C.POINTER(C.c_double), C.POINTER(C.c_double)]
+        view, i64 = C.POINTER(View), C.c_int64
+        L.specache_rotary_plan.argtypes = [C.POINTER(RotaryConfig), C.POINTER(Rotary)]
+        L.specache_rotate.argtypes = [C.POINTER(Rotary), i32, i32, i32, i32, view, view, i32, view, view, view, view, vp, i32, vp]
+        L.specache_window_scratch.argtypes = [C.POINTER(WindowConfig), C.POINTER(i64)]
+        L.specache_window_attend.argtypes = [C.POINTER(WindowConfig), view, view, view, view, vp, vp, vp, i64, vp]
+        L.specache_sample_scratch.argtypes = [C.POINTER(SampleConfig), C.POINTER(i64)]
+        L.specache_sample.argtypes = [C.POINTER(SampleConfig), vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
         for name in EXPORTS:
             if name != "specache_last_error":
                 getattr(L, name).restype = C.c_int
@@ -154,6 +190,130 @@ def measure_link(nbytes=256 << 20, reps=5):
     if rc != OK:
         raise SpeCacheError(rc, "measure_link failed")
     return a.value, b.value
+
+
+# ---- calls without a context: torch tensors, strided where the C call takes views ------------------------------------
+
+def _done(rc):
+    if rc != OK:
+        raise SpeCacheError(rc, lib().specache_last_error(None).decode())
+
+
+def _refuse(what):
+    raise SpeCacheError(EINVAL, what)
+
+
+_TYPES = {}
+
+
+def _type_of(t):
+    if not _TYPES:
+        import torch
+        _TYPES.update({torch.float16: FP16, torch.bfloat16: BF16, torch.float32: FP32})
+    return _TYPES.get(t.dtype, -1)
+
+
+def _here():
+    import torch
+    return torch.cuda.current_device()
+
+
+def _view(t, shape, dtype, device, name):
+    """The specache_view of a [batch, heads, tokens, 128] tensor on the current device, the channels side by side."""
+    if t.shape != shape or _type_of(t) != dtype or t.get_device() != device:
+        _refuse(f"{name} must be a {tuple(shape)} tensor of q's type on the current device")
+    b, h, n, c = t.stride()
+    if c != 1:
+        _refuse(f"{name}: the channels must lie side by side")
+    return View(t.data_ptr(), b if shape[0] > 1 else 0, h if shape[1] > 1 else 0, n if shape[2] > 1 else 0)   # (any stride goes with one)
+
+
+def _flat(t, shape, kind, device, name):
+    """Address of a contiguous tensor of the given shape and type on the current device, or None."""
+    if t is None:
+        return None
+    if t.shape != shape or str(t.dtype) != kind or t.get_device() != device or not t.is_contiguous():
+        _refuse(f"{name} must be a contiguous {tuple(shape)} tensor of {kind} on the current device")
+    return t.data_ptr()
+
+
+def _scratch(t, device):
+    if t is None:
+        return None, 0
+    if t.get_device() != device or not t.is_contiguous():
+        _refuse("scratch must be contiguous and on the current device")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def rotary_plan(rotary_dim=128, base=10000.0, layout=ROTARY_HALF, scaling=ROTARY_UNSCALED, factor=1.0, original_tokens=0,
+                low=0.0, high=0.0, gain=0.0):
+    """A worked-out rotary configuration for rotate (host only)."""
+    out = Rotary()
+    _done(lib().specache_rotary_plan(C.byref(RotaryConfig(rotary_dim, layout, scaling, original_tokens, base, factor, low, high, gain)),
+                                     C.byref(out)))
+    return out
+
+
+def rotate(plan, q, q_out, k=None, k_out=None, v=None, v_out=None, positions=None, first_position=0, stream=None):
+    """q [B, Hq, n, 128] and k [B, Hkv, n, 128] turned by their positions, v as it is, each into its output, in one launch."""
+    B, Hq, n, _ = q.shape
+    Hkv = 0 if k is None and v is None else (v if k is None else k).shape[1]
+    dtype, device = _type_of(q), _here()
+    views = []
+    for name, t, out, heads in (("q", q, q_out, Hq), ("k", k, k_out, Hkv), ("v", v, v_out, Hkv)):
+        if (t is None) != (out is None):
+            _refuse(f"{name} and {name}_out are given or left out together")
+        for x in (t, out):
+            views.append(None if x is None else C.byref(_view(x, (B, heads, n, 128), dtype, device, name)))
+    _done(lib().specache_rotate(C.byref(plan), dtype, B, n, Hq, views[0], views[1], Hkv, *views[2:],
+                                _flat(positions, (B, n), "torch.int32", device, "positions"), first_position, _stream(stream)))
+
+
+def window_scratch(batch, n_q_heads, n_kv_heads, q_tokens, kv_tokens, window=0, sinks=0):
+    """Bytes of scratch memory that window_attend needs for these counts (0: none)."""
+    out = C.c_int64()
+    _done(lib().specache_window_scratch(C.byref(WindowConfig(batch, n_q_heads, n_kv_heads, 128, q_tokens, kv_tokens, window, sinks)),
+                                        C.byref(out)))
+    return out.value
+
+
+def window_attend(q, k, v, out, window=0, sinks=0, q_lengths=None, kv_lengths=None, sm_scale=0.0, scratch=None, stream=None):
+    """Attention of q [B, Hq, n, 128] over k, v [B, Hkv, N, 128] with a sliding window and sinks, into out (q's shape)."""
+    B, Hq, n, _ = q.shape
+    Hkv, N = k.shape[1], k.shape[2]
+    dtype, device = _type_of(q), _here()
+    cfg = WindowConfig(B, Hq, Hkv, 128, n, N, window, sinks, dtype, sm_scale)
+    rows, pairs = (B, Hq, n, 128), (B, Hkv, N, 128)
+    address, size = _scratch(scratch, device)
+    _done(lib().specache_window_attend(C.byref(cfg), C.byref(_view(q, rows, dtype, device, "q")), C.byref(_view(k, pairs, dtype, device, "k")),
+                                       C.byref(_view(v, pairs, dtype, device, "v")), C.byref(_view(out, rows, dtype, device, "out")),
+                                       _flat(q_lengths, (B,), "torch.int32", device, "q_lengths"),
+                                       _flat(kv_lengths, (B,), "torch.int32", device, "kv_lengths"), address, size, _stream(stream)))
+
+
+def sample_scratch(rows, vocab, dtype):
+    """Bytes of scratch memory that sample needs (0: none); dtype: the logits' torch type or FP16, BF16, FP32."""
+    if not isinstance(dtype, int):
+        import torch
+        dtype = _type_of(torch.empty(0, dtype=dtype))
+    out = C.c_int64()
+    _done(lib().specache_sample_scratch(C.byref(SampleConfig(rows, vocab, dtype, vocab)), C.byref(out)))
+    return out.value
+
+
+def sample(logits, u, tokens, temperature=None, top_k=None, top_p=None, min_p=None, scratch=None, stream=None):
+    """tokens[r] from logits [rows, vocab] (rows may lie apart) and the random numbers u [rows]."""
+    R, V = logits.shape
+    device = _here()
+    if logits.get_device() != device or (V > 1 and logits.stride(1) != 1):
+        _refuse("logits must be on the current device, a row's side by side")
+    cfg = SampleConfig(R, V, _type_of(logits), logits.stride(0) if R > 1 else V)
+    f32, i32, shape = "torch.float32", "torch.int32", (R,)
+    address, size = _scratch(scratch, device)
+    _done(lib().specache_sample(C.byref(cfg), logits.data_ptr(), _flat(u, shape, f32, device, "u"),
+                                _flat(temperature, shape, f32, device, "temperature"), _flat(top_k, shape, i32, device, "top_k"),
+                                _flat(top_p, shape, f32, device, "top_p"), _flat(min_p, shape, f32, device, "min_p"),
+                                _flat(tokens, shape, i32, device, "tokens"), address, size, _stream(stream)))
 
 
 class SpeCache:

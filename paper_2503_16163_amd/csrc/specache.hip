@@ -14,6 +14,7 @@
 
 #include "kernels.h"
 #include "layout.h"
+#include "operators.h"
 #include "rows_args.h"
 #include <cstdlib>
 
@@ -388,6 +389,16 @@ int static_scratch_of_current_device(specache_ctx* ctx, float** out) {
 }
 
 }  // namespace
+
+namespace specache {
+int fail_without_context(int code, const char* msg) noexcept {
+    try {
+        return fail(nullptr, code, msg);
+    } catch (...) {   // no memory for the message
+        return code;
+    }
+}
+}  // namespace specache
 
 extern "C" {
 

@@ -1,0 +1,206 @@
+"""specache_window_attend against the definition in 64 bits, row by row.
+
+Tolerance of an output channel, with A = sum_j p_j |v_j| (p the exact weights) and h half a step of the type: the weights' rounding
+h A, the final one h |o|; a score is off by the binary32 sum of 128 products, 2^-17 of sum |q||k| sm_scale at most, which the
+exponential turns into twice that (numerator and sum) of A; the exponential, the binary32 sums and the rescaling 2^-16 A.  In binary16 weights below 2^-14
+of the largest are off by up to 2^-25 absolute: that times the sum of |v| seen."""
+import math
+
+import pytest
+import torch
+
+from paper_2503_16163_amd import binding
+
+pytestmark = pytest.mark.gpu
+
+
+def _reference(q, k, v, window, sinks, n_of, N_of, scale):
+    """(outputs, tolerance) in 64 bits; rows behind a sequence's queries are NaN."""
+    B, Hq, n_all, _ = q.shape
+    G = Hq // k.shape[1]
+    half = torch.finfo(q.dtype).eps / 2
+    out = torch.full(q.shape, math.nan, device=q.device, dtype=torch.float64)
+    tol = torch.zeros(q.shape, device=q.device, dtype=torch.float64)
+    for b in range(B):
+        n, N = n_of[b], N_of[b]
+        if n == 0:
+            continue
+        p = N - n + torch.arange(n, device=q.device)[:, None]
+        j = torch.arange(N, device=q.device)[None]
+        seen = j <= p
+        if window:
+            seen &= (j < sinks) | (p - j < window)
+        for h in range(Hq):
+            K, V, Q = k[b, h // G, :N].double(), v[b, h // G, :N].double(), q[b, h, :n].double()
+            if N == 0:
+                out[b, h, :n] = 0
+                continue
+            x = torch.where(seen, Q @ K.t() * scale, -math.inf)
+            most = x.amax(dim=1, keepdim=True)
+            w = torch.where(seen, (x - torch.where(most == -math.inf, 0.0, most)).exp(), 0.0)
+            total = w.sum(dim=1, keepdim=True)
+            w = torch.where(total > 0, w / total, 0.0)
+            o, A = torch.empty_like(Q), torch.empty_like(Q)
+            if bool(torch.isfinite(V).all()) and bool(torch.isfinite(w).all()):
+                o, A = w @ V, w @ V.abs()
+            else:
+                for i in range(n):
+                    s = seen[i]
+                    o[i] = (w[i, s][:, None] * V[s]).sum(dim=0)
+                    A[i] = (w[i, s][:, None] * V[s].abs()).sum(dim=0)
+            size = torch.where(seen, Q.abs() @ K.abs().t() * scale, 0.0).nan_to_num(0, 0, 0).amax(dim=1, keepdim=True)
+            t = A * (half + 2 * 2.0 ** -17 * size + 2.0 ** -16) + half * o.abs()
+            if q.dtype == torch.float16:
+                t = t + 2.0 ** -25 * (1 + seen.double() @ V.abs().nan_to_num(0, 0, 0))
+            out[b, h, :n], tol[b, h, :n] = o, t
+    return out, tol
+
+
+def _lengths(x, B, most):
+    return [most] * B if x is None else x
+
+
+def _run(q, k, v, window=0, sinks=0, n_of=None, N_of=None, sm_scale=0.0, out=None, stream=None):
+    out = torch.full(q.shape, 7.0, device="cuda", dtype=q.dtype) if out is None else out
+    need = binding.window_scratch(q.shape[0], q.shape[1], k.shape[1], q.shape[2], k.shape[2], window, sinks)
+    scratch = torch.full((need,), 255, dtype=torch.uint8, device="cuda") if need else None
+    as_device = lambda x: None if x is None else torch.tensor(x, dtype=torch.int32, device="cuda")
+    binding.window_attend(q, k, v, out, window, sinks, as_device(n_of), as_device(N_of), sm_scale, scratch, stream)
+    return out
+
+
+def _check(q, k, v, window=0, sinks=0, n_of=None, N_of=None, sm_scale=0.0):
+    B = q.shape[0]
+    got = _run(q, k, v, window, sinks, n_of, N_of, sm_scale)
+    e, tol = _reference(q, k, v, window, sinks, _lengths(n_of, B, q.shape[2]), _lengths(N_of, B, k.shape[2]), sm_scale or 1 / math.sqrt(128))
+    asked = torch.zeros(q.shape, dtype=torch.bool, device="cuda")
+    for b, n in enumerate(_lengths(n_of, B, q.shape[2])):
+        asked[b, :, :n] = True
+    assert bool((got[~asked] == 7.0).all()), "rows behind the queries were written"
+    finite = asked & torch.isfinite(e)
+    assert bool((~torch.isfinite(got))[asked & ~torch.isfinite(e)].all())
+    off = ((got.double() - e).abs() - tol)[finite]
+    assert bool(torch.isfinite(got[finite]).all()) and (off.numel() == 0 or off.max().item() <= 0), off.max().item()
+    return got
+
+
+def _inputs(seed, B, Hq, Hkv, n, N, dtype, big=1.0):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    make = lambda *s: torch.randn(s, generator=gen, device="cuda", dtype=torch.float32)
+    return (make(B, Hq, n, 128) * big).to(dtype), make(B, Hkv, N, 128).to(dtype), make(B, Hkv, N, 128).to(dtype)
+
+
+SHAPES = [  # B, Hq, Hkv, n, N, window, sinks
+    (1, 1, 1, 1, 1, 0, 0), (2, 2, 1, 1, 63, 0, 0), (1, 4, 4, 1, 64, 5, 2), (3, 8, 2, 1, 65, 64, 0), (2, 8, 1, 2, 129, 0, 0), (1, 3, 1, 3, 200, 1, 0),
+    (1, 32, 8, 2, 5003, 0, 0), (2, 8, 8, 1, 5000, 1000, 4), (1, 64, 1, 1, 2500, 0, 0), (1, 16, 2, 4, 9000, 777, 70), (4, 2, 2, 2, 20000, 0, 0),
+    (1, 1, 1, 2, 2, 0, 0), (1, 2, 2, 31, 31, 0, 0), (2, 4, 2, 64, 64, 0, 0), (1, 5, 5, 65, 65, 0, 0), (1, 6, 2, 129, 129, 1, 0), (1, 2, 1, 200, 200, 64, 0),
+    (2, 3, 3, 257, 257, 65, 1), (1, 4, 1, 300, 300, 100, 64), (1, 2, 2, 513, 513, 200, 600), (1, 7, 1, 150, 150, 0, 0), (1, 8, 4, 700, 700, 33, 130),
+    (1, 4, 2, 20, 500, 0, 0), (2, 2, 2, 100, 1000, 300, 5), (1, 8, 1, 33, 3000, 0, 0), (1, 8, 2, 256, 4096, 0, 0), (1, 2, 2, 40, 7, 0, 0), (1, 2, 1, 200, 100, 30, 2),
+]
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("B,Hq,Hkv,n,N,window,sinks", SHAPES)
+def test_window_attend(B, Hq, Hkv, n, N, window, sinks, dtype):
+    q, k, v = _inputs(n * 7 + N, B, Hq, Hkv, n, N, dtype)
+    _check(q, k, v, window, sinks)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("n,N,n_of,N_of,window,sinks", [
+    (1, 700, [1, 0, 1, 1], [700, 5, 0, 1], 0, 0), (2, 9000, [2, 1, 2, 0], [9000, 64, 1, 77], 0, 0), (2, 9000, [2, 2, 1, 2], [8999, 4100, 65, 129], 500, 4),
+    (260, 260, [260, 1, 0, 131], [260, 1, 0, 131], 0, 0), (260, 260, [64, 65, 128, 129], [260, 65, 200, 129], 60, 3), (150, 400, [150, 20, 150, 3], [400, 10, 150, 399], 90, 0),
+    (3, 5000, [3, 3, 3, 3], [0, 1, 2, 5000], 0, 0)])
+def test_ragged_batches(n, N, n_of, N_of, window, sinks, dtype):
+    """Lengths of zero, fewer cached tokens than queries, rows and positions behind the lengths that hold NaN."""
+    q, k, v = _inputs(n + N, 4, 8, 2, n, N, dtype)
+    for b in range(4):
+        q[b, :, n_of[b]:] = math.nan
+        k[b, :, N_of[b]:] = math.nan
+        v[b, :, N_of[b]:] = math.inf
+    _check(q, k, v, window, sinks, n_of, N_of)
+
+
+def test_lengths_are_held_to_the_tensors():
+    q, k, v = _inputs(5, 3, 2, 2, 4, 100, torch.float16)
+    got = _run(q, k, v, n_of=[9, -3, 4], N_of=[1000, 50, -1])
+    want = _run(q, k, v, n_of=[4, 0, 4], N_of=[100, 50, 0])
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("n,N,window,sinks", [(200, 200, 0, 0), (200, 200, 50, 4), (3, 3000, 900, 2), (70, 2000, 0, 0)])
+def test_values_that_are_not_finite_reach_the_rows_that_see_them_alone(n, N, window, sinks, dtype):
+    q, k, v = _inputs(n, 1, 4, 2, n, N, dtype)
+    v[0, 0, N - n // 2 - 1, 3] = math.nan
+    v[0, 1, N - 1, 100] = math.inf
+    v[0, 1, 0, 7] = -math.inf
+    _check(q, k, v, window, sinks)
+    k2 = k.clone()
+    k2[0, 1, N - 1] = math.nan
+    clean, odd = _run(q, k, v.nan_to_num(0, 0, 0), window, sinks), _run(q, k2, v.nan_to_num(0, 0, 0), window, sinks)
+    assert torch.equal(clean[:, :2], odd[:, :2]) and torch.equal(clean[:, :, :n - 1], odd[:, :, :n - 1]) and bool(torch.isnan(odd[:, 2:, n - 1]).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_scores_over_the_whole_range(dtype):
+    """Weights from all on one position to all alike, a scale of the caller's, the largest scores last (the running maximum moves with every tile)."""
+    q, k, v = _inputs(11, 1, 2, 2, 90, 900, dtype, big=20.0)
+    _check(q, k, v, 0, 0)
+    _check(q, k, v, 100, 3, sm_scale=0.003)
+    q, k, v = _inputs(12, 1, 2, 1, 2, 4000, dtype)
+    k[:] = q[:, :1, :1] * torch.linspace(0, 4, 4000, device="cuda")[None, None, :, None].to(dtype)
+    _check(q, k, v, 0, 0)
+    _check(q, torch.zeros_like(k), v, 300, 2)
+
+
+def test_strides_and_in_place():
+    """A fused projection as q, k and v, the output over q, a batch that shares its keys."""
+    x = torch.randn((2, 130, 8 + 2 + 2, 128), device="cuda", dtype=torch.bfloat16)
+    q, k, v = (t.transpose(1, 2) for t in (x[:, :, :8], x[:, :, 8:10], x[:, :, 10:]))
+    want = _check(q, k, v, 50, 3)
+    assert torch.equal(_run(q, k, v, 50, 3, out=q), want)
+    q, k, v = _inputs(3, 1, 4, 2, 3, 3000, torch.float16)
+    many = q.repeat(3, 1, 1, 1)
+    got = _run(many, k.expand(3, -1, -1, -1), v.expand(3, -1, -1, -1))
+    want = _run(many, k.repeat(3, 1, 1, 1), v.repeat(3, 1, 1, 1))
+    assert torch.equal(got, want)
+
+
+def test_caches_beyond_32_bit_offsets():
+    flat = torch.empty((6000 << 20) + 256, device="cuda", dtype=torch.float16)   # 6000 tokens of 2^20 elements: 12.6 GB
+    q, k, v = _inputs(8, 1, 2, 1, 2, 6000, torch.float16)
+    far_k, far_v = flat.as_strided((1, 1, 6000, 128), (0, 0, 1 << 20, 1)), flat.as_strided((1, 1, 6000, 128), (0, 0, 1 << 20, 1), 128)
+    far_k.copy_(k)
+    far_v.copy_(v)
+    assert torch.equal(_run(q, far_k, far_v, 0, 0), _run(q, k, v, 0, 0))
+    q, _, _ = _inputs(9, 1, 2, 1, 130, 6000, torch.float16)
+    assert torch.equal(_run(q, far_k, far_v, 2000, 9), _run(q, k, v, 2000, 9))
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,n,N,window", [(2, 8, 2, 2, 9000, 0), (1, 4, 4, 300, 300, 70)])
+def test_captured_overlapping_and_the_same_every_time(B, Hq, Hkv, n, N, window):
+    """Two graphs with scratch memory of their own, replayed on two streams at a time between eager calls."""
+    sets = []
+    for i in range(2):
+        q, k, v = _inputs(20 + i, B, Hq, Hkv, n, N, torch.bfloat16)
+        need = binding.window_scratch(B, Hq, Hkv, n, N, window, 4)
+        s = dict(q=q, k=k, v=v, out=torch.zeros_like(q), scratch=torch.empty(need, dtype=torch.uint8, device="cuda") if need else None,
+                 N=torch.full((B,), N, dtype=torch.int32, device="cuda"), stream=torch.cuda.Stream(), graph=torch.cuda.CUDAGraph())
+        torch.cuda.synchronize()
+        with torch.cuda.graph(s["graph"], stream=s["stream"]):
+            binding.window_attend(q, k, v, s["out"], window, 4, None, s["N"], 0.0, s["scratch"], torch.cuda.current_stream())
+        sets.append(s)
+    for turn in range(3):
+        for s in sets:
+            s["q"].copy_(torch.randn_like(s["q"]))
+            s["N"].fill_(N - 13 * turn)
+        want = [_run(s["q"], s["k"], s["v"], window, 4, N_of=s["N"].tolist()) for s in sets]
+        torch.cuda.synchronize()
+        for s in sets:
+            with torch.cuda.stream(s["stream"]):
+                s["graph"].replay()
+        torch.cuda.synchronize()
+        for s, w in zip(sets, want):
+            assert torch.equal(s["out"], w)
