@@ -75,19 +75,25 @@ __device__ __forceinline__ void fetch_tile(const uint16_t* base, int64_t stride,
     }
 }
 
+template <bool BF16> constexpr uint32_t kExponents = BF16 ? 0x7F807F80u : 0x7C007C00u;        // of two values: all ones where one is not finite
+template <bool BF16> constexpr uint32_t kAboveExponents = BF16 ? 0x00800080u : 0x04000400u;   // added to them, it then sets the sign's bit
+
 // What a row of queries sees: positions up to `last`, of these the sinks and those from `low` on.
 struct Seen {
     int last, low, sinks;
-    __device__ __forceinline__ bool operator()(int j) const { return j <= last && (j < sinks || j >= low); }
+    __device__ __forceinline__ bool operator()(int j) const { return (j <= last) & ((j < sinks) | (j >= low)); }
 };
 
 template <bool BF16, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void window_kernel(WindowArgs a) {
-    __shared__ __align__(1024) char keys[2][kTileBytes];
-    __shared__ __align__(1024) char values[2][kTileBytes];
-    __shared__ int odd_tile[2];       // a tile of the buffer that has values which are not finite
+    // (arrays of their own: the compiler then sees that what is fetched into one and what is read from another do not meet)
+    __shared__ __align__(1024) char keys_even[kTileBytes];
+    __shared__ __align__(1024) char keys_odd[kTileBytes];
+    __shared__ __align__(1024) char values_even[kTileBytes];
+    __shared__ __align__(1024) char values_odd[kTileBytes];
+    __shared__ int any_dropped;
 
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, half = lane / 32;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
     // the row tiles of a KV head follow each other on one XCD, the longest first
     const int total = gridDim.x, per_xcd = total / 8, rest = total % 8, xcd = blockIdx.x % 8;
     const int id = xcd * per_xcd + min(xcd, rest) + blockIdx.x / 8;
@@ -146,36 +152,48 @@ __global__ __launch_bounds__(256, 2) void window_kernel(WindowArgs a) {
         for (int i = 0; i < 16; ++i) o[dt][i] = 0.0f;
     float m = kNever, l = 0.0f;       // l: of this lane's half of the positions
 
-    if (threadIdx.x < 2) odd_tile[threadIdx.x] = -1;
+    if (threadIdx.x == 0) any_dropped = 0;
     __syncthreads();
     if (i_begin < i_end) {
-        fetch_tile<true>(kbase, a.k.token, tile_at(i_begin) * kTile, N - 1, keys[0], wave, lane);
-        fetch_tile<false>(vbase, a.v.token, tile_at(i_begin) * kTile, N - 1, values[0], wave, lane);
+        fetch_tile<true>(kbase, a.k.token, tile_at(i_begin) * kTile, N - 1, keys_even, wave, lane);
+        fetch_tile<false>(vbase, a.v.token, tile_at(i_begin) * kTile, N - 1, values_even, wave, lane);
     }
-    for (int it = i_begin; it < i_end; ++it) {
-        const int buf = (it - i_begin) & 1;
+    const auto is_edge = [&](int tile0) {   // some row of the workgroup does not see all of the tile
+        return tile0 + kTile - 1 > first_pos || (a.window && tile0 < last_pos - a.window + 1 && tile0 + kTile > a.sinks);
+    };
+    const auto step = [&](int it, char* keys, char* values, char* next_keys, char* next_values) {
         const int tile0 = tile_at(it) * kTile;
         __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
-        const bool edge = tile0 + kTile - 1 > first_pos || (a.window && tile0 < last_pos - a.window + 1 && tile0 + kTile > a.sinks);
-        if (edge) {
-            // rows that do not see a value have it times zero: looked for here, where it matters, by the wave that fetched it
-            uint32_t odd = 0;
-            const uint4v* own = (const uint4v*)(values[buf] + wave * 16 * kD * 2);
+        if (is_edge(tile0)) {
+            // A row that does not see a value has it times zero, so values that are not finite are dropped here, by the wave that
+            // fetched them, and given to the rows that see them after the walk.
+            uint4v* own = (uint4v*)(values + wave * 16 * kD * 2);
+            bool dropped = false;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint4v x = own[i * 64 + lane];
+                uint4v x = own[i * 64 + lane];
+                uint32_t odd = 0;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) odd |= (x[e] & (BF16 ? 0x7F807F80u : 0x7C007C00u)) + (BF16 ? 0x00800080u : 0x04000400u);
+                for (int e = 0; e < 4; ++e) odd |= (x[e] & kExponents<BF16>) + kAboveExponents<BF16>;
+                if (odd & 0x80008000u) {
+                    dropped = true;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t y = (x[e] & kExponents<BF16>) + kAboveExponents<BF16>;
+                        x[e] &= (y & 0x8000u ? 0u : 0xFFFFu) | (y & 0x80000000u ? 0u : 0xFFFF0000u);
+                    }
+                    own[i * 64 + lane] = x;
+                }
             }
-            if (odd & 0x80008000u) odd_tile[buf] = tile0;
+            if (dropped) any_dropped = 1;
         }
         __syncthreads();
         if (it + 1 < i_end) {
-            fetch_tile<true>(kbase, a.k.token, tile_at(it + 1) * kTile, N - 1, keys[buf ^ 1], wave, lane);
-            fetch_tile<false>(vbase, a.v.token, tile_at(it + 1) * kTile, N - 1, values[buf ^ 1], wave, lane);
+            fetch_tile<true>(kbase, a.k.token, tile_at(it + 1) * kTile, N - 1, next_keys, wave, lane);
+            fetch_tile<false>(vbase, a.v.token, tile_at(it + 1) * kTile, N - 1, next_values, wave, lane);
         }
         // none of the wave's rows sees the tile
-        if (tile0 > wave_last || (tile0 + kTile <= wave_first_low && tile0 >= a.sinks)) continue;
+        if (tile0 > wave_last || (tile0 + kTile <= wave_first_low && tile0 >= a.sinks)) return;
 
         float16v s[2];
 #pragma unroll
@@ -185,12 +203,11 @@ __global__ __launch_bounds__(256, 2) void window_kernel(WindowArgs a) {
             const int row = 32 * hf + lane % 32;
 #pragma unroll
             for (int kk = 0; kk < 8; ++kk) {
-                const uint4v kf = *(const uint4v*)(keys[buf] + row * kD * 2 + (((2 * kk + half) ^ key_swizzle(row)) * 16));
+                const uint4v kf = *(const uint4v*)(keys + row * kD * 2 + (((2 * kk + half) ^ key_swizzle(row)) * 16));
                 s[hf] = mfma32<BF16>(kf, qf[kk], s[hf]);
             }
         }
-        const bool wave_edge = tile0 + kTile - 1 > wave_first || (tile0 < wave_low && tile0 + kTile > a.sinks);
-        if (wave_edge) {
+        if (tile0 + kTile - 1 > wave_first || (tile0 < wave_low && tile0 + kTile > a.sinks)) {
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
@@ -220,48 +237,40 @@ __global__ __launch_bounds__(256, 2) void window_kernel(WindowArgs a) {
         }
         // the 4 x 4 block of a lane group: position 4 half + (lane % 16) / 4, channels 16 (lane / 16 % 2) + 4 (lane % 4)
         const int vr = 4 * half + lane % 16 / 4, vc = 16 * (lane / 16 % 2) + 4 * (lane % 4);
-        const auto value_operand = [&](int step, int dt) {
-            uint4v f;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int row = 16 * step + 8 * j + vr, col = 32 * dt + vc;
-                const char* at = values[buf] + row * kD * 2 + ((col / 8) ^ value_swizzle(row)) * 16 + col % 8 * 2;
-                const uint2v w = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)at));
-                f[2 * j] = w[0];
-                f[2 * j + 1] = w[1];
-            }
-            return f;
-        };
-        if (wave_edge && odd_tile[buf] == tile0) {
-            // row by row, without the values that the row does not see
-#pragma unroll 1
-            for (int c = 0; c < 32; ++c) {
-                Seen its = seen;
-                its.last = __builtin_amdgcn_readlane(seen.last, c);
-                its.low = __builtin_amdgcn_readlane(seen.low, c);
+        for (int st = 0; st < 4; ++st)
 #pragma unroll
-                for (int dt = 0; dt < 4; ++dt) {
-                    float16v t;
+            for (int dt = 0; dt < 4; ++dt) {
+                uint4v f;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) t[i] = 0.0f;
-#pragma unroll
-                    for (int step = 0; step < 4; ++step) {
-                        uint4v f = value_operand(step, dt);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (!its(tile0 + 16 * step + 8 * (e / 4) + 4 * half + e % 4)) f[e / 2] &= e % 2 ? 0x0000FFFFu : 0xFFFF0000u;
-                        t = mfma32<BF16>(f, p[step], t);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[dt][i] = lane % 32 == c ? o[dt][i] + t[i] : o[dt][i];
+                for (int j = 0; j < 2; ++j) {
+                    const int row = 16 * st + 8 * j + vr, col = 32 * dt + vc;
+                    const char* at = values + row * kD * 2 + ((col / 8) ^ value_swizzle(row)) * 16 + col % 8 * 2;
+                    const uint2v w = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)at));
+                    f[2 * j] = w[0];
+                    f[2 * j + 1] = w[1];
                 }
+                o[dt] = mfma32<BF16>(f, p[st], o[dt]);
             }
-            continue;
+    };
+    for (int it = i_begin; it < i_end; it += 2) {
+        step(it, keys_even, values_even, keys_odd, values_odd);
+        if (it + 1 < i_end) step(it + 1, keys_odd, values_odd, keys_even, values_even);
+    }
+    __syncthreads();
+    if (any_dropped) {
+        for (int it = i_begin; it < i_end; ++it) {
+            const int tile0 = tile_at(it) * kTile;
+            if (!is_edge(tile0)) continue;
+            for (int j = tile0; j < min(tile0 + kTile, N); ++j)
+#pragma unroll
+                for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const uint32_t x = vbase[j * a.v.token + 32 * dt + 8 * (i / 4) + 4 * half + i % 4];
+                        if ((x & kExponents<BF16> & 0xFFFFu) == (kExponents<BF16> & 0xFFFFu) && seen(j)) o[dt][i] += widen16<BF16>(x);
+                    }
         }
-#pragma unroll
-        for (int step = 0; step < 4; ++step)
-#pragma unroll
-            for (int dt = 0; dt < 4; ++dt) o[dt] = mfma32<BF16>(value_operand(step, dt), p[step], o[dt]);
     }
 
     l += other_half(l);
