@@ -528,7 +528,8 @@ typedef struct specache_window_config {
 int specache_window_scratch(const specache_window_config* cfg, int64_t* bytes);
 
 /*
- * q, out: [batch, n_q_heads, q_tokens] rows; k, v: [batch, n_kv_heads, kv_tokens] rows (q and out may have the same view).
+ * q, out: [batch, n_q_heads, q_tokens] rows; k, v: [batch, n_kv_heads, kv_tokens] rows, at most 2^24 elements from token to token
+ * (q and out may have the same view).
  * q_lengths, kv_lengths: device int32 [batch], the n and N of every sequence, held to 0 .. q_tokens and 0 .. kv_tokens;
  * NULL: q_tokens and kv_tokens.  Rows of q and out from n on and rows of k and v from N on are neither read nor written.
  * Scores, softmax and sums are binary32; the weights are rounded to dtype for their product with v, the output once.  A value

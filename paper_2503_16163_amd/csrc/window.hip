@@ -63,17 +63,38 @@ __device__ __forceinline__ int key_swizzle(int r) { return r & 15; }
 __device__ __forceinline__ int value_swizzle(int r) { return (r & 3) << 2 | (r >> 2 & 1) << 1; }
 
 // One wave's quarter of a tile of keys or values: 16 positions, four at a time.  The LDS side is in order of lanes, so the pieces are
-// exchanged on the way from memory.  Positions from `last` on are that one again (never seen, but finite if it is).
+// exchanged on the way from memory.
 template <bool KEYS>
-__device__ __forceinline__ void fetch_tile(const uint16_t* base, int64_t stride, int first, int last, char* lds, int wave, int lane) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = 16 * wave + 4 * i + lane / 16;
-        const int piece = (lane % 16) ^ (KEYS ? key_swizzle(r) : value_swizzle(r));
-        const int at = min(first + r, last);
-        __builtin_amdgcn_global_load_lds((global_void*)(base + at * stride + piece * 8), (lds_void*)(lds + (16 * wave + 4 * i) * kD * 2), 16, 0, 0);
+struct Fetch {
+    const uint16_t* base;             // position 0 of the head
+    int64_t stride;
+    uint32_t at[4];                   // bytes from the tile's first position to this lane's pieces
+    int wave, lane;
+    __device__ __forceinline__ int position(int i) const { return 16 * wave + 4 * i + lane / 16; }
+    __device__ __forceinline__ uint32_t piece(int i) const {
+        const int r = position(i);
+        return ((lane % 16) ^ (KEYS ? key_swizzle(r) : value_swizzle(r))) * 16;
     }
-}
+    __device__ __forceinline__ void start() {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) at[i] = (uint32_t)position(i) * (uint32_t)stride * 2 + piece(i);
+    }
+    // Positions from `last` on are that one again (no row sees them, but they are finite if it is).
+    __device__ __forceinline__ void operator()(int first, int last, char* lds) const {
+        const char* tile = (const char*)(base + first * stride);
+        if (first + kTile - 1 <= last) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                __builtin_amdgcn_global_load_lds((global_void*)(tile + at[i]), (lds_void*)(lds + (16 * wave + 4 * i) * kD * 2), 16, 0, 0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t r = min(position(i), last - first);
+                __builtin_amdgcn_global_load_lds((global_void*)(tile + (r * (uint32_t)stride * 2 + piece(i))), (lds_void*)(lds + (16 * wave + 4 * i) * kD * 2), 16, 0, 0);
+            }
+        }
+    }
+};
 
 template <bool BF16> constexpr uint32_t kExponents = BF16 ? 0x7F807F80u : 0x7C007C00u;        // of two values: all ones where one is not finite
 template <bool BF16> constexpr uint32_t kAboveExponents = BF16 ? 0x00800080u : 0x04000400u;   // added to them, it then sets the sign's bit
@@ -142,8 +163,10 @@ __global__ __launch_bounds__(256, 2) void window_kernel(WindowArgs a) {
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk) qf[kk] = *(const uint4v*)(qrow + 16 * kk + 8 * half);
     }
-    const uint16_t* kbase = (const uint16_t*)a.k.data + b * a.k.batch + h * a.k.head;
-    const uint16_t* vbase = (const uint16_t*)a.v.data + b * a.v.batch + h * a.v.head;
+    Fetch<true> fetch_keys{(const uint16_t*)a.k.data + b * a.k.batch + h * a.k.head, a.k.token, {}, wave, lane};
+    Fetch<false> fetch_values{(const uint16_t*)a.v.data + b * a.v.batch + h * a.v.head, a.v.token, {}, wave, lane};
+    fetch_keys.start();
+    fetch_values.start();
 
     float16v o[4];
 #pragma unroll
@@ -155,8 +178,8 @@ __global__ __launch_bounds__(256, 2) void window_kernel(WindowArgs a) {
     if (threadIdx.x == 0) any_dropped = 0;
     __syncthreads();
     if (i_begin < i_end) {
-        fetch_tile<true>(kbase, a.k.token, tile_at(i_begin) * kTile, N - 1, keys_even, wave, lane);
-        fetch_tile<false>(vbase, a.v.token, tile_at(i_begin) * kTile, N - 1, values_even, wave, lane);
+        fetch_keys(tile_at(i_begin) * kTile, N - 1, keys_even);
+        fetch_values(tile_at(i_begin) * kTile, N - 1, values_even);
     }
     const auto is_edge = [&](int tile0) {   // some row of the workgroup does not see all of the tile
         return tile0 + kTile - 1 > first_pos || (a.window && tile0 < last_pos - a.window + 1 && tile0 + kTile > a.sinks);
@@ -189,8 +212,8 @@ __global__ __launch_bounds__(256, 2) void window_kernel(WindowArgs a) {
         }
         __syncthreads();
         if (it + 1 < i_end) {
-            fetch_tile<true>(kbase, a.k.token, tile_at(it + 1) * kTile, N - 1, next_keys, wave, lane);
-            fetch_tile<false>(vbase, a.v.token, tile_at(it + 1) * kTile, N - 1, next_values, wave, lane);
+            fetch_keys(tile_at(it + 1) * kTile, N - 1, next_keys);
+            fetch_values(tile_at(it + 1) * kTile, N - 1, next_values);
         }
         // none of the wave's rows sees the tile
         if (tile0 > wave_last || (tile0 + kTile <= wave_first_low && tile0 >= a.sinks)) return;
@@ -267,7 +290,7 @@ __global__ __launch_bounds__(256, 2) void window_kernel(WindowArgs a) {
                 for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const uint32_t x = vbase[j * a.v.token + 32 * dt + 8 * (i / 4) + 4 * half + i % 4];
+                        const uint32_t x = fetch_values.base[j * a.v.token + 32 * dt + 8 * (i / 4) + 4 * half + i % 4];
                         if ((x & kExponents<BF16> & 0xFFFFu) == (kExponents<BF16> & 0xFFFFu) && seen(j)) o[dt][i] += widen16<BF16>(x);
                     }
         }
@@ -390,6 +413,7 @@ int specache_window_attend(const specache_window_config* cfg, const specache_vie
     if (!q || !k || !v || !out) return fail_without_context(SPECACHE_EINVAL, "null view");
     if (!view_fits(*q) || !view_fits(*out) || (cfg->kv_tokens && (!view_fits(*k) || !view_fits(*v))))
         return fail_without_context(SPECACHE_EINVAL, "a view's address must be 16-byte aligned, its strides multiples of 8");
+    if (k->token > (1 << 24) || v->token > (1 << 24)) return fail_without_context(SPECACHE_EINVAL, "token strides of k and v go up to 2^24");
     if (!rows_apart(*out, cfg->batch, cfg->n_q_heads, cfg->q_tokens)) return fail_without_context(SPECACHE_EINVAL, "the output's rows share memory");
     if (p.scratch) {
         if (!scratch || (uintptr_t)scratch % 16) return fail_without_context(SPECACHE_EINVAL, "scratch must be 16-byte aligned");

@@ -106,7 +106,7 @@ def test_window_attend_refuses():
         size = C.c_int64(-7)
         assert binding.lib().specache_window_scratch(C.byref(_config(**change)), C.byref(size)) == binding.EINVAL and size.value == -7
     for views in (dict(q=None), dict(k=None), dict(v=None), dict(out=None), dict(k=View(2 * A + 2, 2560, 1280, 128)), dict(out=View(4 * A, 1536, 0, 128)),
-                  dict(v=View(3 * A, 2560, 1280, 4))):
+                  dict(v=View(3 * A, 2560, 1280, 4)), dict(k=View(2 * A, 0, 0, (1 << 24) + 8))):
         assert _window(_config(), **views) == binding.EINVAL, views
     assert _window(None) == binding.EINVAL
     assert _window(_config(batch=0), q=None) == _window(_config(q_tokens=0), k=None) == binding.OK
