@@ -1,15 +1,19 @@
 // Attention over 16-bit keys and values with a sliding window and sinks.
 //
 // The rows of a KV head are its queries token by token, the heads that share it side by side: row r is query r / G of head
-// r % G.  A workgroup takes 128 of them, 32 per wave, and walks the tiles of 64 positions that any of them sees, with the
-// running maximum and sum of a softmax (the weights of a tile are rounded to the inputs' type for the product with the values, maximum,
-// sum and both products are binary32).
+// r % G.  A wave takes 32 rows and walks the tiles of positions that any of them sees, with the running maximum and sum of a softmax (the
+// weights of a tile are rounded to the inputs' type for the product with the values; maximum, sum and both products are binary32).
 //
 // Both products run with the positions as the matrix cores' rows: S^T = K Q^T leaves a lane 16 scores of ONE query row, so
 // that maximum, sum and rescaling need no exchange but one between the two halves of a wave, and what the lane holds of
 // S^T is, rounded, already the operand that O^T = V^T P^T wants, if the contraction takes the positions in the order in which
 // the first product leaves them (4 of the lower half, 4 of the upper, ...).  The values' operand in that order, channel by
-// channel, comes from LDS through its transposing read.
+// channel, comes from LDS through its transposing read.  Keys and values go to LDS without passing registers.
+//
+// Two kernels.  tile_kernel, for prompts and parts of prompts: the 4 or 8 waves of a workgroup have rows of their own and share the
+// tiles.  step_kernel, for up to 32 rows per KV head: a wave by itself, with tiles of its own; memory bounds it, so that
+// the rows that a short step leaves empty cost nothing.  Where rows are few, either splits the positions into chunks, whose partial
+// results (as fractions of the chunk's own maximum) merge_kernel joins.
 #include "operators.h"
 
 #include <algorithm>
@@ -25,9 +29,8 @@ typedef short short4v __attribute__((ext_vector_type(4)));
 typedef __bf16 bfloat8v __attribute__((ext_vector_type(8)));
 typedef _Float16 half8v __attribute__((ext_vector_type(8)));
 
-constexpr int kTile = 64;             // positions of a tile
-constexpr int kWaves = 4, kWaveRows = 32, kRows = kWaves * kWaveRows;
-constexpr int kTileBytes = kTile * kD * 2;
+constexpr int kWaveRows = 32;
+constexpr int kRowBytes16 = kD * 2;   // a position's keys, or its values
 constexpr float kNever = -1e30f;      // a maximum below every score: nothing seen yet
 constexpr float kLazy = 8.0f;         // the maximum moves when a score exceeds it by more than this (in powers of two)
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -36,10 +39,10 @@ struct WindowArgs {
     specache_view q, k, v, out;
     const int32_t* q_lengths;
     const int32_t* kv_lengths;
-    float* part_o;                    // [row tile][chunk][kRows][kD], not divided by the sum
-    float* part_ml;                   // [row tile][chunk][kRows][2]: maximum (in powers of two), sum
+    float* part_o;                    // [item][chunk][item_rows][kD], not divided by the sum
+    float* part_ml;                   // [item][chunk][item_rows][2]: maximum (in powers of two), sum
     int n_kv_heads, G, q_tokens, kv_tokens, window, sinks;
-    int row_tiles, chunks;
+    int row_tiles, item_rows, chunks; // an item is a tile of item_rows rows of a KV head of a sequence
     float scale;                      // sm_scale in powers of two
 };
 
@@ -57,40 +60,43 @@ __device__ __forceinline__ float other_half(float v) {   // the value of the lan
 typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void global_void;
 
-// Where 16-byte piece c (8 channels) of position r of a tile is, in bytes.  A wave's key reads take one piece of 32 positions at a
-// time, its value reads 64 bytes of 4 positions: either spreads over all banks.
+// Where 16-byte piece c (8 channels) of position r of a tile is: at piece c ^ swizzle(r) of the position's 16.  A wave's key reads take
+// one piece of 32 positions at a time, its value reads 64 bytes of 4 positions: either spreads over all banks (no conflicts counted).
 __device__ __forceinline__ int key_swizzle(int r) { return r & 15; }
 __device__ __forceinline__ int value_swizzle(int r) { return (r & 3) << 2 | (r >> 2 & 1) << 1; }
 
-// One wave's quarter of a tile of keys or values: 16 positions, four at a time.  The LDS side is in order of lanes, so the pieces are
-// exchanged on the way from memory.
-template <bool KEYS>
+// One wave's share of a tile of keys or values: FETCHES times 4 positions from position 4 * FETCHES * part on.  The LDS side is in order of
+// lanes, so the pieces are exchanged on the way from memory.  A lane's places are worked out once: a tile then costs a uniform
+// address and the loads (by 64-bit arithmetic per tile a prompt of 16k tokens with 32 heads took 2476 us instead of 2282).
+template <bool KEYS, int FETCHES>
 struct Fetch {
     const uint16_t* base;             // position 0 of the head
     int64_t stride;
-    uint32_t at[4];                   // bytes from the tile's first position to this lane's pieces
-    int wave, lane;
-    __device__ __forceinline__ int position(int i) const { return 16 * wave + 4 * i + lane / 16; }
+    int part, lane;
+    uint32_t at[FETCHES];             // bytes from the tile's first position to this lane's pieces
+    __device__ __forceinline__ int position(int i) const { return 4 * (FETCHES * part + i) + lane / 16; }
     __device__ __forceinline__ uint32_t piece(int i) const {
         const int r = position(i);
         return ((lane % 16) ^ (KEYS ? key_swizzle(r) : value_swizzle(r))) * 16;
     }
-    __device__ __forceinline__ void start() {
+    __device__ __forceinline__ Fetch(const specache_view& v, int b, int h, int part_, int lane_)
+        : base((const uint16_t*)v.data + b * v.batch + h * v.head), stride(v.token), part(part_), lane(lane_) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) at[i] = (uint32_t)position(i) * (uint32_t)stride * 2 + piece(i);
+        for (int i = 0; i < FETCHES; ++i) at[i] = (uint32_t)position(i) * (uint32_t)stride * 2 + piece(i);
     }
     // Positions from `last` on are that one again (no row sees them, but they are finite if it is).
-    __device__ __forceinline__ void operator()(int first, int last, char* lds) const {
-        const char* tile = (const char*)(base + first * stride);
-        if (first + kTile - 1 <= last) {
+    __device__ __forceinline__ void operator()(int first, int tile, int last, char* lds) const {
+        const char* from = (const char*)(base + first * stride);
+        char* to = lds + 4 * FETCHES * part * kRowBytes16;
+        if (first + tile - 1 <= last) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                __builtin_amdgcn_global_load_lds((global_void*)(tile + at[i]), (lds_void*)(lds + (16 * wave + 4 * i) * kD * 2), 16, 0, 0);
+            for (int i = 0; i < FETCHES; ++i)
+                __builtin_amdgcn_global_load_lds((global_void*)(from + at[i]), (lds_void*)(to + 4 * i * kRowBytes16), 16, 0, 0);
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < FETCHES; ++i) {
                 const uint32_t r = min(position(i), last - first);
-                __builtin_amdgcn_global_load_lds((global_void*)(tile + (r * (uint32_t)stride * 2 + piece(i))), (lds_void*)(lds + (16 * wave + 4 * i) * kD * 2), 16, 0, 0);
+                __builtin_amdgcn_global_load_lds((global_void*)(from + (r * (uint32_t)stride * 2 + piece(i))), (lds_void*)(to + 4 * i * kRowBytes16), 16, 0, 0);
             }
         }
     }
@@ -99,148 +105,103 @@ struct Fetch {
 template <bool BF16> constexpr uint32_t kExponents = BF16 ? 0x7F807F80u : 0x7C007C00u;        // of two values: all ones where one is not finite
 template <bool BF16> constexpr uint32_t kAboveExponents = BF16 ? 0x00800080u : 0x04000400u;   // added to them, it then sets the sign's bit
 
+// A row that does not see a value has it times zero.  Of tiles that some row does not see all of, values that are not finite are therefore dropped
+// (by the wave that fetched them) and given to the rows that see them after the walk.  True where something was dropped.
+template <bool BF16, int FETCHES>
+__device__ __forceinline__ bool drop_odd_values(char* values, int part, int lane) {
+    uint4v* own = (uint4v*)(values + part * FETCHES * 4 * kRowBytes16);
+    bool dropped = false;
+#pragma unroll
+    for (int i = 0; i < FETCHES; ++i) {
+        uint4v x = own[i * 64 + lane];
+        uint32_t odd = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) odd |= (x[e] & kExponents<BF16>) + kAboveExponents<BF16>;
+        if (odd & 0x80008000u) {
+            dropped = true;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t y = (x[e] & kExponents<BF16>) + kAboveExponents<BF16>;
+                x[e] &= (y & 0x8000u ? 0u : 0xFFFFu) | (y & 0x80000000u ? 0u : 0xFFFF0000u);
+            }
+            own[i * 64 + lane] = x;
+        }
+    }
+    return dropped;
+}
+
 // What a row of queries sees: positions up to `last`, of these the sinks and those from `low` on.
 struct Seen {
     int last, low, sinks;
     __device__ __forceinline__ bool operator()(int j) const { return (j <= last) & ((j < sinks) | (j >= low)); }
 };
 
-template <bool BF16, bool SPLIT>
-__global__ __launch_bounds__(256, 2) void window_kernel(WindowArgs a) {
-    // (arrays of their own: the compiler then sees that what is fetched into one and what is read from another do not meet)
-    __shared__ __align__(1024) char keys_even[kTileBytes];
-    __shared__ __align__(1024) char keys_odd[kTileBytes];
-    __shared__ __align__(1024) char values_even[kTileBytes];
-    __shared__ __align__(1024) char values_odd[kTileBytes];
-    __shared__ int any_dropped;
+// The tiles of TILE positions that the rows from position `first` to `last` see between them: those with sinks, then those from the first
+// row's window to the last row's own position.
+template <int TILE>
+struct Walk {
+    int sink_tiles, low_tile, n;
+    __device__ __forceinline__ Walk(int first, int last, int window, int sinks) {
+        low_tile = window ? max(0, first - window + 1) / TILE : 0;
+        const int end = last < 0 ? 0 : last / TILE + 1;
+        sink_tiles = max(0, min((min(sinks, last + 1) + TILE - 1) / TILE, low_tile));
+        n = sink_tiles + max(0, end - low_tile);
+    }
+    __device__ __forceinline__ int position(int i) const { return (i < sink_tiles ? i : i - sink_tiles + low_tile) * TILE; }
+};
+// Some row from `first` to `last` does not see all of the tile.
+template <int TILE>
+__device__ __forceinline__ bool is_edge(int tile0, int first, int last, int window, int sinks) {
+    return tile0 + TILE - 1 > first || (window && tile0 < last - window + 1 && tile0 + TILE > sinks);
+}
 
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
-    // the row tiles of a KV head follow each other on one XCD, the longest first
-    const int total = gridDim.x, per_xcd = total / 8, rest = total % 8, xcd = blockIdx.x % 8;
-    const int id = xcd * per_xcd + min(xcd, rest) + blockIdx.x / 8;
-    const int chunk = SPLIT ? id % a.chunks : 0;
-    const int item = SPLIT ? id / a.chunks : id;
-    const int head_row = item / a.row_tiles, row_tile = a.row_tiles - 1 - item % a.row_tiles;
-    const int b = head_row / a.n_kv_heads, h = head_row % a.n_kv_heads;
-
-    const int n = a.q_lengths ? min(max(a.q_lengths[b], 0), a.q_tokens) : a.q_tokens;
-    const int N = a.kv_lengths ? min(max(a.kv_lengths[b], 0), a.kv_tokens) : a.kv_tokens;
-    const int rows = n * a.G;
-    if (row_tile * kRows >= rows) return;
-
-    const int r = row_tile * kRows + wave * kWaveRows + lane % 32;
-    const bool row_exists = r < rows;
-    const int r_here = min(r, rows - 1);
-    const int token = r_here / a.G, q_head = h * a.G + r_here % a.G;
+// A wave's 32 rows (lane l and l + 32 hold row l) and their softmax over tiles of 32 * BLOCKS positions.
+template <bool BF16, int BLOCKS>
+struct Rows {
+    uint4v q[8];
+    float16v s[BLOCKS], o[4];
+    float m, l;                       // l: of this lane's half of the positions
+    uint4v p[2 * BLOCKS];
     Seen seen;
-    seen.last = N - n + token;
-    seen.low = a.window ? seen.last - a.window + 1 : 0;
-    seen.sinks = a.sinks;
+    int lane, half;
 
-    // positions that the workgroup's rows see: tiles from 0 (sinks), then tiles from low_tile on
-    const int tile_last_row = min(rows, (row_tile + 1) * kRows) - 1;
-    const int first_pos = N - n + row_tile * kRows / a.G, last_pos = N - n + tile_last_row / a.G;
-    const int low_tile = a.window ? max(0, first_pos - a.window + 1) / kTile : 0;
-    const int end_tile = last_pos < 0 ? 0 : last_pos / kTile + 1;
-    const int sink_tiles = min((min(a.sinks, last_pos + 1) + kTile - 1) / kTile, low_tile);
-    const int n_tiles = max(0, sink_tiles) + max(0, end_tile - low_tile);
-    const auto tile_at = [&](int i) { return i < sink_tiles ? i : i - max(0, sink_tiles) + low_tile; };
-    int i_begin = 0, i_end = n_tiles;
-    if constexpr (SPLIT) {
-        const int per = (n_tiles + a.chunks - 1) / a.chunks;
-        i_begin = min(chunk * per, n_tiles);
-        i_end = min(i_begin + per, n_tiles);
+    __device__ __forceinline__ void start(const uint16_t* row, int lane_) {
+        lane = lane_, half = lane / 32;
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk) q[kk] = *(const uint4v*)(row + 16 * kk + 8 * half);
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[dt][i] = 0.0f;
+        m = kNever, l = 0.0f;
     }
-    // the wave's own bounds, for tiles that all of its rows see
-    const int wave_first = N - n + min(row_tile * kRows + wave * kWaveRows, rows - 1) / a.G;
-    const int wave_last = N - n + min(row_tile * kRows + wave * kWaveRows + kWaveRows - 1, rows - 1) / a.G;
-    const int wave_low = a.window ? wave_last - a.window + 1 : 0;
-    const int wave_first_low = a.window ? wave_first - a.window + 1 : 0;
-
-    uint4v qf[8];
-    {
-        const uint16_t* qrow = (const uint16_t*)a.q.data + b * a.q.batch + q_head * a.q.head + token * a.q.token;
+    __device__ __forceinline__ void scores(const char* keys) {
 #pragma unroll
-        for (int kk = 0; kk < 8; ++kk) qf[kk] = *(const uint4v*)(qrow + 16 * kk + 8 * half);
-    }
-    Fetch<true> fetch_keys{(const uint16_t*)a.k.data + b * a.k.batch + h * a.k.head, a.k.token, {}, wave, lane};
-    Fetch<false> fetch_values{(const uint16_t*)a.v.data + b * a.v.batch + h * a.v.head, a.v.token, {}, wave, lane};
-    fetch_keys.start();
-    fetch_values.start();
-
-    float16v o[4];
+        for (int i = 0; i < 16 * BLOCKS; ++i) s[i / 16][i % 16] = 0.0f;
 #pragma unroll
-    for (int dt = 0; dt < 4; ++dt)
+        for (int kk = 0; kk < 8; ++kk)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[dt][i] = 0.0f;
-    float m = kNever, l = 0.0f;       // l: of this lane's half of the positions
-
-    if (threadIdx.x == 0) any_dropped = 0;
-    __syncthreads();
-    if (i_begin < i_end) {
-        fetch_keys(tile_at(i_begin) * kTile, N - 1, keys_even);
-        fetch_values(tile_at(i_begin) * kTile, N - 1, values_even);
-    }
-    const auto is_edge = [&](int tile0) {   // some row of the workgroup does not see all of the tile
-        return tile0 + kTile - 1 > first_pos || (a.window && tile0 < last_pos - a.window + 1 && tile0 + kTile > a.sinks);
-    };
-    const auto step = [&](int it, char* keys, char* values, char* next_keys, char* next_values) {
-        const int tile0 = tile_at(it) * kTile;
-        __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
-        if (is_edge(tile0)) {
-            // A row that does not see a value has it times zero, so values that are not finite are dropped here, by the wave that
-            // fetched them, and given to the rows that see them after the walk.
-            uint4v* own = (uint4v*)(values + wave * 16 * kD * 2);
-            bool dropped = false;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint4v x = own[i * 64 + lane];
-                uint32_t odd = 0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) odd |= (x[e] & kExponents<BF16>) + kAboveExponents<BF16>;
-                if (odd & 0x80008000u) {
-                    dropped = true;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t y = (x[e] & kExponents<BF16>) + kAboveExponents<BF16>;
-                        x[e] &= (y & 0x8000u ? 0u : 0xFFFFu) | (y & 0x80000000u ? 0u : 0xFFFF0000u);
-                    }
-                    own[i * 64 + lane] = x;
-                }
+            for (int blk = 0; blk < BLOCKS; ++blk) {
+                const int r = 32 * blk + lane % 32;
+                s[blk] = mfma32<BF16>(*(const uint4v*)(keys + r * kRowBytes16 + (((2 * kk + half) ^ key_swizzle(r)) * 16)), q[kk], s[blk]);
             }
-            if (dropped) any_dropped = 1;
+    }
+    // position of s[i / 16][i % 16] in a tile, less 4 * half
+    static __device__ __forceinline__ constexpr int place(int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4; }
+    __device__ __forceinline__ void mask(int tile0) {
+        const Seen here{seen.last - tile0 - 4 * half, seen.low - tile0 - 4 * half, seen.sinks - tile0 - 4 * half};
+#pragma unroll
+        for (int i = 0; i < 16 * BLOCKS; ++i) {
+            if (!here(place(i))) s[i / 16][i % 16] = -INFINITY;
+            if (i % 2) __builtin_amdgcn_sched_barrier(0);   // few conditions at a time: they live in scalar registers
         }
-        __syncthreads();
-        if (it + 1 < i_end) {
-            fetch_keys(tile_at(it + 1) * kTile, N - 1, next_keys);
-            fetch_values(tile_at(it + 1) * kTile, N - 1, next_values);
-        }
-        // none of the wave's rows sees the tile
-        if (tile0 > wave_last || (tile0 + kTile <= wave_first_low && tile0 >= a.sinks)) return;
-
-        float16v s[2];
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[hf][i] = 0.0f;
-            const int row = 32 * hf + lane % 32;
-#pragma unroll
-            for (int kk = 0; kk < 8; ++kk) {
-                const uint4v kf = *(const uint4v*)(keys + row * kD * 2 + (((2 * kk + half) ^ key_swizzle(row)) * 16));
-                s[hf] = mfma32<BF16>(kf, qf[kk], s[hf]);
-            }
-        }
-        if (tile0 + kTile - 1 > wave_first || (tile0 < wave_low && tile0 + kTile > a.sinks)) {
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (!seen(tile0 + 32 * hf + 8 * (i / 4) + 4 * half + i % 4)) s[hf][i] = -INFINITY;
-        }
+    }
+    // The maximum moves rarely, so that the sums do: weights up to 2^kLazy of a row's own maximum keep all their bits.
+    __device__ __forceinline__ void move_maximum(float scale) {
         float most = s[0][0];
 #pragma unroll
-        for (int i = 1; i < 32; ++i) most = fmaxf(most, s[i / 16][i % 16]);
-        most = fmaxf(most, other_half(most)) * a.scale;
+        for (int i = 1; i < 16 * BLOCKS; ++i) most = fmaxf(most, s[i / 16][i % 16]);
+        most = fmaxf(most, other_half(most)) * scale;
         if (__ballot(most > m + kLazy)) {
             const float to = fmaxf(m, most), factor = __builtin_amdgcn_exp2f(m - to);
             m = to;
@@ -250,69 +211,48 @@ __global__ __launch_bounds__(256, 2) void window_kernel(WindowArgs a) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[dt][i] *= factor;
         }
-        uint4v p[4];
+    }
+    __device__ __forceinline__ void weights(float scale) {
 #pragma unroll
-        for (int i = 0; i < 32; i += 2) {
-            const float x = __builtin_amdgcn_exp2f(fmaf(s[i / 16][i % 16], a.scale, -m)), y = __builtin_amdgcn_exp2f(fmaf(s[i / 16][i % 16 + 1], a.scale, -m));
+        for (int i = 0; i < 16 * BLOCKS; i += 2) {
+            const float x = __builtin_amdgcn_exp2f(fmaf(s[i / 16][i % 16], scale, -m)), y = __builtin_amdgcn_exp2f(fmaf(s[i / 16][i % 16 + 1], scale, -m));
             l += x;
             l += y;
             p[i / 8][i % 8 / 2] = pack16<BF16>(x, y);
         }
+    }
+    __device__ __forceinline__ void add_values(const char* values) {
         // the 4 x 4 block of a lane group: position 4 half + (lane % 16) / 4, channels 16 (lane / 16 % 2) + 4 (lane % 4)
         const int vr = 4 * half + lane % 16 / 4, vc = 16 * (lane / 16 % 2) + 4 * (lane % 4);
 #pragma unroll
-        for (int st = 0; st < 4; ++st)
+        for (int st = 0; st < 2 * BLOCKS; ++st)
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt) {
                 uint4v f;
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const int row = 16 * st + 8 * j + vr, col = 32 * dt + vc;
-                    const char* at = values + row * kD * 2 + ((col / 8) ^ value_swizzle(row)) * 16 + col % 8 * 2;
+                    const int r = 16 * st + 8 * j + vr, c = 32 * dt + vc;
+                    const char* at = values + r * kRowBytes16 + ((c / 8) ^ value_swizzle(r)) * 16 + c % 8 * 2;
                     const uint2v w = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)at));
                     f[2 * j] = w[0];
                     f[2 * j + 1] = w[1];
                 }
                 o[dt] = mfma32<BF16>(f, p[st], o[dt]);
             }
-    };
-    for (int it = i_begin; it < i_end; it += 2) {
-        step(it, keys_even, values_even, keys_odd, values_odd);
-        if (it + 1 < i_end) step(it + 1, keys_odd, values_odd, keys_even, values_even);
     }
-    __syncthreads();
-    if (any_dropped) {
-        for (int it = i_begin; it < i_end; ++it) {
-            const int tile0 = tile_at(it) * kTile;
-            if (!is_edge(tile0)) continue;
-            for (int j = tile0; j < min(tile0 + kTile, N); ++j)
+    // what drop_odd_values dropped of positions tile0 to end - 1
+    __device__ void give_odd_values(const uint16_t* values, int64_t stride, int tile0, int end) {
+        for (int j = tile0; j < end; ++j)
 #pragma unroll
-                for (int dt = 0; dt < 4; ++dt)
+            for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const uint32_t x = fetch_values.base[j * a.v.token + 32 * dt + 8 * (i / 4) + 4 * half + i % 4];
-                        if ((x & kExponents<BF16> & 0xFFFFu) == (kExponents<BF16> & 0xFFFFu) && seen(j)) o[dt][i] += widen16<BF16>(x);
-                    }
-        }
+                for (int i = 0; i < 16; ++i) {
+                    const uint32_t x = values[j * stride + 32 * dt + 8 * (i / 4) + 4 * half + i % 4];
+                    if ((x & kExponents<BF16> & 0xFFFFu) == (kExponents<BF16> & 0xFFFFu) && seen(j)) o[dt][i] += widen16<BF16>(x);
+                }
     }
-
-    l += other_half(l);
-    if constexpr (SPLIT) {
-        const int64_t place = ((int64_t)(item / a.row_tiles * a.row_tiles + row_tile) * a.chunks + chunk) * kRows + wave * kWaveRows + lane % 32;
-        if (half == 0) {
-            a.part_ml[2 * place] = m;
-            a.part_ml[2 * place + 1] = l;
-        }
-        if (i_begin >= i_end) return;   // nothing to add, and nothing that the merge reads
-#pragma unroll
-        for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *(float4*)(a.part_o + place * kD + 32 * dt + 8 * i + 4 * half) = float4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
-    } else {
-        if (!row_exists) return;
+    __device__ __forceinline__ void store(uint16_t* to) {
         const float by = l == 0.0f ? 0.0f : 1.0f / l;
-        uint16_t* to = (uint16_t*)a.out.data + b * a.out.batch + q_head * a.out.head + token * a.out.token;
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
@@ -320,39 +260,243 @@ __global__ __launch_bounds__(256, 2) void window_kernel(WindowArgs a) {
                 *(uint2v*)(to + 32 * dt + 8 * i + 4 * half) =
                     uint2v{pack16<BF16>(o[dt][4 * i] * by, o[dt][4 * i + 1] * by), pack16<BF16>(o[dt][4 * i + 2] * by, o[dt][4 * i + 3] * by)};
     }
+    // something: the chunk had a tile; without one the merge reads no sums of this chunk
+    __device__ __forceinline__ void store_part(float* part_o, float* part_ml, int64_t place, bool something) {
+        if (half == 0) *(float2*)(part_ml + 2 * place) = float2{m, l};
+        if (!something) return;
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *(float4*)(part_o + place * kD + 32 * dt + 8 * i + 4 * half) = float4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+    }
+};
+
+__device__ __forceinline__ int length_of(const int32_t* lengths, int b, int most) { return lengths ? min(max(lengths[b], 0), most) : most; }
+
+// The workgroups of an item, and the items of a KV head, follow each other on one XCD (workgroups go to the 8 XCDs in turn), whose L2 they share.
+__device__ __forceinline__ int on_one_xcd() {
+    const int total = gridDim.x, per_xcd = total / 8, rest = total % 8, xcd = blockIdx.x % 8;
+    return xcd * per_xcd + min(xcd, rest) + blockIdx.x / 8;
 }
 
-// The chunks of a row, joined: a wave per row, two channels per lane.
+// Tiles of 64 positions travel to LDS while the one before is worked on; a wave takes 1/WAVES of a tile's keys and values.
+// us, 32 heads over a prompt of 16k tokens: 2157 (1.02 PFLOP/s), 8 heads of 4 queries over 32k through a window of 4096 2060.
+template <bool BF16, bool SPLIT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void tile_kernel(WindowArgs a) {
+    constexpr int TILE = 64, ROWS = WAVES * kWaveRows, FETCHES = 16 / WAVES;
+    // (arrays of their own: the compiler then sees that what is fetched into one and what is read from another do not meet, and
+    // does not wait for the next tile in front of a tile's reads)
+    __shared__ __align__(1024) char keys_even[TILE * kRowBytes16];
+    __shared__ __align__(1024) char keys_odd[TILE * kRowBytes16];
+    __shared__ __align__(1024) char values_even[TILE * kRowBytes16];
+    __shared__ __align__(1024) char values_odd[TILE * kRowBytes16];
+    __shared__ int any_dropped;
+
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int id = on_one_xcd(), chunk = SPLIT ? id % a.chunks : 0, item = SPLIT ? id / a.chunks : id;
+    const int b = item / a.row_tiles / a.n_kv_heads, h = item / a.row_tiles % a.n_kv_heads;
+    const int row_tile = a.row_tiles - 1 - item % a.row_tiles;   // the longest first
+    const int n = length_of(a.q_lengths, b, a.q_tokens), N = length_of(a.kv_lengths, b, a.kv_tokens);
+    const int rows = n * a.G, row0 = row_tile * ROWS, wave_row0 = row0 + wave * kWaveRows;
+    if (row0 >= rows) return;
+
+    const int row = wave_row0 + lane % 32, r = min(row, rows - 1), token = r / a.G, q_head = h * a.G + r % a.G;
+    const int first = N - n + row0 / a.G, last = N - n + min(row0 + ROWS - 1, rows - 1) / a.G;
+    const int wave_first = N - n + min(wave_row0, rows - 1) / a.G, wave_last = N - n + min(wave_row0 + kWaveRows - 1, rows - 1) / a.G;
+    const int wave_first_low = a.window ? wave_first - a.window + 1 : 0;
+    const Walk<TILE> walk(first, last, a.window, a.sinks);
+    int i_begin = 0, i_end = walk.n;
+    if constexpr (SPLIT) {
+        const int per = (walk.n + a.chunks - 1) / a.chunks;
+        i_begin = min(chunk * per, walk.n);
+        i_end = min(i_begin + per, walk.n);
+    }
+
+    Rows<BF16, TILE / 32> rs;
+    rs.seen = Seen{N - n + token, a.window ? N - n + token - a.window + 1 : 0, a.sinks};
+    rs.start((const uint16_t*)a.q.data + b * a.q.batch + q_head * a.q.head + token * a.q.token, lane);
+    const Fetch<true, FETCHES> fetch_keys(a.k, b, h, wave, lane);
+    const Fetch<false, FETCHES> fetch_values(a.v, b, h, wave, lane);
+
+    if (threadIdx.x == 0) any_dropped = 0;
+    __syncthreads();
+    if (i_begin < i_end) {
+        fetch_keys(walk.position(i_begin), TILE, N - 1, keys_even);
+        fetch_values(walk.position(i_begin), TILE, N - 1, values_even);
+    }
+    const auto step = [&](int it, char* keys, char* values, char* next_keys, char* next_values) __attribute__((always_inline)) {
+        const int tile0 = walk.position(it);
+        __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+        if (is_edge<TILE>(tile0, first, last, a.window, a.sinks) && drop_odd_values<BF16, FETCHES>(values, wave, lane)) any_dropped = 1;
+        __syncthreads();
+        if (it + 1 < i_end) {
+            fetch_keys(walk.position(it + 1), TILE, N - 1, next_keys);
+            fetch_values(walk.position(it + 1), TILE, N - 1, next_values);
+        }
+        // none of the wave's rows sees the tile
+        if (tile0 > wave_last || (tile0 + TILE <= wave_first_low && tile0 >= a.sinks)) return;
+        rs.scores(keys);
+        // the first reads ahead of the products, then one beside each
+        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+        for (int i = 0; i < 10; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
+        if (is_edge<TILE>(tile0, wave_first, wave_last, a.window, a.sinks)) rs.mask(tile0);
+        rs.move_maximum(a.scale);
+        rs.weights(a.scale);
+        rs.add_values(values);
+        // the first step's weights, then the others' beside the products
+        __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 28, 0);
+#pragma unroll
+        for (int i = 0; i < 12; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 7, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+    };
+    for (int it = i_begin; it < i_end; it += 2) {
+        step(it, keys_even, values_even, keys_odd, values_odd);
+        if (it + 1 < i_end) step(it + 1, keys_odd, values_odd, keys_even, values_even);
+    }
+    __syncthreads();
+    if (any_dropped)
+        for (int it = i_begin; it < i_end; ++it) {
+            const int tile0 = walk.position(it);
+            if (is_edge<TILE>(tile0, first, last, a.window, a.sinks)) rs.give_odd_values(fetch_values.base, a.v.token, tile0, min(tile0 + TILE, N));
+        }
+    rs.l += other_half(rs.l);
+    if constexpr (SPLIT)
+        rs.store_part(a.part_o, a.part_ml, ((int64_t)item * a.chunks + chunk) * ROWS + wave * kWaveRows + lane % 32, i_begin < i_end);
+    else if (row < rows)
+        rs.store((uint16_t*)a.out.data + b * a.out.batch + q_head * a.out.head + token * a.out.token);
+}
+
+// A wave by itself: 32 positions at a time, the next ones on their way while it works on these; five of them on a compute unit (by LDS)
+// keep up to 160 KB in flight there.
+template <bool BF16, bool SPLIT>
+__global__ __launch_bounds__(64, 2) void step_kernel(WindowArgs a) {
+    constexpr int TILE = 32, FETCHES = 8;
+    __shared__ __align__(1024) char keys_even[TILE * kRowBytes16];
+    __shared__ __align__(1024) char keys_odd[TILE * kRowBytes16];
+    __shared__ __align__(1024) char values_even[TILE * kRowBytes16];
+    __shared__ __align__(1024) char values_odd[TILE * kRowBytes16];
+
+    const int lane = threadIdx.x;
+    const int id = on_one_xcd(), chunk = SPLIT ? id % a.chunks : 0, item = SPLIT ? id / a.chunks : id;
+    const int b = item / a.n_kv_heads, h = item % a.n_kv_heads;
+    const int n = length_of(a.q_lengths, b, a.q_tokens), N = length_of(a.kv_lengths, b, a.kv_tokens);
+    const int rows = n * a.G;
+    if (!rows) return;
+
+    const int row = lane % 32, r = min(row, rows - 1), token = r / a.G, q_head = h * a.G + r % a.G;
+    const int first = N - n, last = N - 1;
+    const Walk<TILE> walk(first, last, a.window, a.sinks);
+    int i_begin = 0, i_end = walk.n;
+    if constexpr (SPLIT) {
+        const int per = (walk.n + a.chunks - 1) / a.chunks;
+        i_begin = min(chunk * per, walk.n);
+        i_end = min(i_begin + per, walk.n);
+    }
+
+    Rows<BF16, 1> rs;
+    rs.seen = Seen{N - n + token, a.window ? N - n + token - a.window + 1 : 0, a.sinks};
+    const Fetch<true, FETCHES> fetch_keys(a.k, b, h, 0, lane);
+    const Fetch<false, FETCHES> fetch_values(a.v, b, h, 0, lane);
+    bool dropped = false;
+    if (i_begin < i_end) {
+        fetch_keys(walk.position(i_begin), TILE, N - 1, keys_even);
+        fetch_values(walk.position(i_begin), TILE, N - 1, values_even);
+    }
+    rs.start((const uint16_t*)a.q.data + b * a.q.batch + q_head * a.q.head + token * a.q.token, lane);
+    const auto step = [&](int it, char* keys, char* values, char* next_keys, char* next_values) __attribute__((always_inline)) {
+        const int tile0 = walk.position(it);
+        asm volatile("" ::: "memory");        // (the buffers' last reads are behind)
+        __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+        if (it + 1 < i_end) {
+            fetch_keys(walk.position(it + 1), TILE, N - 1, next_keys);
+            fetch_values(walk.position(it + 1), TILE, N - 1, next_values);
+            __builtin_amdgcn_s_waitcnt(0x4F78);   // vmcnt(24): this tile's keys are there
+        } else {
+            __builtin_amdgcn_s_waitcnt(0x0F78);   // vmcnt(8)
+        }
+        asm volatile("" ::: "memory");
+        rs.scores(keys);
+        const bool edge = is_edge<TILE>(tile0, first, last, a.window, a.sinks);
+        if (edge) rs.mask(tile0);
+        rs.move_maximum(a.scale);
+        rs.weights(a.scale);
+        asm volatile("" ::: "memory");
+        if (it + 1 < i_end) __builtin_amdgcn_s_waitcnt(0x4F70);   // vmcnt(16): and its values
+        else __builtin_amdgcn_s_waitcnt(0x0F70);
+        asm volatile("" ::: "memory");
+        if (edge) dropped |= drop_odd_values<BF16, FETCHES>(values, 0, lane);
+        rs.add_values(values);
+    };
+    for (int it = i_begin; it < i_end; it += 2) {
+        step(it, keys_even, values_even, keys_odd, values_odd);
+        if (it + 1 < i_end) step(it + 1, keys_odd, values_odd, keys_even, values_even);
+    }
+    if (__ballot(dropped))
+        for (int it = i_begin; it < i_end; ++it) {
+            const int tile0 = walk.position(it);
+            if (is_edge<TILE>(tile0, first, last, a.window, a.sinks)) rs.give_odd_values(fetch_values.base, a.v.token, tile0, min(tile0 + TILE, N));
+        }
+    rs.l += other_half(rs.l);
+    if (row >= rows) return;
+    if constexpr (SPLIT) rs.store_part(a.part_o, a.part_ml, ((int64_t)item * a.chunks + chunk) * a.item_rows + row, i_begin < i_end);
+    else rs.store((uint16_t*)a.out.data + b * a.out.batch + q_head * a.out.head + token * a.out.token);
+}
+
+// The chunks of a row, joined: two channels per lane, the chunks dealt to the waves of a workgroup.
+constexpr int kMergeWaves = 4;
 template <bool BF16>
-__global__ __launch_bounds__(256) void window_merge_kernel(WindowArgs a) {
-    const int lane = threadIdx.x % 64;
-    const int64_t id = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
-    const int row = id % kRows, item = id / kRows;
-    const int row_tile = item % a.row_tiles, b = item / a.row_tiles / a.n_kv_heads, h = item / a.row_tiles % a.n_kv_heads;
-    const int n = a.q_lengths ? min(max(a.q_lengths[b], 0), a.q_tokens) : a.q_tokens;
-    const int r = row_tile * kRows + row;
-    if (r >= n * a.G) return;
-    const float* ml = a.part_ml + 2 * ((int64_t)item * a.chunks * kRows + row);
-    const float* po = a.part_o + ((int64_t)item * a.chunks * kRows + row) * kD + 2 * lane;
+__global__ __launch_bounds__(64 * kMergeWaves) void merge_kernel(WindowArgs a) {
+    __shared__ float part[kMergeWaves][kD + 2];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int row = blockIdx.x % a.item_rows, item = blockIdx.x / a.item_rows;
+    const int b = item / a.row_tiles / a.n_kv_heads, h = item / a.row_tiles % a.n_kv_heads;
+    const int r = (a.row_tiles - 1 - item % a.row_tiles) * a.item_rows + row;
+    if (r >= length_of(a.q_lengths, b, a.q_tokens) * a.G) return;
+    const int64_t place = (int64_t)item * a.chunks * a.item_rows + row;
+    const float2* ml = (const float2*)a.part_ml + place;
+    const float* po = a.part_o + place * kD + 2 * lane;
+    // every lane a chunk: the largest maximum, which all waves work out alike
     float m = kNever;
-    for (int c = 0; c < a.chunks; ++c) m = fmaxf(m, ml[(int64_t)c * kRows * 2]);
+    for (int c = lane; c < a.chunks; c += 64) m = fmaxf(m, ml[(int64_t)c * a.item_rows].x);
+    for (int d = 32; d; d /= 2) m = fmaxf(m, __shfl_xor(m, d));
     float l = 0.0f, x = 0.0f, y = 0.0f;
-    for (int c = 0; c < a.chunks; ++c) {
-        const float lc = ml[(int64_t)c * kRows * 2 + 1];
-        if (lc == 0.0f) continue;
-        const float w = __builtin_amdgcn_exp2f(ml[(int64_t)c * kRows * 2] - m);
-        const float2 oc = *(const float2*)(po + (int64_t)c * kRows * kD);
-        l = fmaf(w, lc, l);
+#pragma unroll 4
+    for (int c = wave; c < a.chunks; c += kMergeWaves) {
+        const float2 one = ml[(int64_t)c * a.item_rows];
+        if (one.y == 0.0f) continue;   // (nothing was stored)
+        const float w = __builtin_amdgcn_exp2f(one.x - m);
+        const float2 oc = *(const float2*)(po + (int64_t)c * a.item_rows * kD);
+        l = fmaf(w, one.y, l);
         x = fmaf(w, oc.x, x);
         y = fmaf(w, oc.y, y);
     }
+    part[wave][2 * lane] = x;
+    part[wave][2 * lane + 1] = y;
+    if (lane == 0) part[wave][kD] = l;
+    __syncthreads();
+    if (wave) return;
+    l = x = y = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kMergeWaves; ++w) l += part[w][kD], x += part[w][2 * lane], y += part[w][2 * lane + 1];
     const float by = l == 0.0f ? 0.0f : 1.0f / l;
     uint16_t* to = (uint16_t*)a.out.data + b * a.out.batch + (h * a.G + r % a.G) * a.out.head + r / a.G * a.out.token;
     *(uint32_t*)(to + 2 * lane) = pack16<BF16>(x * by, y * by);
 }
 
+enum { kStep, kTile4, kTile8 };
 struct Plan {
-    int row_tiles = 0, chunks = 1;
+    int kernel = kStep, row_tiles = 1, item_rows = 0, chunks = 1;
     int64_t items = 0, scratch = 0;
 };
 
@@ -370,21 +514,41 @@ int check(const specache_window_config* c) {
     return SPECACHE_OK;
 }
 
-// Row tiles that are too few to fill the chip (two workgroups per compute unit) have their positions split into chunks, of at least
-// four tiles each.
 int plan_of(const specache_window_config& c, Plan& p) {
     const int G = c.n_q_heads / c.n_kv_heads;
-    p.row_tiles = (int)(((int64_t)c.q_tokens * G + kRows - 1) / kRows);
-    p.items = (int64_t)c.batch * c.n_kv_heads * p.row_tiles;
-    int64_t most = c.kv_tokens;
-    if (c.window) most = std::min<int64_t>(most, (int64_t)c.window + c.sinks + kRows);
-    const int64_t tiles = (most + kTile - 1) / kTile;
-    int64_t chunks = p.items ? 512 / p.items : 1;
-    chunks = std::min(chunks, tiles / 4);
+    const int64_t rows = (int64_t)c.q_tokens * G;
+    int64_t most = c.kv_tokens;                     // positions that a row tile walks
+    if (c.window) most = std::min<int64_t>(most, (int64_t)c.window + c.sinks + 128);
+    const int64_t heads = (int64_t)c.batch * c.n_kv_heads;
+    int64_t chunks = 1;
+    if (rows <= kWaveRows) {
+        p.kernel = kStep;
+        p.item_rows = (int)rows;
+        p.items = heads * (rows > 0);
+        const int64_t tiles = (most + 31) / 32;
+        const int64_t at_once = 256 * 5;            // waves that the chip holds
+        if (p.items) chunks = std::min(std::max(at_once / p.items, tiles / 32), tiles / 2);
+    } else {
+        p.kernel = most >= 2048 ? kTile8 : kTile4;
+        p.item_rows = p.kernel == kTile8 ? 256 : 128;
+        p.row_tiles = (int)((rows + p.item_rows - 1) / p.item_rows);
+        p.items = heads * p.row_tiles;
+        if (p.items) chunks = std::min<int64_t>((p.kernel == kTile8 ? 256 : 512) / p.items, (most + 63) / 64 / 4);
+    }
     p.chunks = (int)std::max<int64_t>(chunks, 1);
-    if (p.items * p.chunks > INT32_MAX / 64) return fail_without_context(SPECACHE_EINVAL, "too many rows");
-    p.scratch = p.chunks > 1 ? p.items * p.chunks * kRows * (kD + 2) * (int64_t)sizeof(float) : 0;
+    if (p.items * p.chunks > INT32_MAX / 256) return fail_without_context(SPECACHE_EINVAL, "too many rows");
+    p.scratch = p.chunks > 1 ? p.items * p.chunks * p.item_rows * (kD + 2) * (int64_t)sizeof(float) : 0;
     return SPECACHE_OK;
+}
+
+template <bool BF16>
+void launch(const Plan& p, const WindowArgs& a, hipStream_t stream) {
+    const dim3 grid((unsigned)(p.items * p.chunks));
+    const bool split = p.chunks > 1;
+    if (p.kernel == kStep) hipLaunchKernelGGL((split ? step_kernel<BF16, true> : step_kernel<BF16, false>), grid, dim3(64), 0, stream, a);
+    else if (p.kernel == kTile4) hipLaunchKernelGGL((split ? tile_kernel<BF16, true, 4> : tile_kernel<BF16, false, 4>), grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((split ? tile_kernel<BF16, true, 8> : tile_kernel<BF16, false, 8>), grid, dim3(512), 0, stream, a);
+    if (split) hipLaunchKernelGGL(merge_kernel<BF16>, dim3((unsigned)(p.items * p.item_rows)), dim3(64 * kMergeWaves), 0, stream, a);
 }
 
 }  // namespace
@@ -427,7 +591,7 @@ int specache_window_attend(const specache_window_config* cfg, const specache_vie
     a.q_lengths = q_lengths;
     a.kv_lengths = kv_lengths;
     a.part_o = (float*)scratch;
-    a.part_ml = a.part_o + p.items * p.chunks * kRows * kD;
+    a.part_ml = a.part_o + p.items * p.chunks * p.item_rows * kD;
     a.n_kv_heads = cfg->n_kv_heads;
     a.G = cfg->n_q_heads / cfg->n_kv_heads;
     a.q_tokens = cfg->q_tokens;
@@ -435,15 +599,11 @@ int specache_window_attend(const specache_window_config* cfg, const specache_vie
     a.window = cfg->window;
     a.sinks = cfg->sinks;
     a.row_tiles = p.row_tiles;
+    a.item_rows = p.item_rows;
     a.chunks = p.chunks;
     a.scale = (cfg->sm_scale > 0.0f ? cfg->sm_scale : 0.08838834764831845f) * kLog2e;
-    const bool bf16 = cfg->dtype == SPECACHE_BF16, split = p.chunks > 1;
-    const auto kernel = bf16 ? (split ? window_kernel<true, true> : window_kernel<true, false>)
-                             : (split ? window_kernel<false, true> : window_kernel<false, false>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.items * p.chunks)), dim3(256), 0, (hipStream_t)stream, a);
-    if (split)
-        hipLaunchKernelGGL(bf16 ? window_merge_kernel<true> : window_merge_kernel<false>, dim3((unsigned)(p.items * kRows / 4)), dim3(256), 0,
-                           (hipStream_t)stream, a);
+    if (cfg->dtype == SPECACHE_BF16) launch<true>(p, a, (hipStream_t)stream);
+    else launch<false>(p, a, (hipStream_t)stream);
     return launched();
 }
 
