@@ -557,7 +557,7 @@ enum { SPECACHE_FP32 = 2 };   /* a type of logits only */
 
 typedef struct specache_sample_config {
     int32_t rows;        /* >= 0                                                                        */
-    int32_t vocab;       /* 1 .. 2^24                                                                   */
+    int32_t vocab;       /* 1 .. 2^20                                                                   */
     int32_t dtype;       /* SPECACHE_FP16, SPECACHE_BF16 or SPECACHE_FP32: type of the logits           */
     int64_t row_stride;  /* elements from a row to the next, >= 0 (0: every row is the first)           */
 } specache_sample_config;

@@ -2,10 +2,13 @@
 //
 // All three limits keep a prefix of the row in the order of its logits (the lower index first among equals), and so is the
 // choice a place in that order: the first element at which a count, or the running sum of the weights, reaches a target.  Nothing
-// is sorted for it.  A histogram over the logarithm of the weights gives every bin's count and sum; the bin that holds the target is taken
-// apart further, by the bits of its logits, until its elements fit in LDS, where they are ranked.  Weights are whole numbers
-// (a binary32 exponential in units of 2^-E of the largest weight), so sums are exact in any order and every way to an element meets the
-// same ones.
+// of the row's length is sorted for it.
+//   - Few tokens kept: those that can be are listed in LDS, sorted there, and their weights summed in order.  With top_k the list is what
+//     is not below the k-th largest of the threads' own maxima (there are k such elements at least, and hardly more); without it, what
+//     a histogram over the logarithm of the weights puts in or before the bin where the kept mass ends.
+//   - Many: the histogram's bin that holds a target is taken apart further, by the bits of its logits, until its elements fit in the list.
+// An element's weight is r 2^(-bin / 64): the power of the bin, of which there are 64 per power of two, and a whole number r of units 2^-R,
+// so that a bin's sum is exact in whatever order it is made; sums of bins and of listed elements are binary64 in a fixed order.
 #include "operators.h"
 
 #include <cmath>
@@ -16,7 +19,9 @@ namespace {
 constexpr int kThreads = 1024, kWavesPerRow = kThreads / 64;
 constexpr int kBins = 2048;            // two per thread
 constexpr float kBinsPerLog2 = 64.0f;  // 32 powers of two of the weights; what is lighter shares the last bin
-constexpr int kFits = 1024;            // elements that are ranked at once
+constexpr int kList = 2048;            // elements that are sorted at once
+constexpr int kRanked = 256;           // of these few each is compared with all the others instead
+constexpr int kMostVocab = 1 << 20;
 
 struct SampleArgs {
     const void* logits;
@@ -24,92 +29,113 @@ struct SampleArgs {
     const int32_t* top_k;
     int32_t* tokens;
     int64_t row_stride;
-    int vocab, unit_log2;              // weights in 2^-unit_log2
-};
-
-struct Place {                         // an element in the order: elements and weights up to and with it
-    uint32_t count;
-    uint64_t mass;
-    int index;
+    int vocab;
+    int unit_log2, count_shift;        // R; a bin is its elements' number << count_shift | the sum of their r
 };
 
 struct Shared {
-    uint32_t count[kBins];
-    uint64_t mass[kBins];
+    uint64_t bins[kBins];
+    uint64_t list[kList];              // descending_key << 32 | index: ascending is the order of the row
+    uint64_t sorted[kRanked];
+    double wave_mass[kWavesPerRow];
     uint32_t wave_count[kWavesPerRow];
-    uint64_t wave_mass[kWavesPerRow];
-    float list_value[kFits];
-    int list_index[kFits];
-    uint32_t list_n, key_low, key_high, found_bin;
-    uint32_t found_count;
-    uint64_t found_mass;
+    float wave_most[kWavesPerRow];
+    int wave_first[kWavesPerRow];
+    uint32_t list_n, key_low, key_high, found_bin, found_count;
+    double found_mass;
     int found_index;
+    double mark_mass[3];
+    uint32_t mark_count[3];
+    uint64_t border_units;
 };
 
-template <typename T> __device__ __forceinline__ float logit_of(T x);
-template <> __device__ __forceinline__ float logit_of<float>(float x) { return x; }
-template <> __device__ __forceinline__ float logit_of<_Float16>(_Float16 x) { return (float)x; }
-template <> __device__ __forceinline__ float logit_of<__bf16>(__bf16 x) { return (float)x; }
+template <typename T> __device__ __forceinline__ float logit_of(T x) { return (float)x; }
 
-// f(logit, index) for every allowed token of a row, in no order.  16-byte loads between the first and the last aligned address.
+// f(vector, first index, elements) over a row: 16-byte loads between the first and the last aligned address, four ahead, single elements
+// before and behind.  A thread's calls come in ascending order of the index.
+template <typename T, typename F>
+__device__ __forceinline__ void each_vector(const T* row, int n, F&& f) {
+    constexpr int kVec = 16 / sizeof(T), kAhead = 4;
+    typedef T Vec __attribute__((ext_vector_type(kVec)));
+    const int head = min(n, (int)((16 - (uintptr_t)row % 16) % 16 / sizeof(T)));
+    const int vecs = (n - head) / kVec, tail = head + vecs * kVec;
+    if ((int)threadIdx.x < head) {
+        Vec x{};
+        x[0] = row[threadIdx.x];
+        f(x, (int)threadIdx.x, 1);
+    }
+    const Vec* body = (const Vec*)(row + head);
+    int v = threadIdx.x;
+    for (; v + (kAhead - 1) * kThreads < vecs; v += kAhead * kThreads) {
+        Vec x[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) x[i] = body[v + i * kThreads];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) f(x[i], head + (v + i * kThreads) * kVec, kVec);
+    }
+    for (; v < vecs; v += kThreads) f(body[v], head + v * kVec, kVec);
+    if (tail + (int)threadIdx.x < n) {
+        Vec x{};
+        x[0] = row[tail + threadIdx.x];
+        f(x, tail + (int)threadIdx.x, 1);
+    }
+}
+// f(logit, index) for every allowed token
 template <typename T, typename F>
 __device__ __forceinline__ void each(const T* row, int n, F&& f) {
     constexpr int kVec = 16 / sizeof(T);
-    const auto one = [&](T x, int i) {
-        const float l = logit_of(x);
-        if (l > -INFINITY) f(l, i);   // (false for NaN as well)
-    };
-    const int head = min(n, (int)((16 - (uintptr_t)row % 16) % 16 / sizeof(T)));
-    const int vecs = (n - head) / kVec;
-    for (int i = threadIdx.x; i < head; i += kThreads) one(row[i], i);
-    typedef T Vec __attribute__((ext_vector_type(kVec)));
-    const Vec* body = (const Vec*)(row + head);
-#pragma unroll 2
-    for (int v = threadIdx.x; v < vecs; v += kThreads) {
-        const Vec x = body[v];
+    each_vector(row, n, [&](const auto& x, int i, int elements) {
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) one(x[e], head + v * kVec + e);
-    }
-    for (int i = head + vecs * kVec + threadIdx.x; i < n; i += kThreads) one(row[i], i);
+        for (int e = 0; e < kVec; ++e) {
+            const float l = logit_of(x[e]);
+            if (l > -INFINITY && e < elements) f(l, i + e);   // (false for NaN as well)
+        }
+    });
 }
 
 struct Weights {
-    float most, per_log2;
-    int unit_log2;
-    // log2 of the weight: never rises as the logit falls
-    __device__ __forceinline__ float log2_of(float l) const { return l == most ? 0.0f : (l - most) * per_log2; }
-    __device__ __forceinline__ uint64_t of_log2(float a) const {
-        const float w = __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(a), unit_log2 - 32);
-        const uint32_t hi = (uint32_t)w;
-        return (uint64_t)hi << 32 | (uint32_t)((w - (float)hi) * 4294967296.0f);
+    float most, bins_per_logit, unit;      // unit: 2^R
+    // bins below the largest logit: never falls as the logit does
+    __device__ __forceinline__ float depth(float l) const { return l == most ? 0.0f : (most - l) * bins_per_logit; }
+    __device__ __forceinline__ uint32_t bin_of(float depth) const { return (uint32_t)fminf(depth, kBins - 1.0f); }
+    __device__ __forceinline__ uint32_t units(float depth, uint32_t bin) const {
+        return (uint32_t)fmaf(__builtin_amdgcn_exp2f(((float)bin - depth) * (1.0f / kBinsPerLog2)), unit, 0.5f);
     }
-    __device__ __forceinline__ uint64_t of(float l) const { return of_log2(log2_of(l)); }
+    __device__ __forceinline__ double of_bin(uint64_t units, uint32_t bin) const {
+        return (double)units * (exp2(-(double)(bin % 64) / kBinsPerLog2) / ((double)unit * (double)(1ull << bin / 64)));
+    }
+    __device__ __forceinline__ double of(float l) const {
+        const float d = depth(l);
+        const uint32_t b = bin_of(d);
+        return of_bin(units(d, b), b);
+    }
 };
 
-__device__ __forceinline__ uint32_t wave_add(uint32_t v) {
-    for (int d = 32; d; d /= 2) v += __shfl_xor(v, d);
-    return v;
-}
-__device__ __forceinline__ uint64_t wave_add(uint64_t v) {
-    for (int d = 32; d; d /= 2) v += __shfl_xor((unsigned long long)v, d);
-    return v;
+__device__ __forceinline__ uint32_t descending_key(float l) { return ~float_to_key(l); }
+__device__ __forceinline__ float logit_of_key(uint32_t descending) {
+    const uint32_t k = ~descending;
+    return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
 }
 
-// the sums of (count, mass) over the threads before this one
-__device__ __forceinline__ void sums_before(Shared& s, uint32_t& count, uint64_t& mass) {
+// the sums of (count, mass) over the threads before this one, in the threads' order
+__device__ __forceinline__ void sums_before(Shared& s, uint32_t& count, double& mass) {
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     uint32_t c = count;
-    uint64_t m = mass;
+    double m = mass;
     for (int d = 1; d < 64; d *= 2) {
         const uint32_t cc = __shfl_up(c, d);
-        const uint64_t mm = __shfl_up((unsigned long long)m, d);
+        const double mm = __shfl_up(m, d);
         if (lane >= d) c += cc, m += mm;
     }
     if (lane == 63) s.wave_count[wave] = c, s.wave_mass[wave] = m;
+    const uint32_t c_before = __shfl_up(c, 1);
+    const double m_before = __shfl_up(m, 1);
+    count = lane ? c_before : 0, mass = lane ? m_before : 0.0;
     __syncthreads();
-    c -= count, m -= mass;
-    for (int w = 0; w < wave; ++w) c += s.wave_count[w], m += s.wave_mass[w];
-    count = c, mass = m;
+    uint32_t cw = 0;
+    double mw = 0.0;
+    for (int w = 0; w < wave; ++w) cw += s.wave_count[w], mw += s.wave_mass[w];
+    count += cw, mass = mw + mass;
     __syncthreads();
 }
 
@@ -118,231 +144,415 @@ struct Target {
     bool by_count, pass;
     uint32_t count;
     double mass;
-    __device__ __forceinline__ bool reached(uint32_t c, uint64_t m) const {
-        return by_count ? c >= count : pass ? (double)m > mass : (double)m >= mass;
-    }
+    __device__ __forceinline__ bool reached(uint32_t c, double m) const { return by_count ? c >= count : pass ? m > mass : m >= mass; }
 };
 
-// Bins in the order of the elements: the one in which the target is reached, with what lies before it.
-__device__ __forceinline__ void find_bin(Shared& s, const Target& t, uint32_t& before_count, uint64_t& before_mass, uint32_t& bin) {
-    const uint32_t c0 = s.count[2 * threadIdx.x], c1 = s.count[2 * threadIdx.x + 1];
-    const uint64_t m0 = s.mass[2 * threadIdx.x], m1 = s.mass[2 * threadIdx.x + 1];
-    uint32_t c = c0 + c1;
-    uint64_t m = m0 + m1;
-    sums_before(s, c, m);
-    c += before_count, m += before_mass;
+struct Place { uint32_t count; double mass; int index; };   // an element: elements and weights up to and with it
+
+// The elements and the mass of the bins before every bin: [bin] for this thread's two and all together.
+struct BinSums {
+    uint32_t count[3];
+    double mass[3];
+};
+// weight_bin < 0: the bins are those of the weights; else they are parts of that one
+__device__ __forceinline__ BinSums sum_bins(Shared& s, const Weights& w, int count_shift, int weight_bin) {
+    BinSums b;
+    const uint64_t mask = (1ull << count_shift) - 1;
+    uint32_t c[2];
+    double m[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint64_t bin = s.bins[2 * threadIdx.x + i];
+        c[i] = (uint32_t)(bin >> count_shift);
+        m[i] = bin ? w.of_bin(bin & mask, weight_bin < 0 ? 2 * threadIdx.x + i : weight_bin) : 0.0;
+    }
+    b.count[0] = c[0] + c[1], b.mass[0] = m[0] + m[1];
+    sums_before(s, b.count[0], b.mass[0]);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) b.count[i + 1] = b.count[i] + c[i], b.mass[i + 1] = b.mass[i] + m[i];
+    return b;
+}
+// The bin in which the target is reached and what lies before it; where it is not (sums made in another order can fall short at the very end):
+// the last one that holds anything, or kBins.
+template <bool OR_LAST>
+__device__ __forceinline__ uint32_t find_bin(Shared& s, const BinSums& b, const Target& t, uint32_t& before_count, double& before_mass) {
     if (threadIdx.x == 0) s.found_bin = kBins;
     __syncthreads();
-    // (exactly one bin: reached with it and not before it; an empty bin changes nothing)
-    const bool r0 = t.reached(c, m), r1 = t.reached(c + c0, m + m0), r2 = t.reached(c + c0 + c1, m + m0 + m1);
-    if (!r0 && r1 && c0) s.found_bin = 2 * threadIdx.x, s.found_count = c, s.found_mass = m;
-    if (!r1 && r2 && c1) s.found_bin = 2 * threadIdx.x + 1, s.found_count = c + c0, s.found_mass = m + m0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)   // (exactly one bin: reached with it and not before it; an empty bin changes nothing)
+        if (!t.reached(before_count + b.count[i], before_mass + b.mass[i]) && t.reached(before_count + b.count[i + 1], before_mass + b.mass[i + 1]))
+            s.found_bin = 2 * threadIdx.x + i, s.found_count = before_count + b.count[i], s.found_mass = before_mass + b.mass[i];
     __syncthreads();
-    bin = s.found_bin;
+    uint32_t bin = s.found_bin;
+    if (OR_LAST && bin == kBins) {
+        __syncthreads();
+        if (threadIdx.x == 0) s.found_bin = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (b.count[i + 1] > b.count[i]) atomicMax(&s.found_bin, 2 * threadIdx.x + i);
+        __syncthreads();
+        bin = s.found_bin;
+        if (threadIdx.x == bin / 2) s.found_count = before_count + b.count[bin % 2], s.found_mass = before_mass + b.mass[bin % 2];
+        __syncthreads();
+    }
     before_count = s.found_count, before_mass = s.found_mass;
+    __syncthreads();
+    return bin;
+}
+
+__device__ __forceinline__ void clear_bins(Shared& s) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < kBins; i += kThreads) s.bins[i] = 0;
     __syncthreads();
 }
 
-__device__ __forceinline__ uint32_t descending_key(float l) { return ~float_to_key(l); }
+// The listed elements (n of them, at most kList), sorted.
+__device__ __forceinline__ const uint64_t* sort_list(Shared& s, uint32_t n) {
+    if (n <= kRanked) {
+        if (threadIdx.x < n) {
+            const uint64_t x = s.list[threadIdx.x];
+            uint32_t rank = 0;
+            for (uint32_t j = 0; j < n; ++j) rank += s.list[j] < x;
+            s.sorted[rank] = x;
+        }
+        __syncthreads();
+        return s.sorted;
+    }
+    uint32_t all = 2 * kRanked;
+    while (all < n) all *= 2;
+    for (uint32_t i = n + threadIdx.x; i < all; i += kThreads) s.list[i] = ~0ull;
+    for (uint32_t size = 2; size <= all; size *= 2)
+        for (uint32_t apart = size / 2; apart; apart /= 2) {
+            __syncthreads();
+            const uint32_t t = threadIdx.x;
+            if (t < all / 2) {
+                const uint32_t i = 2 * apart * (t / apart) + t % apart, j = i + apart;
+                const uint64_t x = s.list[i], y = s.list[j];
+                if ((x > y) == !(i & size)) s.list[i] = y, s.list[j] = x;
+            }
+        }
+    __syncthreads();
+    return s.list;
+}
 
-// The element at which t is reached; the histogram of all elements by log2 of the weights is in s.count, s.mass on entry and
-// may be gone on return.
+// this thread's two places in the sorted list: counts and masses up to and with them, beginning with what lies before the list
+__device__ __forceinline__ void sum_list(Shared& s, const Weights& w, const uint64_t* list, uint32_t n, uint32_t before_count, double before_mass,
+                                         uint32_t (&count)[3], double (&mass)[3]) {
+    double m[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) m[i] = 2 * threadIdx.x + i < n ? w.of(logit_of_key((uint32_t)(list[2 * threadIdx.x + i] >> 32))) : 0.0;
+    count[0] = 0, mass[0] = m[0] + m[1];
+    sums_before(s, count[0], mass[0]);
+    mass[0] = before_mass + mass[0];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) mass[i + 1] = mass[i] + m[i];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) count[i] = before_count + min(2 * threadIdx.x + i, n);
+}
+
+// The element at which t is reached, from the weights' histogram in s.bins; kept is false where that had to make room.
 template <typename T>
-__device__ Place find(Shared& s, const T* row, int n, const Weights& w, const Target& t) {
-    uint32_t before_count = 0, bin;
-    uint64_t before_mass = 0;
-    find_bin(s, t, before_count, before_mass, bin);
-    if (bin == kBins) return Place{0, 0, -1};   // the target is not reached
-    bool by_log2 = true;
+__device__ __forceinline__ Place find(Shared& s, const T* row, const SampleArgs& a, const Weights& w, const Target& t, bool& kept) {
+    const int n = a.vocab;
+    uint32_t before_count = 0;
+    double before_mass = 0.0;
+    uint32_t bin = find_bin<true>(s, sum_bins(s, w, a.count_shift, -1), t, before_count, before_mass);
+    const uint32_t weight_bin = bin;
     uint32_t low = 0, high = 0xFFFFFFFFu;
     const auto inside = [&](float l) {
-        if (by_log2) return (uint32_t)fminf(-w.log2_of(l) * kBinsPerLog2, kBins - 1.0f) == bin;
         const uint32_t k = descending_key(l);
-        return k >= low && k <= high;
+        return w.bin_of(w.depth(l)) == weight_bin && k >= low && k <= high;
     };
-    uint32_t here = s.count[bin];
-    __syncthreads();
-    while (here > kFits) {
+    uint32_t here = (uint32_t)(s.bins[bin] >> a.count_shift);
+    bool equal = false;
+    while (here > kList && !equal) {
+        kept = false;
         if (threadIdx.x == 0) s.key_low = 0xFFFFFFFFu, s.key_high = 0;
-        __syncthreads();
+        clear_bins(s);
         uint32_t k_min = 0xFFFFFFFFu, k_max = 0;
         each(row, n, [&](float l, int) {
-            if (inside(l)) {
-                const uint32_t k = descending_key(l);
-                k_min = min(k_min, k), k_max = max(k_max, k);
-            }
+            if (inside(l)) k_min = min(k_min, descending_key(l)), k_max = max(k_max, descending_key(l));
         });
         atomicMin(&s.key_low, k_min);
         atomicMax(&s.key_high, k_max);
         __syncthreads();
-        const uint32_t new_low = s.key_low, new_high = s.key_high;
-        if (new_low == new_high) break;         // all equal
-        const uint32_t span = new_high - new_low;
-        const int shift = span < kBins ? 0 : 32 - __builtin_clz(span) - 11;
-        for (int i = threadIdx.x; i < kBins; i += kThreads) s.count[i] = 0, s.mass[i] = 0;
-        __syncthreads();
+        const uint32_t from = s.key_low, span = s.key_high - from;
+        equal = span == 0;   // (key_low is theirs)
+        if (equal) break;
+        const int shift = span < kBins ? 0 : 21 - __builtin_clz(span);
         each(row, n, [&](float l, int) {
-            if (inside(l)) {
-                const uint32_t at = (descending_key(l) - new_low) >> shift;
-                atomicAdd(&s.count[at], 1u);
-                atomicAdd((unsigned long long*)&s.mass[at], (unsigned long long)w.of(l));
-            }
+            if (inside(l)) atomicAdd((unsigned long long*)&s.bins[(descending_key(l) - from) >> shift], 1ull << a.count_shift | w.units(w.depth(l), weight_bin));
         });
         __syncthreads();
-        find_bin(s, t, before_count, before_mass, bin);
-        by_log2 = false;
-        low = new_low + (bin << shift);
+        bin = find_bin<true>(s, sum_bins(s, w, a.count_shift, weight_bin), t, before_count, before_mass);
+        low = from + (bin << shift);
         high = low + ((1u << shift) - 1);
-        here = s.count[bin];
+        here = (uint32_t)(s.bins[bin] >> a.count_shift);
         __syncthreads();
     }
-    if (here > kFits) {
-        // equal ones, in the order of their indices: every thread counts a stretch of the row
-        const int per = (n + kThreads - 1) / kThreads, from = min(n, (int)threadIdx.x * per), to = min(n, from + per);
+    if (equal) {
+        // which of them it is, and that one in the order of their indices: every thread counts a stretch of the row
+        const double one = w.of(logit_of_key(s.key_low));
+        uint32_t k = here;
+        if (t.by_count) k = t.count - before_count;
+        else if (one > 0.0) k = (uint32_t)fmin(fmax((t.mass - before_mass) / one, 1.0), (double)here);
+        while (k < here && !t.reached(before_count + k, before_mass + k * one)) ++k;
+        while (k > 1 && t.reached(before_count + k - 1, before_mass + (k - 1) * one)) --k;
+        const int per = (n + kThreads - 1) / kThreads, begin = min(n, (int)threadIdx.x * per), end = min(n, begin + per);
         const auto same = [&](int i) {
             const float l = logit_of(row[i]);
             return l > -INFINITY && inside(l);
         };
         uint32_t c = 0;
-        float value = 0;
-        for (int i = from; i < to; ++i)
-            if (same(i)) ++c, value = logit_of(row[i]);
-        const uint64_t each_one = c ? w.of(value) : 0;
+        for (int i = begin; i < end; ++i) c += same(i);
         uint32_t place = c;
-        uint64_t mass = c * each_one;
-        sums_before(s, place, mass);
-        place += before_count, mass += before_mass;
-        if (c && !t.reached(place, mass) && t.reached(place + c, mass + c * each_one))
-            for (int i = from; i < to; ++i)
-                if (same(i)) {
-                    ++place, mass += each_one;
-                    if (t.reached(place, mass)) {
-                        s.found_count = place, s.found_mass = mass, s.found_index = i;
-                        break;
-                    }
-                }
+        double unused = 0.0;
+        sums_before(s, place, unused);
+        if (place < k && k <= place + c)
+            for (int i = begin; i < end; ++i)
+                if (same(i) && ++place == k) s.found_index = i;
         __syncthreads();
-        const Place p{s.found_count, s.found_mass, s.found_index};
+        const Place p{before_count + k, before_mass + k * one, s.found_index};
         __syncthreads();
         return p;
     }
     if (threadIdx.x == 0) s.list_n = 0;
     __syncthreads();
     each(row, n, [&](float l, int i) {
-        if (inside(l)) {
-            const uint32_t at = atomicAdd(&s.list_n, 1u);
-            if (at < kFits) s.list_value[at] = l, s.list_index[at] = i;
-        }
+        if (inside(l)) s.list[atomicAdd(&s.list_n, 1u)] = (uint64_t)descending_key(l) << 32 | (uint32_t)i;   // (here of them)
     });
     __syncthreads();
-    // every element's rank and the weights ahead of it
-    const uint32_t have = min(s.list_n, (uint32_t)kFits);
-    if (threadIdx.x < have) {
-        const float l = s.list_value[threadIdx.x];
-        const int i = s.list_index[threadIdx.x];
-        uint32_t c = before_count + 1;
-        uint64_t m = before_mass + w.of(l);
-        for (uint32_t j = 0; j < have; ++j) {
-            const float lj = s.list_value[j];
-            if (lj > l || (lj == l && s.list_index[j] < i)) ++c, m += w.of(lj);
-        }
-        if (t.reached(c, m) && !t.reached(c - 1, m - w.of(l))) s.found_count = c, s.found_mass = m, s.found_index = i;
-    }
+    const uint32_t have = s.list_n;
+    const uint64_t* list = sort_list(s, have);
+    uint32_t count[3];
+    double mass[3];
+    sum_list(s, w, list, have, before_count, before_mass, count, mass);
+    // the first that reaches it, or the last one
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (2 * threadIdx.x + i < have && !t.reached(count[i], mass[i]) && (t.reached(count[i + 1], mass[i + 1]) || 2 * threadIdx.x + i + 1 == have))
+            s.found_count = count[i + 1], s.found_mass = mass[i + 1], s.found_index = (int)(uint32_t)list[2 * threadIdx.x + i];
     __syncthreads();
     const Place p{s.found_count, s.found_mass, s.found_index};
     __syncthreads();
     return p;
 }
 
+// What limits a row's choice; a limit that is off: count = all, mass_part >= 1, depth < 0.
+struct Limits {
+    uint32_t count;
+    float mass_part, depth, u;
+};
+
+// The choice from a sorted list that holds all kept elements.  total: the mass of which mass_part is kept; < 0: that of the first lim.count.
+__device__ __forceinline__ int choose(Shared& s, const Weights& w, const uint64_t* list, uint32_t n, const Limits& lim, double total) {
+    uint32_t count[3];
+    double mass[3];
+    sum_list(s, w, list, n, 0, 0.0, count, mass);
+    const uint32_t first = 2 * threadIdx.x, n_count = min(lim.count, n);
+    if (threadIdx.x == 0) s.mark_count[0] = s.mark_count[1] = n_count, s.mark_count[2] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (first + i + 1 == n_count) s.mark_mass[0] = mass[i + 1];
+    __syncthreads();
+    if (lim.mass_part < 1.0f) {
+        const double need = (double)lim.mass_part * (total < 0.0 ? s.mark_mass[0] : total);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)   // (one place at most)
+            if (first + i < n_count && (first + i == 0 || mass[i] < need) && mass[i + 1] >= need) s.mark_count[0] = first + i + 1;
+    }
+    if (lim.depth >= 0.0f) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (first + i < n) {
+                const bool here = w.depth(logit_of_key((uint32_t)(list[first + i] >> 32))) <= lim.depth;
+                const bool next = first + i + 1 < n && w.depth(logit_of_key((uint32_t)(list[first + i + 1] >> 32))) <= lim.depth;
+                if (here && !next) s.mark_count[1] = first + i + 1;
+            }
+    }
+    __syncthreads();
+    const uint32_t kept = min(s.mark_count[0], s.mark_count[1]);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (first + i + 1 == kept) s.mark_mass[1] = mass[i + 1], s.mark_count[2] = first + i;
+    __syncthreads();
+    const double need = (double)lim.u * s.mark_mass[1];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (first + i < kept && mass[i] <= need && mass[i + 1] > need) s.mark_count[2] = first + i;
+    __syncthreads();
+    return (int)(uint32_t)list[s.mark_count[2]];
+}
+
+// A workgroup per row.  @SAMPLE@
 template <typename T>
 __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     __shared__ Shared s;
     const int r = blockIdx.x, n = a.vocab;
     const T* row = (const T*)a.logits + r * a.row_stride;
+    constexpr int kVec = 16 / sizeof(T);
 
-    // the largest logit and its first place
-    float most = -INFINITY;
-    int first = 0x7FFFFFFF;
-    each(row, n, [&](float l, int i) {
-        if (l > most || (l == most && i < first)) most = l, first = i;
+    // the largest logit; a thread keeps where its own largest one is first
+    float own_most = -INFINITY;
+    int own_at = 0;
+    each_vector(row, n, [&](const auto& x, int i, int elements) {
+        float most = logit_of(x[0]);
+#pragma unroll
+        for (int e = 1; e < kVec; ++e) most = fmaxf(most, e < elements ? logit_of(x[e]) : -INFINITY);
+        if (most > own_most) own_most = most, own_at = i;
     });
-    for (int d = 32; d; d /= 2) {
-        const float l = __shfl_xor(most, d);
-        const int i = __shfl_xor(first, d);
-        if (l > most || (l == most && i < first)) most = l, first = i;
-    }
-    if (threadIdx.x % 64 == 0) s.list_value[threadIdx.x / 64] = most, s.list_index[threadIdx.x / 64] = first;
+    float most = own_most;
+    for (int d = 32; d; d /= 2) most = fmaxf(most, __shfl_xor(most, d));
+    if (threadIdx.x % 64 == 0) s.wave_most[threadIdx.x / 64] = most;
+    if (threadIdx.x == 0) s.key_low = 0x7FFFFFFFu, s.key_high = 0, s.list_n = 0;
     __syncthreads();
-    for (int w = 0; w < kWavesPerRow; ++w) {
-        const float l = s.list_value[w];
-        const int i = s.list_index[w];
-        if (l > most || (l == most && i < first)) most = l, first = i;
-    }
+    for (int w = 0; w < kWavesPerRow; ++w) most = fmaxf(most, s.wave_most[w]);
     float temperature = a.temperature ? a.temperature[r] : 1.0f;
     if (temperature != temperature) temperature = 1.0f;
     if (temperature <= 0.0f || most == -INFINITY) {
-        if (threadIdx.x == 0) a.tokens[r] = most == -INFINITY ? -1 : first;
+        if (own_most == most && most > -INFINITY)
+            for (int i = own_at; i < min(own_at + kVec, n); ++i)
+                if (logit_of(row[i]) == most) {
+                    atomicMin(&s.key_low, (uint32_t)i);
+                    break;
+                }
+        __syncthreads();
+        if (threadIdx.x == 0) a.tokens[r] = most == -INFINITY ? -1 : (int)s.key_low;
         return;
     }
-    const Weights w{most, 1.44269504088896340736f / temperature, a.unit_log2};
+    const Weights w{most, kBinsPerLog2 * 1.44269504088896340736f / temperature, __builtin_amdgcn_ldexpf(1.0f, a.unit_log2)};
     const int top_k = a.top_k ? a.top_k[r] : 0;
     const float top_p = a.top_p ? a.top_p[r] : 1.0f, min_p = a.min_p ? a.min_p[r] : 0.0f;
-    const float min_log2 = min_p > 0.0f ? fminf(log2f(min_p), 0.0f) : -INFINITY;
-    const float u = fminf(fmaxf(a.u[r], 0.0f), 0x1.fffffep-1f);
+    Limits lim;
+    lim.count = top_k > 0 && top_k < n ? top_k : 0xFFFFFFFFu;
+    if (top_p <= 0.0f) lim.count = 1;
+    lim.mass_part = top_p > 0.0f && top_p < 1.0f ? top_p : 1.0f;
+    lim.depth = min_p > 0.0f ? fmaxf(-kBinsPerLog2 * log2f(min_p), 0.0f) : -1.0f;
+    lim.u = fminf(fmaxf(a.u[r], 0.0f), 0x1.fffffep-1f);
 
-    uint32_t all = 0, heavy = 0;
-    uint64_t all_mass = 0, heavy_mass = 0;
-    const auto histogram = [&]() {
+    if (lim.count <= kThreads) {
+        // the bin of the count-th largest of the threads' own largest, the least of those up to there, and what is not below it
+        clear_bins(s);
+        const uint32_t own_bin = w.bin_of(w.depth(own_most));
+        if (own_most > -INFINITY) atomicAdd((unsigned long long*)&s.bins[own_bin], 1ull << a.count_shift);
         __syncthreads();
-        for (int i = threadIdx.x; i < kBins; i += kThreads) s.count[i] = 0, s.mass[i] = 0;
+        uint32_t before_count = 0;
+        double before_mass = 0.0;
+        const uint32_t bin = find_bin<false>(s, sum_bins(s, w, a.count_shift, -1), Target{true, false, lim.count, 0.0}, before_count, before_mass);
+        if (own_most > -INFINITY && own_bin <= bin) atomicMax(&s.key_high, descending_key(own_most));
         __syncthreads();
-        uint32_t c = 0, hc = 0;
-        uint64_t m = 0, hm = 0;
-        each(row, n, [&](float l, int) {
-            const float at = w.log2_of(l);
-            const uint64_t mass = w.of_log2(at);
-            const uint32_t bin = (uint32_t)fminf(-at * kBinsPerLog2, kBins - 1.0f);
-            atomicAdd(&s.count[bin], 1u);
-            atomicAdd((unsigned long long*)&s.mass[bin], (unsigned long long)mass);
-            ++c, m += mass;
-            if (at >= min_log2) ++hc, hm += mass;
+        const float least = bin == kBins ? -INFINITY : logit_of_key(s.key_high);
+        each_vector(row, n, [&](const auto& x, int i, int elements) {
+            float l[kVec];
+            bool any = false;
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) {
+                l[e] = e < elements ? logit_of(x[e]) : -INFINITY;
+                any |= l[e] >= least;
+            }
+            if (any)
+#pragma unroll
+                for (int e = 0; e < kVec; ++e)
+                    if (l[e] >= least && l[e] > -INFINITY) {
+                        const uint32_t at = atomicAdd(&s.list_n, 1u);
+                        if (at < kList) s.list[at] = (uint64_t)descending_key(l[e]) << 32 | (uint32_t)(i + e);
+                    }
         });
-        all = c, all_mass = m, heavy = hc, heavy_mass = hm;
         __syncthreads();
-    };
-    const auto over_the_row = [&](uint32_t& c, uint64_t& m) {
-        c = wave_add(c), m = wave_add(m);
-        if (threadIdx.x % 64 == 0) s.wave_count[threadIdx.x / 64] = c, s.wave_mass[threadIdx.x / 64] = m;
-        __syncthreads();
-        c = 0, m = 0;
-        for (int i = 0; i < kWavesPerRow; ++i) c += s.wave_count[i], m += s.wave_mass[i];
+        const uint32_t listed = s.list_n;
+        if (listed <= kList) {
+            const int token = choose(s, w, sort_list(s, listed), listed, lim, -1.0);
+            if (threadIdx.x == 0) a.tokens[r] = token;
+            return;
+        }
+    }
+
+    const auto histogram = [&]() {
+        clear_bins(s);
+        each(row, n, [&](float l, int) {
+            const float d = w.depth(l);
+            const uint32_t bin = w.bin_of(d);
+            atomicAdd((unsigned long long*)&s.bins[bin], 1ull << a.count_shift | w.units(d, bin));
+        });
         __syncthreads();
     };
     histogram();
-    over_the_row(all, all_mass);
-    over_the_row(heavy, heavy_mass);
+    const BinSums bins = sum_bins(s, w, a.count_shift, -1);
+    if (threadIdx.x == kThreads - 1) s.mark_count[0] = bins.count[2], s.mark_mass[0] = bins.mass[2];
+    __syncthreads();
+    const uint32_t all = s.mark_count[0];
+    const double all_mass = s.mark_mass[0];
+    const bool count_on = lim.count < all, mass_on = lim.mass_part < 1.0f, depth_on = lim.depth >= 0.0f;
+    // the bin behind which nothing is kept
+    uint32_t end = kBins - 1;
+    uint32_t before_count = 0;
+    double before_mass = 0.0;
+    if (count_on) end = min(end, find_bin<false>(s, bins, Target{true, false, lim.count, 0.0}, before_count, before_mass));
+    else if (mass_on) end = min(end, find_bin<false>(s, bins, Target{false, false, 0, (double)lim.mass_part * all_mass}, before_count, before_mass));
+    if (depth_on && !(count_on && mass_on)) end = min(end, w.bin_of(lim.depth));
+    if (threadIdx.x == end / 2) s.mark_count[1] = bins.count[end % 2 + 1];
+    if (threadIdx.x == 0) s.list_n = 0;
+    __syncthreads();
+    if (s.mark_count[1] <= kList) {
+        each(row, n, [&](float l, int i) {
+            if (w.bin_of(w.depth(l)) <= end) s.list[atomicAdd(&s.list_n, 1u)] = (uint64_t)descending_key(l) << 32 | (uint32_t)i;
+        });
+        __syncthreads();
+        const uint32_t listed = s.list_n;
+        const int token = choose(s, w, sort_list(s, listed), listed, lim, count_on ? -1.0 : all_mass);
+        if (threadIdx.x == 0) a.tokens[r] = token;
+        return;
+    }
+
     uint32_t kept = all;
-    uint64_t mass = all_mass;
-    const uint32_t heavy_count = heavy;
-    const uint64_t heavy_sum = heavy_mass;
-    if (top_k > 0 && (uint32_t)top_k < all) {
-        const Place p = find(s, row, n, w, Target{true, false, (uint32_t)top_k, 0.0});
-        kept = p.count, mass = p.mass;
-        histogram();
+    double mass = all_mass;
+    bool whole = true;                 // s.bins are still those of the row
+    if (depth_on) {
+        // whole bins, and of the one that holds the border what is not behind it
+        const uint32_t border = w.bin_of(lim.depth);
+        uint32_t c = 0;
+        uint64_t units = 0;
+        each(row, n, [&](float l, int) {
+            const float d = w.depth(l);
+            if (!(d <= lim.depth)) return;
+            ++c;
+            if (w.bin_of(d) == border) units += w.units(d, border);
+        });
+        if (threadIdx.x == 0) s.mark_count[1] = 0, s.border_units = 0;
+        if (threadIdx.x == border / 2) s.mark_mass[1] = bins.mass[border % 2];
+        __syncthreads();
+        atomicAdd(&s.mark_count[1], c);
+        atomicAdd((unsigned long long*)&s.border_units, (unsigned long long)units);
+        __syncthreads();
+        if (threadIdx.x == 0) s.mark_mass[1] += w.of_bin(s.border_units, border);
+        __syncthreads();
     }
-    if (top_p < 1.0f) {
-        const Place p = find(s, row, n, w, top_p > 0.0f ? Target{false, false, 0, (double)top_p * (double)mass} : Target{true, false, 1, 0.0});
-        if (p.count && p.count < kept) kept = p.count, mass = p.mass;
-        histogram();
+    const uint32_t heavy = depth_on ? s.mark_count[1] : all;
+    const double heavy_mass = depth_on ? s.mark_mass[1] : all_mass;
+    // the end of the first top_k, of the mass that is kept of them, and the choice
+    for (int stage = count_on ? 0 : mass_on ? 1 : 2; stage < 3; ++stage) {
+        if (stage == 1 && !mass_on) continue;
+        if (stage == 2 && heavy < kept) mass = heavy_mass;
+        Target t;
+        t.by_count = stage == 0, t.pass = stage == 2, t.count = lim.count;
+        t.mass = (stage == 1 ? (double)lim.mass_part : (double)lim.u) * mass;
+        if (!whole) histogram();
+        whole = true;
+        const Place p = find(s, row, a, w, t, whole);
+        if (stage == 2) {
+            if (threadIdx.x == 0) a.tokens[r] = p.index;
+        } else if (p.count < kept) {
+            kept = p.count, mass = p.mass;
+        }
     }
-    if (heavy_count < kept) mass = heavy_sum;
-    const Place p = find(s, row, n, w, Target{false, true, 0, (double)u * (double)mass});
-    if (threadIdx.x == 0) a.tokens[r] = p.index;
 }
 
 int check(const specache_sample_config* c) {
     if (!c) return fail_without_context(SPECACHE_EINVAL, "null configuration");
-    if (c->rows < 0 || c->vocab < 1 || c->vocab > (1 << 24)) return fail_without_context(SPECACHE_EINVAL, "rows must not be negative, vocab 1 to 2^24");
+    if (c->rows < 0 || c->vocab < 1 || c->vocab > kMostVocab) return fail_without_context(SPECACHE_EINVAL, "rows must not be negative, vocab 1 to 2^20");
     if (c->dtype != SPECACHE_FP16 && c->dtype != SPECACHE_BF16 && c->dtype != SPECACHE_FP32)
         return fail_without_context(SPECACHE_EINVAL, "dtype must be SPECACHE_FP16, SPECACHE_BF16 or SPECACHE_FP32");
     if (c->row_stride < 0) return fail_without_context(SPECACHE_EINVAL, "row_stride must not be negative");
@@ -373,10 +583,12 @@ int specache_sample(const specache_sample_config* cfg, const void* logits, const
     for (const void* x : {(const void*)u, (const void*)tokens, (const void*)temperature, (const void*)top_k, (const void*)top_p, (const void*)min_p})
         if ((uintptr_t)x % 4) return fail_without_context(SPECACHE_EINVAL, "u, tokens and parameters must be 4-byte aligned");
     if (!u || !tokens) return fail_without_context(SPECACHE_EINVAL, "null u or tokens");
-    SampleArgs a{logits, u, temperature, top_p, min_p, top_k, tokens, cfg->row_stride, cfg->vocab, 0};
+    SampleArgs a{logits, u, temperature, top_p, min_p, top_k, tokens, cfg->row_stride, cfg->vocab, 0, 0};
+    // 2^bits >= vocab elements: bits + 1 bits for their number, bits + R + 1 for the sum of their r <= 2^R
     int bits = 0;
     while ((1 << bits) < cfg->vocab) ++bits;
-    a.unit_log2 = 62 - bits < 46 ? 62 - bits : 46;   // the sum of a row stays below 2^63
+    a.unit_log2 = 62 - 2 * bits < 28 ? 62 - 2 * bits : 28;
+    a.count_shift = bits + a.unit_log2 + 1;
     const auto kernel = cfg->dtype == SPECACHE_FP32 ? sample_kernel<float> : cfg->dtype == SPECACHE_BF16 ? sample_kernel<__bf16> : sample_kernel<_Float16>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)cfg->rows), dim3(kThreads), 0, (hipStream_t)stream, a);
     return launched();

@@ -125,7 +125,7 @@ def _sample(cfg, logits=A, u=A, temperature=None, top_k=None, top_p=None, min_p=
 
 
 def test_sample_refuses():
-    for cfg in (None, SampleConfig(-1, 10, 0, 10), SampleConfig(1, 0, 0, 10), SampleConfig(1, (1 << 24) + 1, 0, 1 << 25), SampleConfig(1, 10, 3, 10), SampleConfig(1, 10, 0, -1)):
+    for cfg in (None, SampleConfig(-1, 10, 0, 10), SampleConfig(1, 0, 0, 10), SampleConfig(1, (1 << 20) + 1, 0, 1 << 21), SampleConfig(1, 10, 3, 10), SampleConfig(1, 10, 0, -1)):
         assert _sample(cfg) == binding.EINVAL
         if cfg is not None:
             assert binding.lib().specache_sample_scratch(C.byref(cfg), C.byref(C.c_int64())) == binding.EINVAL
