@@ -47,6 +47,7 @@ struct Shared {
     double mark_mass[3];
     uint32_t mark_count[3];
     uint64_t border_units;
+    double power[64];                  // 2^(-i / 64) / 2^R
 };
 
 template <typename T> __device__ __forceinline__ float logit_of(T x) { return (float)x; }
@@ -94,15 +95,16 @@ __device__ __forceinline__ void each(const T* row, int n, F&& f) {
 }
 
 struct Weights {
-    float most, bins_per_logit, unit;      // unit: 2^R
-    // bins below the largest logit: never falls as the logit does
-    __device__ __forceinline__ float depth(float l) const { return l == most ? 0.0f : (most - l) * bins_per_logit; }
+    float most, bins_per_logit, unit;      // bins_per_logit: above 0; unit: 2^R
+    const double* power;
+    // bins below the largest logit: never falls as the logit does (0 for the difference of two infinities)
+    __device__ __forceinline__ float depth(float l) const { return fmaxf((most - l) * bins_per_logit, 0.0f); }
     __device__ __forceinline__ uint32_t bin_of(float depth) const { return (uint32_t)fminf(depth, kBins - 1.0f); }
     __device__ __forceinline__ uint32_t units(float depth, uint32_t bin) const {
         return (uint32_t)fmaf(__builtin_amdgcn_exp2f(((float)bin - depth) * (1.0f / kBinsPerLog2)), unit, 0.5f);
     }
     __device__ __forceinline__ double of_bin(uint64_t units, uint32_t bin) const {
-        return (double)units * (exp2(-(double)(bin % 64) / kBinsPerLog2) / ((double)unit * (double)(1ull << bin / 64)));
+        return __builtin_amdgcn_ldexp((double)units * power[bin % 64], -(int)(bin / 64));
     }
     __device__ __forceinline__ double of(float l) const {
         const float d = depth(l);
@@ -155,6 +157,7 @@ struct BinSums {
     double mass[3];
 };
 // weight_bin < 0: the bins are those of the weights; else they are parts of that one
+template <bool MASS = true>
 __device__ __forceinline__ BinSums sum_bins(Shared& s, const Weights& w, int count_shift, int weight_bin) {
     BinSums b;
     const uint64_t mask = (1ull << count_shift) - 1;
@@ -164,7 +167,7 @@ __device__ __forceinline__ BinSums sum_bins(Shared& s, const Weights& w, int cou
     for (int i = 0; i < 2; ++i) {
         const uint64_t bin = s.bins[2 * threadIdx.x + i];
         c[i] = (uint32_t)(bin >> count_shift);
-        m[i] = bin ? w.of_bin(bin & mask, weight_bin < 0 ? 2 * threadIdx.x + i : weight_bin) : 0.0;
+        m[i] = MASS && bin ? w.of_bin(bin & mask, weight_bin < 0 ? 2 * threadIdx.x + i : weight_bin) : 0.0;
     }
     b.count[0] = c[0] + c[1], b.mass[0] = m[0] + m[1];
     sums_before(s, b.count[0], b.mass[0]);
@@ -193,7 +196,7 @@ __device__ __forceinline__ uint32_t find_bin(Shared& s, const BinSums& b, const 
             if (b.count[i + 1] > b.count[i]) atomicMax(&s.found_bin, 2 * threadIdx.x + i);
         __syncthreads();
         bin = s.found_bin;
-        if (threadIdx.x == bin / 2) s.found_count = before_count + b.count[bin % 2], s.found_mass = before_mass + b.mass[bin % 2];
+        if (threadIdx.x == bin / 2) s.found_count = before_count + (bin % 2 ? b.count[1] : b.count[0]), s.found_mass = before_mass + (bin % 2 ? b.mass[1] : b.mass[0]);
         __syncthreads();
     }
     before_count = s.found_count, before_mass = s.found_mass;
@@ -408,6 +411,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     for (int d = 32; d; d /= 2) most = fmaxf(most, __shfl_xor(most, d));
     if (threadIdx.x % 64 == 0) s.wave_most[threadIdx.x / 64] = most;
     if (threadIdx.x == 0) s.key_low = 0x7FFFFFFFu, s.key_high = 0, s.list_n = 0;
+    if (threadIdx.x < 64) s.power[threadIdx.x] = exp2(-(double)threadIdx.x / 64 - a.unit_log2);
     __syncthreads();
     for (int w = 0; w < kWavesPerRow; ++w) most = fmaxf(most, s.wave_most[w]);
     float temperature = a.temperature ? a.temperature[r] : 1.0f;
@@ -423,7 +427,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
         if (threadIdx.x == 0) a.tokens[r] = most == -INFINITY ? -1 : (int)s.key_low;
         return;
     }
-    const Weights w{most, kBinsPerLog2 * 1.44269504088896340736f / temperature, __builtin_amdgcn_ldexpf(1.0f, a.unit_log2)};
+    const Weights w{most, fmaxf(kBinsPerLog2 * 1.44269504088896340736f / temperature, 0x1p-126f), __builtin_amdgcn_ldexpf(1.0f, a.unit_log2), s.power};
     const int top_k = a.top_k ? a.top_k[r] : 0;
     const float top_p = a.top_p ? a.top_p[r] : 1.0f, min_p = a.min_p ? a.min_p[r] : 0.0f;
     Limits lim;
@@ -433,7 +437,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     lim.depth = min_p > 0.0f ? fmaxf(-kBinsPerLog2 * log2f(min_p), 0.0f) : -1.0f;
     lim.u = fminf(fmaxf(a.u[r], 0.0f), 0x1.fffffep-1f);
 
-    if (lim.count <= kThreads) {
+    if (lim.count <= kThreads * 3 / 4) {
         // the bin of the count-th largest of the threads' own largest, the least of those up to there, and what is not below it
         clear_bins(s);
         const uint32_t own_bin = w.bin_of(w.depth(own_most));
@@ -441,7 +445,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
         __syncthreads();
         uint32_t before_count = 0;
         double before_mass = 0.0;
-        const uint32_t bin = find_bin<false>(s, sum_bins(s, w, a.count_shift, -1), Target{true, false, lim.count, 0.0}, before_count, before_mass);
+        const uint32_t bin = find_bin<false>(s, sum_bins<false>(s, w, a.count_shift, -1), Target{true, false, lim.count, 0.0}, before_count, before_mass);
         if (own_most > -INFINITY && own_bin <= bin) atomicMax(&s.key_high, descending_key(own_most));
         __syncthreads();
         const float least = bin == kBins ? -INFINITY : logit_of_key(s.key_high);
@@ -493,7 +497,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     if (count_on) end = min(end, find_bin<false>(s, bins, Target{true, false, lim.count, 0.0}, before_count, before_mass));
     else if (mass_on) end = min(end, find_bin<false>(s, bins, Target{false, false, 0, (double)lim.mass_part * all_mass}, before_count, before_mass));
     if (depth_on && !(count_on && mass_on)) end = min(end, w.bin_of(lim.depth));
-    if (threadIdx.x == end / 2) s.mark_count[1] = bins.count[end % 2 + 1];
+    if (threadIdx.x == end / 2) s.mark_count[1] = end % 2 ? bins.count[2] : bins.count[1];
     if (threadIdx.x == 0) s.list_n = 0;
     __syncthreads();
     if (s.mark_count[1] <= kList) {
@@ -522,7 +526,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
             if (w.bin_of(d) == border) units += w.units(d, border);
         });
         if (threadIdx.x == 0) s.mark_count[1] = 0, s.border_units = 0;
-        if (threadIdx.x == border / 2) s.mark_mass[1] = bins.mass[border % 2];
+        if (threadIdx.x == border / 2) s.mark_mass[1] = border % 2 ? bins.mass[1] : bins.mass[0];
         __syncthreads();
         atomicAdd(&s.mark_count[1], c);
         atomicAdd((unsigned long long*)&s.border_units, (unsigned long long)units);
@@ -532,6 +536,63 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     }
     const uint32_t heavy = depth_on ? s.mark_count[1] : all;
     const double heavy_mass = depth_on ? s.mark_mass[1] : all_mass;
+    // Without top_k the end of the kept mass and the choice are looked for together: the bin of the first is known, and so is, but for that bin's own
+    // mass, the choice's, hardly ever more than one; their elements are listed side by side.
+    if (mass_on && !count_on) {
+        const double need = (double)lim.mass_part * all_mass;
+        uint32_t c_end = 0, c_low = 0, c_high = 0;
+        double m_end = 0.0, m_low = 0.0, m_high = 0.0;
+        const uint32_t b_end = find_bin<true>(s, bins, Target{false, false, 0, need}, c_end, m_end);
+        const double m_most = m_end + w.of_bin(s.bins[b_end] & ((1ull << a.count_shift) - 1), b_end);
+        const double least = heavy < c_end ? heavy_mass : m_end, most_kept = heavy < c_end ? heavy_mass : m_most;
+        const uint32_t b_low = find_bin<true>(s, bins, Target{false, true, 0, (double)lim.u * least}, c_low, m_low);
+        const uint32_t b_high = find_bin<true>(s, bins, Target{false, true, 0, (double)lim.u * most_kept}, c_high, m_high);
+        if (threadIdx.x == b_high / 2) s.mark_count[2] = (b_high % 2 ? bins.count[2] : bins.count[1]) - c_low;
+        if (threadIdx.x == 0) s.list_n = 0;
+        __syncthreads();
+        const uint32_t n_low = s.mark_count[2], n_end = b_end > b_high ? (uint32_t)(s.bins[b_end] >> a.count_shift) : 0;
+        if (b_low <= b_high && b_high <= b_end && n_low + n_end <= kList) {
+            each(row, n, [&](float l, int i) {
+                const uint32_t bin = w.bin_of(w.depth(l));
+                if ((bin >= b_low && bin <= b_high) || bin == b_end) s.list[atomicAdd(&s.list_n, 1u)] = (uint64_t)descending_key(l) << 32 | (uint32_t)i;
+            });
+            __syncthreads();
+            const uint32_t listed = s.list_n;
+            const uint64_t* list = sort_list(s, listed);
+            uint32_t count[3];
+            double mass[3];
+            sum_list(s, w, list, listed, c_low, m_low, count, mass);
+            // the elements of b_end, where it is not among the others, begin with what lies before that bin
+            const uint32_t first = 2 * threadIdx.x;
+            if (threadIdx.x == 0) s.mark_mass[0] = m_low, s.found_index = -1;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (first + i + 1 == n_low) s.mark_mass[0] = mass[i + 1];
+            __syncthreads();
+            const double moved = n_end ? m_end - s.mark_mass[0] : 0.0;
+            double before[2], after[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const bool in_end = first + i >= n_low;
+                before[i] = mass[i] + (in_end ? moved : 0.0), after[i] = mass[i + 1] + (in_end ? moved : 0.0);
+                count[i] = in_end ? c_end + first + i + 1 - n_low : c_low + first + i + 1;
+                if (first + i < listed && before[i] < need && (after[i] >= need || first + i + 1 == listed)) s.found_count = count[i], s.found_mass = after[i];
+            }
+            __syncthreads();
+            const uint32_t kept_count = s.found_count;
+            const double aim = (double)lim.u * (heavy < kept_count ? heavy_mass : s.found_mass);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (first + i < listed && before[i] <= aim && after[i] > aim && count[i] <= kept_count) s.found_index = (int)(uint32_t)list[first + i];
+            __syncthreads();
+            if (s.found_index >= 0) {
+                if (threadIdx.x == 0) a.tokens[r] = s.found_index;
+                return;
+            }
+            __syncthreads();
+        }
+    }
     // the end of the first top_k, of the mass that is kept of them, and the choice
     for (int stage = count_on ? 0 : mass_on ? 1 : 2; stage < 3; ++stage) {
         if (stage == 1 && !mass_on) continue;
