@@ -34,7 +34,7 @@ struct SampleArgs {
 };
 
 struct Shared {
-    uint64_t bins[kBins];
+    uint64_t bins[kBins + 64];         // the last ones take what is not allowed, a lane each
     uint64_t list[kList];              // descending_key << 32 | index: ascending is the order of the row
     uint64_t sorted[kRanked];
     double wave_mass[kWavesPerRow];
@@ -94,12 +94,44 @@ __device__ __forceinline__ void each(const T* row, int n, F&& f) {
     });
 }
 
+// f(logit, index) for every allowed token inside (hardly any: a vector without one costs its comparisons)
+template <typename T, typename Inside, typename F>
+__device__ __forceinline__ void each_where(const T* row, int n, Inside&& inside, F&& f) {
+    constexpr int kVec = 16 / sizeof(T);
+    each_vector(row, n, [&](const auto& x, int i, int elements) {
+        bool any = false;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) any |= inside(logit_of(x[e]));
+        if (any)
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) {
+                const float l = logit_of(x[e]);
+                if (inside(l) && l > -INFINITY && e < elements) f(l, i + e);
+            }
+    });
+}
+struct Range {
+    float least, most;
+    __device__ __forceinline__ bool operator()(float l) const { return l >= least && l <= most; }
+};
+
 struct Weights {
     float most, bins_per_logit, unit;      // bins_per_logit: above 0; unit: 2^R
     const double* power;
     // bins below the largest logit: never falls as the logit does (0 for the difference of two infinities)
     __device__ __forceinline__ float depth(float l) const { return fmaxf((most - l) * bins_per_logit, 0.0f); }
     __device__ __forceinline__ uint32_t bin_of(float depth) const { return (uint32_t)fminf(depth, kBins - 1.0f); }
+    // logits between which all elements of bins first to last lie (and few others): the depth is turned round with room for its roundings
+    __device__ __forceinline__ float below(uint32_t last) const {
+        if (last >= kBins - 1 || !(most < INFINITY)) return -INFINITY;
+        const float d = ((float)last + 1.01f) / bins_per_logit;
+        return most - d - (d * 0x1p-16f + fabsf(most) * 0x1p-20f);
+    }
+    __device__ __forceinline__ float above(uint32_t first) const {
+        if (!first || !(most < INFINITY)) return INFINITY;
+        const float d = ((float)first - 0.01f) / bins_per_logit;
+        return most - d + (d * 0x1p-16f + fabsf(most) * 0x1p-20f);
+    }
     __device__ __forceinline__ uint32_t units(float depth, uint32_t bin) const {
         return (uint32_t)fmaf(__builtin_amdgcn_exp2f(((float)bin - depth) * (1.0f / kBinsPerLog2)), unit, 0.5f);
     }
@@ -262,6 +294,7 @@ __device__ __forceinline__ Place find(Shared& s, const T* row, const SampleArgs&
     double before_mass = 0.0;
     uint32_t bin = find_bin<true>(s, sum_bins(s, w, a.count_shift, -1), t, before_count, before_mass);
     const uint32_t weight_bin = bin;
+    const Range range{w.below(bin), w.above(bin)};
     uint32_t low = 0, high = 0xFFFFFFFFu;
     const auto inside = [&](float l) {
         const uint32_t k = descending_key(l);
@@ -274,7 +307,7 @@ __device__ __forceinline__ Place find(Shared& s, const T* row, const SampleArgs&
         if (threadIdx.x == 0) s.key_low = 0xFFFFFFFFu, s.key_high = 0;
         clear_bins(s);
         uint32_t k_min = 0xFFFFFFFFu, k_max = 0;
-        each(row, n, [&](float l, int) {
+        each_where(row, n, range, [&](float l, int) {
             if (inside(l)) k_min = min(k_min, descending_key(l)), k_max = max(k_max, descending_key(l));
         });
         atomicMin(&s.key_low, k_min);
@@ -284,7 +317,7 @@ __device__ __forceinline__ Place find(Shared& s, const T* row, const SampleArgs&
         equal = span == 0;   // (key_low is theirs)
         if (equal) break;
         const int shift = span < kBins ? 0 : 21 - __builtin_clz(span);
-        each(row, n, [&](float l, int) {
+        each_where(row, n, range, [&](float l, int) {
             if (inside(l)) atomicAdd((unsigned long long*)&s.bins[(descending_key(l) - from) >> shift], 1ull << a.count_shift | w.units(w.depth(l), weight_bin));
         });
         __syncthreads();
@@ -322,7 +355,7 @@ __device__ __forceinline__ Place find(Shared& s, const T* row, const SampleArgs&
     }
     if (threadIdx.x == 0) s.list_n = 0;
     __syncthreads();
-    each(row, n, [&](float l, int i) {
+    each_where(row, n, range, [&](float l, int i) {
         if (inside(l)) s.list[atomicAdd(&s.list_n, 1u)] = (uint64_t)descending_key(l) << 32 | (uint32_t)i;   // (here of them)
     });
     __syncthreads();
@@ -476,10 +509,14 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
 
     const auto histogram = [&]() {
         clear_bins(s);
-        each(row, n, [&](float l, int) {
-            const float d = w.depth(l);
-            const uint32_t bin = w.bin_of(d);
-            atomicAdd((unsigned long long*)&s.bins[bin], 1ull << a.count_shift | w.units(d, bin));
+        // without branches: what is not allowed is counted where nobody looks
+        each_vector(row, n, [&](const auto& x, int, int elements) {
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) {
+                const float l = logit_of(x[e]), d = w.depth(l);
+                const uint32_t bin = w.bin_of(d), place = l > -INFINITY && e < elements ? bin : kBins + threadIdx.x % 64;
+                atomicAdd((unsigned long long*)&s.bins[place], 1ull << a.count_shift | w.units(d, bin));
+            }
         });
         __syncthreads();
     };
@@ -501,7 +538,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     if (threadIdx.x == 0) s.list_n = 0;
     __syncthreads();
     if (s.mark_count[1] <= kList) {
-        each(row, n, [&](float l, int i) {
+        each_where(row, n, Range{w.below(end), INFINITY}, [&](float l, int i) {
             if (w.bin_of(w.depth(l)) <= end) s.list[atomicAdd(&s.list_n, 1u)] = (uint64_t)descending_key(l) << 32 | (uint32_t)i;
         });
         __syncthreads();
@@ -552,7 +589,8 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
         __syncthreads();
         const uint32_t n_low = s.mark_count[2], n_end = b_end > b_high ? (uint32_t)(s.bins[b_end] >> a.count_shift) : 0;
         if (b_low <= b_high && b_high <= b_end && n_low + n_end <= kList) {
-            each(row, n, [&](float l, int i) {
+            const Range choice{w.below(b_high), w.above(b_low)}, border{w.below(b_end), w.above(b_end)};
+            each_where(row, n, [&](float l) { return choice(l) || border(l); }, [&](float l, int i) {
                 const uint32_t bin = w.bin_of(w.depth(l));
                 if ((bin >= b_low && bin <= b_high) || bin == b_end) s.list[atomicAdd(&s.list_n, 1u)] = (uint64_t)descending_key(l) << 32 | (uint32_t)i;
             });
