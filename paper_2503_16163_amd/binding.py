@@ -8,6 +8,8 @@ or a call fails, an exception is raised.
 """
 import ctypes as C
 import os
+import struct
+import threading
 
 from . import build as _build
 
@@ -109,7 +111,7 @@ def lib():
         L.specache_timing.argtypes = [vp, i32, vp, vp]
         L.specache_measure_hbm_read.argtypes = [C.c_int64, i32, C.POINTER(C.c_double)]
         L.specache_measure_link.argtypes = [C.c_int64, i32, C.POINTER(C.c_double), C.POINTER(C.c_double)]
-        view, i64 = C.POINTER(View), C.c_int64
+        view, i64 = vp, C.c_int64      # (addresses of View structures)
         L.specache_rotary_plan.argtypes = [C.POINTER(RotaryConfig), C.POINTER(Rotary)]
         L.specache_rotate.argtypes = [C.POINTER(Rotary), i32, i32, i32, i32, view, view, i32, view, view, view, view, vp, i32, vp]
         L.specache_window_scratch.argtypes = [C.POINTER(WindowConfig), C.POINTER(i64)]
@@ -203,36 +205,65 @@ def _refuse(what):
     raise SpeCacheError(EINVAL, what)
 
 
-_TYPES = {}
+_torch, _TYPES = None, {}
 
 
-def _type_of(t):
-    if not _TYPES:
+def _with_torch():
+    """Imports torch on the first call (the package itself needs none)."""
+    global _torch
+    if _torch is None:
         import torch
         _TYPES.update({torch.float16: FP16, torch.bfloat16: BF16, torch.float32: FP32})
-    return _TYPES.get(t.dtype, -1)
+        _torch = torch
+    return _torch
 
 
 def _here():
-    import torch
-    return torch.cuda.current_device()
+    return _with_torch().cuda.current_device()
 
 
-def _view(t, shape, dtype, device, name):
-    """The specache_view of a [batch, heads, tokens, 128] tensor on the current device, the channels side by side."""
-    if t.shape != shape or _type_of(t) != dtype or t.get_device() != device:
-        _refuse(f"{name} must be a {tuple(shape)} tensor of q's type on the current device")
-    b, h, n, c = t.stride()
-    if c != 1:
-        _refuse(f"{name}: the channels must lie side by side")
-    return View(t.data_ptr(), b if shape[0] > 1 else 0, h if shape[1] > 1 else 0, n if shape[2] > 1 else 0)   # (any stride goes with one)
+def _type_of(t):
+    _with_torch()
+    return _TYPES.get(t.dtype, -1)
+
+
+class _Views(threading.local):
+    """Room for the specache_views of one call (the call is over before the thread makes another)."""
+
+    def __init__(self):
+        self.room = (C.c_int64 * 24)()
+        at = C.addressof(self.room)
+        self.at = tuple(at + 32 * i for i in range(6))
+
+
+_room = _Views()
+_PACK = {n: struct.Struct(f"{4 * n}q").pack_into for n in (4, 6)}
+
+
+def _views(device, dtype, names, tensors, shapes):
+    """Addresses of the specache_views of [batch, heads, tokens, 128] tensors (or None) of the given type and shapes on the current device,
+    the channels side by side.  (Packed at once: a ctypes structure for each cost a call 6 of its 12 us.)"""
+    fields = []
+    for t, shape in zip(tensors, shapes):
+        if t is None:
+            fields += (0, 0, 0, 0)
+            continue
+        if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
+            _refuse(f"{names[len(fields) // 4]} must be a {tuple(shape)} tensor of q's type on the current device")
+        b, h, n, c = t.stride()
+        if c != 1:
+            _refuse(f"{names[len(fields) // 4]}: the channels must lie side by side")
+        # (any stride goes with a single one)
+        fields += (t.data_ptr(), b if shape[0] > 1 else 0, h if shape[1] > 1 else 0, n if shape[2] > 1 else 0)
+    _PACK[len(tensors)](_room.room, 0, *fields)
+    return _room.at
 
 
 def _flat(t, shape, kind, device, name):
     """Address of a contiguous tensor of the given shape and type on the current device, or None."""
     if t is None:
         return None
-    if t.shape != shape or str(t.dtype) != kind or t.get_device() != device or not t.is_contiguous():
+    if t.shape != shape or t.dtype is not kind or t.get_device() != device or not t.is_contiguous():
         _refuse(f"{name} must be a contiguous {tuple(shape)} tensor of {kind} on the current device")
     return t.data_ptr()
 
@@ -256,17 +287,20 @@ def rotary_plan(rotary_dim=128, base=10000.0, layout=ROTARY_HALF, scaling=ROTARY
 
 def rotate(plan, q, q_out, k=None, k_out=None, v=None, v_out=None, positions=None, first_position=0, stream=None):
     """q [B, Hq, n, 128] and k [B, Hkv, n, 128] turned by their positions, v as it is, each into its output, in one launch."""
-    B, Hq, n, _ = q.shape
-    Hkv = 0 if k is None and v is None else (v if k is None else k).shape[1]
-    dtype, device = _type_of(q), _here()
-    views = []
-    for name, t, out, heads in (("q", q, q_out, Hq), ("k", k, k_out, Hkv), ("v", v, v_out, Hkv)):
-        if (t is None) != (out is None):
-            _refuse(f"{name} and {name}_out are given or left out together")
-        for x in (t, out):
-            views.append(None if x is None else C.byref(_view(x, (B, heads, n, 128), dtype, device, name)))
-    _done(lib().specache_rotate(C.byref(plan), dtype, B, n, Hq, views[0], views[1], Hkv, *views[2:],
-                                _flat(positions, (B, n), "torch.int32", device, "positions"), first_position, _stream(stream)))
+    shape = q.shape
+    B, Hq, n, _ = shape
+    kv = v if k is None else k
+    kv_shape = None if kv is None else (B, kv.shape[1], n, 128)
+    if (k is None) != (k_out is None) or (v is None) != (v_out is None):
+        _refuse("a tensor and its output are given or left out together")
+    device = _here()
+    if shape[3] != 128:
+        _refuse("a head has 128 channels")
+    a = _views(device, q.dtype, ("q", "q_out", "k", "k_out", "v", "v_out"), (q, q_out, k, k_out, v, v_out),
+               (shape, shape, kv_shape, kv_shape, kv_shape, kv_shape))
+    _done(lib().specache_rotate(C.byref(plan), _type_of(q), B, n, Hq, a[0], a[1], 0 if kv is None else kv_shape[1],
+                                None if k is None else a[2], None if k is None else a[3], None if v is None else a[4], None if v is None else a[5],
+                                _flat(positions, (B, n), _torch.int32, device, "positions"), first_position, _stream(stream)))
 
 
 def window_scratch(batch, n_q_heads, n_kv_heads, q_tokens, kv_tokens, window=0, sinks=0):
@@ -279,23 +313,23 @@ def window_scratch(batch, n_q_heads, n_kv_heads, q_tokens, kv_tokens, window=0, 
 
 def window_attend(q, k, v, out, window=0, sinks=0, q_lengths=None, kv_lengths=None, sm_scale=0.0, scratch=None, stream=None):
     """Attention of q [B, Hq, n, 128] over k, v [B, Hkv, N, 128] with a sliding window and sinks, into out (q's shape)."""
-    B, Hq, n, _ = q.shape
-    Hkv, N = k.shape[1], k.shape[2]
-    dtype, device = _type_of(q), _here()
-    cfg = WindowConfig(B, Hq, Hkv, 128, n, N, window, sinks, dtype, sm_scale)
-    rows, pairs = (B, Hq, n, 128), (B, Hkv, N, 128)
+    rows, pairs = q.shape, k.shape
+    B, Hq, n, D = rows
+    device = _here()
+    if pairs[0] != B or D != 128 or pairs[3] != 128:
+        _refuse("q is [B, Hq, n, 128], k and v are [B, Hkv, N, 128]")
+    a = _views(device, q.dtype, ("q", "k", "v", "out"), (q, k, v, out), (rows, pairs, pairs, rows))
+    cfg = WindowConfig(B, Hq, pairs[1], D, n, pairs[2], window, sinks, _type_of(q), sm_scale)
     address, size = _scratch(scratch, device)
-    _done(lib().specache_window_attend(C.byref(cfg), C.byref(_view(q, rows, dtype, device, "q")), C.byref(_view(k, pairs, dtype, device, "k")),
-                                       C.byref(_view(v, pairs, dtype, device, "v")), C.byref(_view(out, rows, dtype, device, "out")),
-                                       _flat(q_lengths, (B,), "torch.int32", device, "q_lengths"),
-                                       _flat(kv_lengths, (B,), "torch.int32", device, "kv_lengths"), address, size, _stream(stream)))
+    _done(lib().specache_window_attend(C.byref(cfg), a[0], a[1], a[2], a[3], _flat(q_lengths, (B,), _torch.int32, device, "q_lengths"),
+                                       _flat(kv_lengths, (B,), _torch.int32, device, "kv_lengths"), address, size, _stream(stream)))
 
 
 def sample_scratch(rows, vocab, dtype):
     """Bytes of scratch memory that sample needs (0: none); dtype: the logits' torch type or FP16, BF16, FP32."""
     if not isinstance(dtype, int):
-        import torch
-        dtype = _type_of(torch.empty(0, dtype=dtype))
+        _with_torch()
+        dtype = _TYPES.get(dtype, -1)
     out = C.c_int64()
     _done(lib().specache_sample_scratch(C.byref(SampleConfig(rows, vocab, dtype, vocab)), C.byref(out)))
     return out.value
@@ -308,7 +342,7 @@ def sample(logits, u, tokens, temperature=None, top_k=None, top_p=None, min_p=No
     if logits.get_device() != device or (V > 1 and logits.stride(1) != 1):
         _refuse("logits must be on the current device, a row's side by side")
     cfg = SampleConfig(R, V, _type_of(logits), logits.stride(0) if R > 1 else V)
-    f32, i32, shape = "torch.float32", "torch.int32", (R,)
+    f32, i32, shape = _torch.float32, _torch.int32, (R,)
     address, size = _scratch(scratch, device)
     _done(lib().specache_sample(C.byref(cfg), logits.data_ptr(), _flat(u, shape, f32, device, "u"),
                                 _flat(temperature, shape, f32, device, "temperature"), _flat(top_k, shape, i32, device, "top_k"),

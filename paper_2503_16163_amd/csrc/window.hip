@@ -308,9 +308,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tile_kernel(WindowArgs a) {
     const Walk<TILE> walk(first, last, a.window, a.sinks);
     int i_begin = 0, i_end = walk.n;
     if constexpr (SPLIT) {
-        const int per = (walk.n + a.chunks - 1) / a.chunks;
-        i_begin = min(chunk * per, walk.n);
-        i_end = min(i_begin + per, walk.n);
+        i_begin = (int)((int64_t)walk.n * chunk / a.chunks);
+        i_end = (int)((int64_t)walk.n * (chunk + 1) / a.chunks);
     }
 
     Rows<BF16, TILE / 32> rs;
@@ -377,18 +376,23 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tile_kernel(WindowArgs a) {
         rs.store((uint16_t*)a.out.data + b * a.out.batch + q_head * a.out.head + token * a.out.token);
 }
 
-// A wave by itself: 32 positions at a time, the next ones on their way while it works on these; five of them on a compute unit (by LDS)
-// keep up to 160 KB in flight there.
-template <bool BF16, bool SPLIT>
-__global__ __launch_bounds__(64, 2) void step_kernel(WindowArgs a) {
-    constexpr int TILE = 32, FETCHES = 8;
-    __shared__ __align__(1024) char keys_even[TILE * kRowBytes16];
-    __shared__ __align__(1024) char keys_odd[TILE * kRowBytes16];
-    __shared__ __align__(1024) char values_even[TILE * kRowBytes16];
-    __shared__ __align__(1024) char values_odd[TILE * kRowBytes16];
+// Waves by themselves: 32 positions at a time, the next ones on their way while a wave works on these; the waves of a workgroup take a chunk's
+// tiles in turn and join their results in LDS at its end.  Memory is what bounds it, latency where a wave has few tiles (1.1 us each).  By
+// workgroups of 1, 2 and 4 waves, with one round of them, us (the time of reading once at 6.2 TB/s): 32 heads over 32768 positions 98, 100, 115
+// (87), 4 of 32 on 8 heads and two rows over 8192 33, 32, 32 (22), one sequence of 1 head over 100000 35, 28, 24 (8), 32 heads and two rows through a
+// window of 4096 22, 23, 23 (11); 16 ragged sequences of 8 heads up to 32768 265, 251, 262 (203), and 236 with workgroups dealt to the XCDs
+// as they come instead of a sequence's together.
+template <bool BF16, bool SPLIT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void step_kernel(WindowArgs a) {
+    constexpr int TILE = 32, FETCHES = 8, BYTES = TILE * kRowBytes16;
+    __shared__ __align__(1024) char keys_even[WAVES * BYTES];
+    __shared__ __align__(1024) char keys_odd[WAVES * BYTES];
+    __shared__ __align__(1024) char values_even[WAVES * BYTES];
+    __shared__ __align__(1024) char values_odd[WAVES * BYTES];
+    __shared__ float2 joined[WAVES][kWaveRows];
 
-    const int lane = threadIdx.x;
-    const int id = on_one_xcd(), chunk = SPLIT ? id % a.chunks : 0, item = SPLIT ? id / a.chunks : id;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int id = blockIdx.x, chunk = SPLIT ? id % a.chunks : 0, item = SPLIT ? id / a.chunks : id;
     const int b = item / a.n_kv_heads, h = item % a.n_kv_heads;
     const int n = length_of(a.q_lengths, b, a.q_tokens), N = length_of(a.kv_lengths, b, a.kv_tokens);
     const int rows = n * a.G;
@@ -399,101 +403,160 @@ __global__ __launch_bounds__(64, 2) void step_kernel(WindowArgs a) {
     const Walk<TILE> walk(first, last, a.window, a.sinks);
     int i_begin = 0, i_end = walk.n;
     if constexpr (SPLIT) {
-        const int per = (walk.n + a.chunks - 1) / a.chunks;
-        i_begin = min(chunk * per, walk.n);
-        i_end = min(i_begin + per, walk.n);
+        i_begin = (int)((int64_t)walk.n * chunk / a.chunks);
+        i_end = (int)((int64_t)walk.n * (chunk + 1) / a.chunks);
     }
+    const int i_first = i_begin + wave;
 
     Rows<BF16, 1> rs;
     rs.seen = Seen{N - n + token, a.window ? N - n + token - a.window + 1 : 0, a.sinks};
     const Fetch<true, FETCHES> fetch_keys(a.k, b, h, 0, lane);
     const Fetch<false, FETCHES> fetch_values(a.v, b, h, 0, lane);
     bool dropped = false;
-    if (i_begin < i_end) {
-        fetch_keys(walk.position(i_begin), TILE, N - 1, keys_even);
-        fetch_values(walk.position(i_begin), TILE, N - 1, values_even);
+    if (i_first < i_end) {
+        fetch_keys(walk.position(i_first), TILE, N - 1, keys_even + wave * BYTES);
+        fetch_values(walk.position(i_first), TILE, N - 1, values_even + wave * BYTES);
     }
     rs.start((const uint16_t*)a.q.data + b * a.q.batch + q_head * a.q.head + token * a.q.token, lane);
     const auto step = [&](int it, char* keys, char* values, char* next_keys, char* next_values) __attribute__((always_inline)) {
         const int tile0 = walk.position(it);
+        const bool more = it + WAVES < i_end;
         asm volatile("" ::: "memory");        // (the buffers' last reads are behind)
         __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
-        if (it + 1 < i_end) {
-            fetch_keys(walk.position(it + 1), TILE, N - 1, next_keys);
-            fetch_values(walk.position(it + 1), TILE, N - 1, next_values);
+        if (more) {
+            fetch_keys(walk.position(it + WAVES), TILE, N - 1, next_keys + wave * BYTES);
+            fetch_values(walk.position(it + WAVES), TILE, N - 1, next_values + wave * BYTES);
             __builtin_amdgcn_s_waitcnt(0x4F78);   // vmcnt(24): this tile's keys are there
         } else {
             __builtin_amdgcn_s_waitcnt(0x0F78);   // vmcnt(8)
         }
         asm volatile("" ::: "memory");
-        rs.scores(keys);
+        rs.scores(keys + wave * BYTES);
         const bool edge = is_edge<TILE>(tile0, first, last, a.window, a.sinks);
         if (edge) rs.mask(tile0);
         rs.move_maximum(a.scale);
         rs.weights(a.scale);
         asm volatile("" ::: "memory");
-        if (it + 1 < i_end) __builtin_amdgcn_s_waitcnt(0x4F70);   // vmcnt(16): and its values
+        if (more) __builtin_amdgcn_s_waitcnt(0x4F70);   // vmcnt(16): and its values
         else __builtin_amdgcn_s_waitcnt(0x0F70);
         asm volatile("" ::: "memory");
-        if (edge) dropped |= drop_odd_values<BF16, FETCHES>(values, 0, lane);
-        rs.add_values(values);
+        if (edge) dropped |= drop_odd_values<BF16, FETCHES>(values + wave * BYTES, 0, lane);
+        rs.add_values(values + wave * BYTES);
     };
-    for (int it = i_begin; it < i_end; it += 2) {
+    for (int it = i_first; it < i_end; it += 2 * WAVES) {
         step(it, keys_even, values_even, keys_odd, values_odd);
-        if (it + 1 < i_end) step(it + 1, keys_odd, values_odd, keys_even, values_even);
+        if (it + WAVES < i_end) step(it + WAVES, keys_odd, values_odd, keys_even, values_even);
     }
     if (__ballot(dropped))
-        for (int it = i_begin; it < i_end; ++it) {
+        for (int it = i_first; it < i_end; it += WAVES) {
             const int tile0 = walk.position(it);
             if (is_edge<TILE>(tile0, first, last, a.window, a.sinks)) rs.give_odd_values(fetch_values.base, a.v.token, tile0, min(tile0 + TILE, N));
         }
     rs.l += other_half(rs.l);
-    if (row >= rows) return;
-    if constexpr (SPLIT) rs.store_part(a.part_o, a.part_ml, ((int64_t)item * a.chunks + chunk) * a.item_rows + row, i_begin < i_end);
-    else rs.store((uint16_t*)a.out.data + b * a.out.batch + q_head * a.out.head + token * a.out.token);
+
+    // every wave's sums to LDS (a row's channels turned by 4 per row: no two rows of a group of lanes meet in a bank), then four channels per thread
+    __syncthreads();
+    char* const room = wave == 0 ? keys_even : wave == 1 ? keys_odd : wave == 2 ? values_even : values_odd;
+    if (row < rows) {
+        if (lane < 32) joined[wave][row] = float2{rs.m, rs.l};
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *(float4*)(room + (row * kD + (32 * dt + 8 * i + 4 * rs.half + 4 * row) % kD) * 4) =
+                    float4{rs.o[dt][4 * i], rs.o[dt][4 * i + 1], rs.o[dt][4 * i + 2], rs.o[dt][4 * i + 3]};
+    }
+    __syncthreads();
+    for (int at = threadIdx.x; at < rows * (kD / 4); at += 64 * WAVES) {
+        const int row = at / (kD / 4), c = at % (kD / 4) * 4;
+        float m = kNever, l = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) m = fmaxf(m, joined[w][row].x);
+        float4 o{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float2 ml = joined[w][row];
+            const float f = __builtin_amdgcn_exp2f(ml.x - m);
+            const char* from = w == 0 ? keys_even : w == 1 ? keys_odd : w == 2 ? values_even : values_odd;
+            const float4 x = *(const float4*)(from + (row * kD + (c + 4 * row) % kD) * 4);
+            l = fmaf(f, ml.y, l);
+            o.x = fmaf(f, x.x, o.x), o.y = fmaf(f, x.y, o.y), o.z = fmaf(f, x.z, o.z), o.w = fmaf(f, x.w, o.w);
+        }
+        if constexpr (SPLIT) {
+            const int64_t place = ((int64_t)item * a.chunks + chunk) * a.item_rows + row;
+            if (c == 0) *(float2*)(a.part_ml + 2 * place) = float2{m, l};
+            *(float4*)(a.part_o + place * kD + c) = o;
+        } else {
+            const float by = l == 0.0f ? 0.0f : 1.0f / l;
+            uint16_t* to = (uint16_t*)a.out.data + b * a.out.batch + (h * a.G + row % a.G) * a.out.head + row / a.G * a.out.token;
+            *(uint2v*)(to + c) = uint2v{pack16<BF16>(o.x * by, o.y * by), pack16<BF16>(o.z * by, o.w * by)};
+        }
+    }
 }
 
-// The chunks of a row, joined: two channels per lane, the chunks dealt to the waves of a workgroup.
+// The chunks of a row, joined: two channels per lane, the chunks dealt to the waves of a workgroup.  What it takes is latency, so every load of a
+// wave's first chunks is asked for at once, and each wave goes by its own chunks' maximum (4.9 us of a step of one short sequence
+// with the loads behind the row's maximum, 4.5 so).
 constexpr int kMergeWaves = 4;
 template <bool BF16>
 __global__ __launch_bounds__(64 * kMergeWaves) void merge_kernel(WindowArgs a) {
-    __shared__ float part[kMergeWaves][kD + 2];
+    __shared__ float part[kMergeWaves][kD];
+    __shared__ float2 joined[kMergeWaves];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int row = blockIdx.x % a.item_rows, item = blockIdx.x / a.item_rows;
     const int b = item / a.row_tiles / a.n_kv_heads, h = item / a.row_tiles % a.n_kv_heads;
     const int r = (a.row_tiles - 1 - item % a.row_tiles) * a.item_rows + row;
-    if (r >= length_of(a.q_lengths, b, a.q_tokens) * a.G) return;
+    const int n = length_of(a.q_lengths, b, a.q_tokens);
     const int64_t place = (int64_t)item * a.chunks * a.item_rows + row;
     const float2* ml = (const float2*)a.part_ml + place;
     const float* po = a.part_o + place * kD + 2 * lane;
-    // every lane a chunk: the largest maximum, which all waves work out alike
-    float m = kNever;
-    for (int c = lane; c < a.chunks; c += 64) m = fmaxf(m, ml[(int64_t)c * a.item_rows].x);
-    for (int d = 32; d; d /= 2) m = fmaxf(m, __shfl_xor(m, d));
-    float l = 0.0f, x = 0.0f, y = 0.0f;
-#pragma unroll 4
-    for (int c = wave; c < a.chunks; c += kMergeWaves) {
-        const float2 one = ml[(int64_t)c * a.item_rows];
-        if (one.y == 0.0f) continue;   // (nothing was stored)
-        const float w = __builtin_amdgcn_exp2f(one.x - m);
-        const float2 oc = *(const float2*)(po + (int64_t)c * a.item_rows * kD);
-        l = fmaf(w, one.y, l);
-        x = fmaf(w, oc.x, x);
-        y = fmaf(w, oc.y, y);
+    float m = kNever, l = 0.0f, x = 0.0f, y = 0.0f;
+    constexpr int kAhead = 8;
+    for (int c0 = wave; c0 < a.chunks; c0 += kAhead * kMergeWaves) {
+        float2 one[kAhead], oc[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int64_t at = (int64_t)min(c0 + i * kMergeWaves, a.chunks - 1) * a.item_rows;
+            one[i] = ml[at];
+            oc[i] = *(const float2*)(po + at * kD);
+        }
+        if (r >= n * a.G) return;      // (no row: nothing was stored, and nothing is asked of what was loaded)
+        float most = m;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) most = fmaxf(most, one[i].x);
+        const float moved = __builtin_amdgcn_exp2f(m - most);
+        l *= moved, x *= moved, y *= moved;
+        m = most;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (c0 + i * kMergeWaves >= a.chunks || one[i].y == 0.0f) continue;   // (an empty chunk stored no sums)
+            const float w = __builtin_amdgcn_exp2f(one[i].x - m);
+            l = fmaf(w, one[i].y, l);
+            x = fmaf(w, oc[i].x, x);
+            y = fmaf(w, oc[i].y, y);
+        }
     }
-    part[wave][2 * lane] = x;
-    part[wave][2 * lane + 1] = y;
-    if (lane == 0) part[wave][kD] = l;
+    *(float2*)&part[wave][2 * lane] = float2{x, y};
+    if (lane == 0) joined[wave] = float2{m, l};
     __syncthreads();
-    if (wave) return;
+    if (wave || r >= n * a.G) return;
+#pragma unroll
+    for (int w = 0; w < kMergeWaves; ++w) m = fmaxf(m, joined[w].x);
     l = x = y = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kMergeWaves; ++w) l += part[w][kD], x += part[w][2 * lane], y += part[w][2 * lane + 1];
+    for (int w = 0; w < kMergeWaves; ++w) {
+        const float f = __builtin_amdgcn_exp2f(joined[w].x - m);
+        const float2 o = *(const float2*)&part[w][2 * lane];
+        l = fmaf(f, joined[w].y, l);
+        x = fmaf(f, o.x, x);
+        y = fmaf(f, o.y, y);
+    }
     const float by = l == 0.0f ? 0.0f : 1.0f / l;
     uint16_t* to = (uint16_t*)a.out.data + b * a.out.batch + (h * a.G + r % a.G) * a.out.head + r / a.G * a.out.token;
     *(uint32_t*)(to + 2 * lane) = pack16<BF16>(x * by, y * by);
 }
 
+constexpr int kStepWaves = 2;
 enum { kStep, kTile4, kTile8 };
 struct Plan {
     int kernel = kStep, row_tiles = 1, item_rows = 0, chunks = 1;
@@ -514,6 +577,15 @@ int check(const specache_window_config* c) {
     return SPECACHE_OK;
 }
 
+// Steps: one round of workgroups (two on a compute unit by their LDS), chunks of at most 64 tiles (2048 positions) so that a ragged batch's lengths
+// even out, a tile for every wave at least, and no more than 256 chunks of a row to merge unless they are that long.  us, by chunks: one sequence of 8
+// KV heads, 131072 positions, 64 chunks 98, 80 chunks (a second round) 116, 128 101; 16 ragged sequences of 8 heads up to 32768 positions, chunks of 64 tiles 236, of 128
+// 261; 1 head, 100000 positions, 128 chunks 28, 256 26, 512 33.  Up to 4 tiles per wave no chunks at all, as a merge is a launch more: 256
+// positions 7.8 us against 9.0 with them, 512 positions 12.0 against 9.5.
+// Prompts: 8 waves to a workgroup where a row tile walks 2048 positions or more (8 waves / 4: a prompt of 16k tokens 2148 / 2225 us, through a
+// window of 4096 1974 / 2014, but ragged ones of up to 3001 tokens through 512 189 / 172: its first tiles and edges are then most of a walk);
+// row tiles that are too few for the chip have their positions split, at least four tiles to a chunk.
+constexpr int64_t kStepsAtOnce = 512;
 int plan_of(const specache_window_config& c, Plan& p) {
     const int G = c.n_q_heads / c.n_kv_heads;
     const int64_t rows = (int64_t)c.q_tokens * G;
@@ -526,10 +598,12 @@ int plan_of(const specache_window_config& c, Plan& p) {
         p.item_rows = (int)rows;
         p.items = heads * (rows > 0);
         const int64_t tiles = (most + 31) / 32;
-        const int64_t at_once = 256 * 5;            // waves that the chip holds
-        if (p.items) chunks = std::min(std::max(at_once / p.items, tiles / 32), tiles / 2);
+        if (p.items && tiles > 4 * kStepWaves) {
+            chunks = std::max(kStepsAtOnce / p.items, tiles / 64);
+            chunks = std::min({chunks, tiles / kStepWaves, std::max<int64_t>(256, tiles / 64)});
+        }
     } else {
-        p.kernel = most >= 2048 ? kTile8 : kTile4;
+        p.kernel = most >= 2048 && rows > 128 ? kTile8 : kTile4;
         p.item_rows = p.kernel == kTile8 ? 256 : 128;
         p.row_tiles = (int)((rows + p.item_rows - 1) / p.item_rows);
         p.items = heads * p.row_tiles;
@@ -545,7 +619,7 @@ template <bool BF16>
 void launch(const Plan& p, const WindowArgs& a, hipStream_t stream) {
     const dim3 grid((unsigned)(p.items * p.chunks));
     const bool split = p.chunks > 1;
-    if (p.kernel == kStep) hipLaunchKernelGGL((split ? step_kernel<BF16, true> : step_kernel<BF16, false>), grid, dim3(64), 0, stream, a);
+    if (p.kernel == kStep) hipLaunchKernelGGL((split ? step_kernel<BF16, true, kStepWaves> : step_kernel<BF16, false, kStepWaves>), grid, dim3(64 * kStepWaves), 0, stream, a);
     else if (p.kernel == kTile4) hipLaunchKernelGGL((split ? tile_kernel<BF16, true, 4> : tile_kernel<BF16, false, 4>), grid, dim3(256), 0, stream, a);
     else hipLaunchKernelGGL((split ? tile_kernel<BF16, true, 8> : tile_kernel<BF16, false, 8>), grid, dim3(512), 0, stream, a);
     if (split) hipLaunchKernelGGL(merge_kernel<BF16>, dim3((unsigned)(p.items * p.item_rows)), dim3(64 * kMergeWaves), 0, stream, a);

@@ -137,6 +137,7 @@ def test_sample_refuses():
 
 def test_bindings_refuse_tensors_that_are_not_on_the_device(monkeypatch):
     import torch
+    binding._with_torch()
     monkeypatch.setattr(binding, "_here", lambda: 0)
     x = torch.zeros((1, 2, 3, 128), dtype=torch.float16)
     for call in (lambda: binding.rotate(binding.rotary_plan(), x, x), lambda: binding.window_attend(x, x, x, x),
