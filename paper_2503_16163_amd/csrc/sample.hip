@@ -6,10 +6,12 @@
 //   - Few tokens kept: those that can be are listed in LDS, sorted there, and their weights summed in order.  With top_k the list is what
 //     is not below the k-th largest of the threads' own maxima (there are k such elements at least, and hardly more); without it, what
 //     a histogram over the logarithm of the weights puts in or before the bin where the kept mass ends.
-//   - Many: the histogram's bin that holds a target is taken apart further, by the bits of its logits, until its elements fit in the list.
+//   - Many: the elements of the histogram's bins that hold the targets are listed; a bin that holds too many is taken apart further, by the bits
+//     of its logits.
 // An element's weight is r 2^(-bin / 64): the power of the bin, of which there are 64 per power of two, and a whole number r of units 2^-R,
 // so that a bin's sum is exact in whatever order it is made; sums of bins and of listed elements are binary64 in a fixed order.
 #include "operators.h"
+#include "wave_ops.h"
 
 #include <cmath>
 
@@ -20,7 +22,9 @@ constexpr int kThreads = 1024, kWavesPerRow = kThreads / 64;
 constexpr int kBins = 2048;            // two per thread
 constexpr float kBinsPerLog2 = 64.0f;  // 32 powers of two of the weights; what is lighter shares the last bin
 constexpr int kList = 2048;            // elements that are sorted at once
-constexpr int kRanked = 256;           // of these few each is compared with all the others instead
+constexpr int kFew = 256;              // a list so short is sorted by comparing each with all the others,
+constexpr int kRanked = 1024;          // of a bin's so many each is compared with all the others
+constexpr int kTable = 32768;          // vectors of a row whose largest logits are kept (32 of each thread)
 constexpr int kMostVocab = 1 << 20;
 
 struct SampleArgs {
@@ -36,7 +40,7 @@ struct SampleArgs {
 struct Shared {
     uint64_t bins[kBins + 64];         // the last ones take what is not allowed, a lane each
     uint64_t list[kList];              // descending_key << 32 | index: ascending is the order of the row
-    uint64_t sorted[kRanked];
+    uint64_t sorted[kList];
     double wave_mass[kWavesPerRow];
     uint32_t wave_count[kWavesPerRow];
     float wave_most[kWavesPerRow];
@@ -48,11 +52,14 @@ struct Shared {
     uint32_t mark_count[3];
     uint64_t border_units;
     double power[64];                  // 2^(-i / 64) / 2^R
+    uint16_t vector_most[kTable];      // of a thread's own vectors: the largest logit's key, its upper half rounded up
+    uint32_t places[kBins];            // sort_list: elements of a bin, then the place of its first
+    uint32_t crowded;
 };
 
 template <typename T> __device__ __forceinline__ float logit_of(T x) { return (float)x; }
 
-// f(vector, first index, elements) over a row: 16-byte loads between the first and the last aligned address, four ahead, single elements
+// f(vector, first index, elements, number of the vector or -1) over a row: 16-byte loads between the first and the last aligned address, four ahead, single elements
 // before and behind.  A thread's calls come in ascending order of the index.
 template <typename T, typename F>
 __device__ __forceinline__ void each_vector(const T* row, int n, F&& f) {
@@ -63,7 +70,7 @@ __device__ __forceinline__ void each_vector(const T* row, int n, F&& f) {
     if ((int)threadIdx.x < head) {
         Vec x{};
         x[0] = row[threadIdx.x];
-        f(x, (int)threadIdx.x, 1);
+        f(x, (int)threadIdx.x, 1, -1);
     }
     const Vec* body = (const Vec*)(row + head);
     int v = threadIdx.x;
@@ -72,20 +79,20 @@ __device__ __forceinline__ void each_vector(const T* row, int n, F&& f) {
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) x[i] = body[v + i * kThreads];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) f(x[i], head + (v + i * kThreads) * kVec, kVec);
+        for (int i = 0; i < kAhead; ++i) f(x[i], head + (v + i * kThreads) * kVec, kVec, v + i * kThreads);
     }
-    for (; v < vecs; v += kThreads) f(body[v], head + v * kVec, kVec);
+    for (; v < vecs; v += kThreads) f(body[v], head + v * kVec, kVec, v);
     if (tail + (int)threadIdx.x < n) {
         Vec x{};
         x[0] = row[tail + threadIdx.x];
-        f(x, tail + (int)threadIdx.x, 1);
+        f(x, tail + (int)threadIdx.x, 1, -1);
     }
 }
 // f(logit, index) for every allowed token
 template <typename T, typename F>
 __device__ __forceinline__ void each(const T* row, int n, F&& f) {
     constexpr int kVec = 16 / sizeof(T);
-    each_vector(row, n, [&](const auto& x, int i, int elements) {
+    each_vector(row, n, [&](const auto& x, int i, int elements, int) {
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
             const float l = logit_of(x[e]);
@@ -98,7 +105,7 @@ __device__ __forceinline__ void each(const T* row, int n, F&& f) {
 template <typename T, typename Inside, typename F>
 __device__ __forceinline__ void each_where(const T* row, int n, Inside&& inside, F&& f) {
     constexpr int kVec = 16 / sizeof(T);
-    each_vector(row, n, [&](const auto& x, int i, int elements) {
+    each_vector(row, n, [&](const auto& x, int i, int elements, int) {
         bool any = false;
 #pragma unroll
         for (int e = 0; e < kVec; ++e) any |= inside(logit_of(x[e]));
@@ -109,6 +116,33 @@ __device__ __forceinline__ void each_where(const T* row, int n, Inside&& inside,
                 if (inside(l) && l > -INFINITY && e < elements) f(l, i + e);
             }
     });
+}
+// The same for the tokens that are not below `least`; vectors that hold none are not read again where the row's table says so.
+template <typename T, typename F>
+__device__ __forceinline__ void each_from(const Shared& s, const T* row, int n, float least, F&& f) {
+    constexpr int kVec = 16 / sizeof(T);
+    typedef T Vec __attribute__((ext_vector_type(kVec)));
+    const int head = min(n, (int)((16 - (uintptr_t)row % 16) % 16 / sizeof(T)));
+    const int vecs = (n - head) / kVec, tail = head + vecs * kVec;
+    if (vecs > kTable) {
+        each_where(row, n, [&](float l) { return l >= least; }, f);
+        return;
+    }
+    const auto one = [&](T x, int i) {
+        const float l = logit_of(x);
+        if (l >= least && l > -INFINITY) f(l, i);
+    };
+    if ((int)threadIdx.x < head) one(row[threadIdx.x], threadIdx.x);
+    if (tail + (int)threadIdx.x < n) one(row[tail + threadIdx.x], tail + threadIdx.x);
+    const uint32_t from = float_to_key(least) >> 16;
+    uint32_t wanted = 0;
+    for (int v = threadIdx.x, i = 0; v < vecs; v += kThreads, ++i) wanted |= (uint32_t)(s.vector_most[v] >= from) << i;
+    for (; wanted; wanted &= wanted - 1) {
+        const int v = threadIdx.x + __builtin_ctz(wanted) * kThreads;
+        const Vec x = ((const Vec*)(row + head))[v];
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) one(x[e], head + v * kVec + e);
+    }
 }
 struct Range {
     float least, most;
@@ -242,29 +276,80 @@ __device__ __forceinline__ void clear_bins(Shared& s) {
     __syncthreads();
 }
 
-// The listed elements (n of them, at most kList), sorted.
-__device__ __forceinline__ const uint64_t* sort_list(Shared& s, uint32_t n) {
-    if (n <= kRanked) {
+// One more listed element; what does not fit is counted.
+__device__ __forceinline__ void list_one(Shared& s, float l, int i) {
+    const uint32_t at = atomicAdd(&s.list_n, 1u);
+    if (at < kList) s.list[at] = (uint64_t)descending_key(l) << 32 | (uint32_t)i;
+}
+
+// The listed elements (n of them, at most kList), sorted: few are compared with each other, more put to their bins' places and there compared
+// with their bin's others; where a bin holds very many, by exchanges (66 steps for 2048).  us, a row of 32000 by exchanges / so: top_k 1000 33 / 25, top_p 0.9 29 /
+// 22; 50 by their bins' places 11.9, compared with each other 11.
+__device__ __forceinline__ const uint64_t* sort_list(Shared& s, const Weights& w, uint32_t n) {
+    if (n <= kFew) {
         if (threadIdx.x < n) {
             const uint64_t x = s.list[threadIdx.x];
             uint32_t rank = 0;
+#pragma unroll 8
             for (uint32_t j = 0; j < n; ++j) rank += s.list[j] < x;
             s.sorted[rank] = x;
         }
         __syncthreads();
         return s.sorted;
     }
-    uint32_t all = 2 * kRanked;
+    const uint32_t first = 2 * threadIdx.x;
+    s.places[first] = s.places[first + 1] = 0;
+    if (threadIdx.x == 0) s.crowded = 0;
+    __syncthreads();
+    uint64_t x[2];
+    uint32_t bin[2], place[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t at = threadIdx.x + i * kThreads;
+        if (at < n) {
+            x[i] = s.list[at];
+            bin[i] = w.bin_of(w.depth(logit_of_key((uint32_t)(x[i] >> 32))));
+            place[i] = atomicAdd(&s.places[bin[i]], 1u);
+        }
+    }
+    __syncthreads();
+    const uint32_t c0 = s.places[first], c1 = s.places[first + 1];
+    if (c0 > kRanked || c1 > kRanked) s.crowded = 1;
+    uint32_t before = c0 + c1;
+    double unused = 0.0;
+    sums_before(s, before, unused);
+    s.places[first] = before, s.places[first + 1] = before + c0;
+    __syncthreads();
+    if (!s.crowded) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (threadIdx.x + i * kThreads < n) s.sorted[s.places[bin[i]] + place[i]] = x[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (threadIdx.x + i * kThreads < n) {
+                const uint32_t from = s.places[bin[i]], to = bin[i] + 1 < kBins ? s.places[bin[i] + 1] : n;
+                uint32_t rank = from;
+#pragma unroll 8
+                for (uint32_t j = from; j < to; ++j) rank += s.sorted[j] < x[i];
+                s.list[rank] = x[i];
+            }
+        __syncthreads();
+        return s.list;
+    }
+    uint32_t all = 2;
     while (all < n) all *= 2;
     for (uint32_t i = n + threadIdx.x; i < all; i += kThreads) s.list[i] = ~0ull;
     for (uint32_t size = 2; size <= all; size *= 2)
         for (uint32_t apart = size / 2; apart; apart /= 2) {
-            __syncthreads();
+            // (a wave's 128 elements are its own until two threads of different waves meet)
+            if (apart >= 128 || (apart == 64 && size >= 256) || size == 2) __syncthreads();
+            else wave_sync();
             const uint32_t t = threadIdx.x;
             if (t < all / 2) {
                 const uint32_t i = 2 * apart * (t / apart) + t % apart, j = i + apart;
-                const uint64_t x = s.list[i], y = s.list[j];
-                if ((x > y) == !(i & size)) s.list[i] = y, s.list[j] = x;
+                const uint64_t p = s.list[i], q = s.list[j];
+                if ((p > q) == !(i & size)) s.list[i] = q, s.list[j] = p;
             }
         }
     __syncthreads();
@@ -356,11 +441,11 @@ __device__ __forceinline__ Place find(Shared& s, const T* row, const SampleArgs&
     if (threadIdx.x == 0) s.list_n = 0;
     __syncthreads();
     each_where(row, n, range, [&](float l, int i) {
-        if (inside(l)) s.list[atomicAdd(&s.list_n, 1u)] = (uint64_t)descending_key(l) << 32 | (uint32_t)i;   // (here of them)
+        if (inside(l)) list_one(s, l, i);   // (here of them)
     });
     __syncthreads();
     const uint32_t have = s.list_n;
-    const uint64_t* list = sort_list(s, have);
+    const uint64_t* list = sort_list(s, w, have);
     uint32_t count[3];
     double mass[3];
     sum_list(s, w, list, have, before_count, before_mass, count, mass);
@@ -423,7 +508,12 @@ __device__ __forceinline__ int choose(Shared& s, const Weights& w, const uint64_
     return (int)(uint32_t)list[s.mark_count[2]];
 }
 
-// A workgroup per row.  @SAMPLE@
+// A workgroup per row: it reads the row once for its largest logits (256 rows of 128256 in bfloat16, 66 MB: greedy choices take 14 us, where the bytes need
+// 11), and again what it cannot leave out.  The same rows with top_k 50 22 us (of the second reading only the vectors whose largest logit
+// counts; 28 with all of it), 1000 51, without a limit 56, top_p 0.9 59: the histogram of a whole row, 20 us of vector instructions and LDS
+// additions on its compute unit, and a third reading.  Two rows of 32000: 4.8, 11.5, 25, 20, 22 us, a chain of some 20 barriers and as many
+// exchanges.  A row to a workgroup, not to several: with as many rows as compute units nothing is gained, and few rows would pay a launch
+// (3 us) for each reading.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     __shared__ Shared s;
@@ -434,11 +524,15 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     // the largest logit; a thread keeps where its own largest one is first
     float own_most = -INFINITY;
     int own_at = 0;
-    each_vector(row, n, [&](const auto& x, int i, int elements) {
+    each_vector(row, n, [&](const auto& x, int i, int elements, int v) {
         float most = logit_of(x[0]);
 #pragma unroll
         for (int e = 1; e < kVec; ++e) most = fmaxf(most, e < elements ? logit_of(x[e]) : -INFINITY);
         if (most > own_most) own_most = most, own_at = i;
+        if (v >= 0 && v < kTable) {
+            const uint32_t key = float_to_key(most);
+            s.vector_most[v] = (uint16_t)min((key >> 16) + (key % 65536 != 0), 0xFFFFu);
+        }
     });
     float most = own_most;
     for (int d = 32; d; d /= 2) most = fmaxf(most, __shfl_xor(most, d));
@@ -470,38 +564,35 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     lim.depth = min_p > 0.0f ? fmaxf(-kBinsPerLog2 * log2f(min_p), 0.0f) : -1.0f;
     lim.u = fminf(fmaxf(a.u[r], 0.0f), 0x1.fffffep-1f);
 
-    if (lim.count <= kThreads * 3 / 4) {
-        // the bin of the count-th largest of the threads' own largest, the least of those up to there, and what is not below it
+    if (lim.count <= kThreads) {
+        // the bin of the count-th largest of the threads' own largest; the least of those up to there
         clear_bins(s);
         const uint32_t own_bin = w.bin_of(w.depth(own_most));
         if (own_most > -INFINITY) atomicAdd((unsigned long long*)&s.bins[own_bin], 1ull << a.count_shift);
         __syncthreads();
         uint32_t before_count = 0;
         double before_mass = 0.0;
-        const uint32_t bin = find_bin<false>(s, sum_bins<false>(s, w, a.count_shift, -1), Target{true, false, lim.count, 0.0}, before_count, before_mass);
+        const Target last{true, false, lim.count, 0.0};
+        const uint32_t bin = find_bin<false>(s, sum_bins<false>(s, w, a.count_shift, -1), last, before_count, before_mass);
         if (own_most > -INFINITY && own_bin <= bin) atomicMax(&s.key_high, descending_key(own_most));
         __syncthreads();
         const float least = bin == kBins ? -INFINITY : logit_of_key(s.key_high);
-        each_vector(row, n, [&](const auto& x, int i, int elements) {
-            float l[kVec];
-            bool any = false;
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) {
-                l[e] = e < elements ? logit_of(x[e]) : -INFINITY;
-                any |= l[e] >= least;
-            }
-            if (any)
-#pragma unroll
-                for (int e = 0; e < kVec; ++e)
-                    if (l[e] >= least && l[e] > -INFINITY) {
-                        const uint32_t at = atomicAdd(&s.list_n, 1u);
-                        if (at < kList) s.list[at] = (uint64_t)descending_key(l[e]) << 32 | (uint32_t)(i + e);
-                    }
+        uint32_t end = kBins;
+        if (lim.count > kThreads * 3 / 4) {
+            // many more than count are not below that: their histogram first
+            clear_bins(s);
+            each_from(s, row, n, least, [&](float l, int) { atomicAdd((unsigned long long*)&s.bins[w.bin_of(w.depth(l))], 1ull << a.count_shift); });
+            __syncthreads();
+            before_count = 0;
+            end = find_bin<false>(s, sum_bins<false>(s, w, a.count_shift, -1), last, before_count, before_mass);
+        }
+        each_from(s, row, n, least, [&](float l, int i) {
+            if (w.bin_of(w.depth(l)) <= end) list_one(s, l, i);
         });
         __syncthreads();
         const uint32_t listed = s.list_n;
         if (listed <= kList) {
-            const int token = choose(s, w, sort_list(s, listed), listed, lim, -1.0);
+            const int token = choose(s, w, sort_list(s, w, listed), listed, lim, -1.0);
             if (threadIdx.x == 0) a.tokens[r] = token;
             return;
         }
@@ -510,7 +601,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     const auto histogram = [&]() {
         clear_bins(s);
         // without branches: what is not allowed is counted where nobody looks
-        each_vector(row, n, [&](const auto& x, int, int elements) {
+        each_vector(row, n, [&](const auto& x, int, int elements, int) {
 #pragma unroll
             for (int e = 0; e < kVec; ++e) {
                 const float l = logit_of(x[e]), d = w.depth(l);
@@ -538,12 +629,12 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     if (threadIdx.x == 0) s.list_n = 0;
     __syncthreads();
     if (s.mark_count[1] <= kList) {
-        each_where(row, n, Range{w.below(end), INFINITY}, [&](float l, int i) {
-            if (w.bin_of(w.depth(l)) <= end) s.list[atomicAdd(&s.list_n, 1u)] = (uint64_t)descending_key(l) << 32 | (uint32_t)i;
+        each_from(s, row, n, w.below(end), [&](float l, int i) {
+            if (w.bin_of(w.depth(l)) <= end) list_one(s, l, i);
         });
         __syncthreads();
         const uint32_t listed = s.list_n;
-        const int token = choose(s, w, sort_list(s, listed), listed, lim, count_on ? -1.0 : all_mass);
+        const int token = choose(s, w, sort_list(s, w, listed), listed, lim, count_on ? -1.0 : all_mass);
         if (threadIdx.x == 0) a.tokens[r] = token;
         return;
     }
@@ -592,11 +683,11 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
             const Range choice{w.below(b_high), w.above(b_low)}, border{w.below(b_end), w.above(b_end)};
             each_where(row, n, [&](float l) { return choice(l) || border(l); }, [&](float l, int i) {
                 const uint32_t bin = w.bin_of(w.depth(l));
-                if ((bin >= b_low && bin <= b_high) || bin == b_end) s.list[atomicAdd(&s.list_n, 1u)] = (uint64_t)descending_key(l) << 32 | (uint32_t)i;
+                if ((bin >= b_low && bin <= b_high) || bin == b_end) list_one(s, l, i);
             });
             __syncthreads();
             const uint32_t listed = s.list_n;
-            const uint64_t* list = sort_list(s, listed);
+            const uint64_t* list = sort_list(s, w, listed);
             uint32_t count[3];
             double mass[3];
             sum_list(s, w, list, listed, c_low, m_low, count, mass);
