@@ -47,8 +47,9 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
 // angles once for all of them.  Memory is what bounds it.  The tile weighs reads, in which a token's heads lie side by side, against writes, in
 // which a head's tokens do: rotating 32k tokens of 32 + 8 heads and copying 8 (805 MB, 163 us at the rate of a large copy) takes 193 us with 1
 // token, 178 with 2, 172 with 4, 173 with 8, 178 with 16, 184 with 32.
-// STREAM: stores that leave the caches to others, for outputs that would not stay in them: the same 172 -> 164 us, 3 x 5003 tokens
-// 96 -> 61 (the input then stays in the memory-side cache).
+// STREAM: stores that leave the caches to others, for outputs that would not stay in them (the same 172 -> 164 us), where every access of a row's 8 lanes is a
+// line's 128 bytes; halves of less than the whole head, whose lines two accesses share, are written through the caches instead
+// (16k tokens of 32 + 32 heads, 32 of 128 channels turned, 197 us; past them 249).
 template <bool BF16, bool HALF, bool STREAM>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a) {
     const int part = threadIdx.x % kParts, slot = threadIdx.x / kParts;
@@ -57,16 +58,18 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a) {
     const int d = a.plan.rotary_dim, heads_here = (kThreads / kParts) >> a.tile_log2;
     if (t >= a.tokens) return;
 
-    const bool turns = 16 * part < d;
-    // pair e of this part joins element e of both accesses (halves), or elements 2 e, 2 e + 1 of the two in a row
-    const int c0 = HALF && turns ? 8 * part : 16 * part;
-    const int c1 = HALF && turns ? 8 * part + d / 2 : 16 * part + 8;
+    // Halves: pair e of this part joins element e of both accesses.  Neighbours: pairs 0 to 3 are the first access's, 4 to 7 the second's.  Channels that
+    // stay are dealt like the others, so that an access of neighbouring lanes is in few pieces.
+    const bool turns[2] = {(HALF ? 16 : 8) * part < d, HALF ? 16 * part < d : 8 * part + kD / 2 < d};
+    const int c0 = HALF && !turns[0] ? d / 2 + 8 * part : 8 * part;
+    const int c1 = c0 + (!HALF ? kD / 2 : turns[0] ? d / 2 : (kD - d) / 2);
     float cosine[8], sine[8];
-    if (turns) {
+    if (turns[0]) {
         const int64_t p = a.positions ? a.positions[(int64_t)b * a.tokens + t] : a.first + t;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const uint64_t angle = (uint64_t)p * a.plan.turns[8 * part + e];
+            const int pair = HALF ? 8 * part + e : 4 * part + e % 4 + e / 4 * (kD / 4);
+            const uint64_t angle = (uint64_t)p * a.plan.turns[pair];   // (0 for pairs that there are not)
             const float x = (float)(int32_t)(angle >> 32) * 0x1p-32f;
             cosine[e] = __builtin_amdgcn_cosf(x) * a.plan.gain;
             sine[e] = __builtin_amdgcn_sinf(x) * a.plan.gain;
@@ -96,7 +99,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a) {
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             if (!to[i]) continue;
-            if (turns && !is_v[i]) {
+            if (turns[0] && !is_v[i]) {
                 float x[2][8], y[2][8];
                 unpack8<BF16>(u[i][0], x[0]);
                 unpack8<BF16>(u[i][1], x[1]);
@@ -108,7 +111,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a) {
                     y[r1][e1] = fmaf(q, cosine[e], p * sine[e]);
                 }
                 u[i][0] = pack8<BF16>(y[0]);
-                u[i][1] = pack8<BF16>(y[1]);
+                if (turns[1]) u[i][1] = pack8<BF16>(y[1]);
             }
             store16<STREAM>(to[i] + c0, u[i][0]);
             store16<STREAM>(to[i] + c1, u[i][1]);
@@ -212,8 +215,8 @@ int specache_rotate(const specache_rotary* plan, int32_t dtype, int32_t batch, i
     if (split < 1) split = 1;
     if (split > passes) split = passes;
     const dim3 grid((unsigned)tiles, (unsigned)split);
-    const bool stream_out = (int64_t)batch * tokens * n * kD * 2 > kCached;
     const bool half = plan->layout == SPECACHE_ROTARY_HALF;
+    const bool stream_out = (int64_t)batch * tokens * n * kD * 2 > kCached && (!half || plan->rotary_dim == kD);
     const auto kernel = dtype == SPECACHE_BF16
                             ? (half ? (stream_out ? rotate_kernel<true, true, true> : rotate_kernel<true, true, false>)
                                     : (stream_out ? rotate_kernel<true, false, true> : rotate_kernel<true, false, false>))
