@@ -516,7 +516,7 @@ typedef struct specache_window_config {
     int32_t n_kv_heads; /* >= 1                                                                        */
     int32_t head_dim;   /* must be 128                                                                 */
     int32_t q_tokens;   /* rows of q and out per sequence and head, >= 0                               */
-    int32_t kv_tokens;  /* rows of k and v per sequence and head, >= 0; up to 2^30                     */
+    int32_t kv_tokens;  /* rows of k and v per sequence and head, >= 0; up to 2^28                     */
     int32_t window;     /* positions seen, the row's own included; 0: all                              */
     int32_t sinks;      /* first positions that stay visible behind the window, >= 0                   */
     int32_t dtype;      /* SPECACHE_FP16 or SPECACHE_BF16: type of q, k, v and out                     */

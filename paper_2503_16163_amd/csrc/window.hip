@@ -572,10 +572,14 @@ int check(const specache_window_config* c) {
     if (c->head_dim != kD) return fail_without_context(SPECACHE_EINVAL, "head_dim must be 128");
     if (c->dtype != SPECACHE_FP16 && c->dtype != SPECACHE_BF16) return fail_without_context(SPECACHE_EINVAL, "dtype must be SPECACHE_FP16 or SPECACHE_BF16");
     if (!std::isfinite(c->sm_scale)) return fail_without_context(SPECACHE_EINVAL, "sm_scale must be finite");
-    if (c->kv_tokens > (1 << 30) || (int64_t)c->q_tokens * (c->n_q_heads / c->n_kv_heads) > (1 << 30))
+    // (positions, and their distances from a window's or a tile's edge, then keep to 32 bits)
+    if (c->kv_tokens > (1 << 28) || (int64_t)c->q_tokens * (c->n_q_heads / c->n_kv_heads) > (1 << 28))
         return fail_without_context(SPECACHE_EINVAL, "too many tokens");
     return SPECACHE_OK;
 }
+
+// a window that holds every position is none
+int window_of(const specache_window_config& c) { return c.window < c.kv_tokens ? c.window : 0; }
 
 // Steps: one round of workgroups (two on a compute unit by their LDS), chunks of at most 64 tiles (2048 positions) so that a ragged batch's lengths
 // even out, a tile for every wave at least, and no more than 256 chunks of a row to merge unless they are that long.  us, by chunks: one sequence of 8
@@ -590,7 +594,7 @@ int plan_of(const specache_window_config& c, Plan& p) {
     const int G = c.n_q_heads / c.n_kv_heads;
     const int64_t rows = (int64_t)c.q_tokens * G;
     int64_t most = c.kv_tokens;                     // positions that a row tile walks
-    if (c.window) most = std::min<int64_t>(most, (int64_t)c.window + c.sinks + 128);
+    if (window_of(c)) most = std::min<int64_t>(most, (int64_t)c.window + c.sinks + 128);
     const int64_t heads = (int64_t)c.batch * c.n_kv_heads;
     int64_t chunks = 1;
     if (rows <= kWaveRows) {
@@ -670,8 +674,8 @@ int specache_window_attend(const specache_window_config* cfg, const specache_vie
     a.G = cfg->n_q_heads / cfg->n_kv_heads;
     a.q_tokens = cfg->q_tokens;
     a.kv_tokens = cfg->kv_tokens;
-    a.window = cfg->window;
-    a.sinks = cfg->sinks;
+    a.window = window_of(*cfg);
+    a.sinks = std::min(cfg->sinks, cfg->kv_tokens);
     a.row_tiles = p.row_tiles;
     a.item_rows = p.item_rows;
     a.chunks = p.chunks;

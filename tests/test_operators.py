@@ -101,7 +101,7 @@ def _window(cfg, q=View(A, 1536, 384, 128), k=View(2 * A, 2560, 1280, 128), v=Vi
 
 def test_window_attend_refuses():
     for change in (dict(batch=-1), dict(q_tokens=-1), dict(kv_tokens=-1), dict(window=-1), dict(sinks=-1), dict(n_kv_heads=0), dict(n_q_heads=3), dict(n_q_heads=130),
-                   dict(head_dim=64), dict(dtype=2), dict(sm_scale=math.nan), dict(sm_scale=math.inf), dict(kv_tokens=(1 << 30) + 1), dict(q_tokens=1 << 30)):
+                   dict(head_dim=64), dict(dtype=2), dict(sm_scale=math.nan), dict(sm_scale=math.inf), dict(kv_tokens=(1 << 28) + 1), dict(q_tokens=1 << 28)):
         assert _window(_config(**change)) == binding.EINVAL, change
         size = C.c_int64(-7)
         assert binding.lib().specache_window_scratch(C.byref(_config(**change)), C.byref(size)) == binding.EINVAL and size.value == -7
