@@ -4,8 +4,8 @@
 // choice a place in that order: the first element at which a count, or the running sum of the weights, reaches a target.  Nothing
 // of the row's length is sorted for it.
 //   - Few tokens kept: those that can be are listed in LDS, sorted there, and their weights summed in order.  With top_k the list is what
-//     is not below the k-th largest of the threads' own maxima (there are k such elements at least, and hardly more); without it, what
-//     a histogram over the logarithm of the weights puts in or before the bin where the kept mass ends.
+//     is not below the k-th largest of the threads' own maxima, or of the 16-byte vectors' (there are k such elements at least, and hardly more);
+//     without it, what a histogram over the logarithm of the weights puts in or before the bin where the kept mass ends.
 //   - Many: the elements of the histogram's bins that hold the targets are listed; a bin that holds too many is taken apart further, by the bits
 //     of its logits.
 // An element's weight is r 2^(-bin / 64): the power of the bin, of which there are 64 per power of two, and a whole number r of units 2^-R,
@@ -25,6 +25,9 @@ constexpr int kList = 2048;            // elements that are sorted at once
 constexpr int kFew = 256;              // a list so short is sorted by comparing each with all the others,
 constexpr int kRanked = 1024;          // of a bin's so many each is compared with all the others
 constexpr int kTable = 32768;          // vectors of a row whose largest logits are kept (32 of each thread)
+// top_k by the threads' largest logits, by the vectors': us, 256 rows of 128256 / 17 of 49999 in fp32, top_k 100 by the one 22.3 / 13.0, by the other 23.8 / 14.4;
+// 200 24.6 / 15.7 and 25.7 / 16.3; 400 25.9 / 15.7 by the vectors', 1400 36 / 20.
+constexpr int kFewMaxima = 256, kMostByMaxima = 1536;
 constexpr int kMostVocab = 1 << 20;
 
 struct SampleArgs {
@@ -137,11 +140,20 @@ __device__ __forceinline__ void each_from(const Shared& s, const T* row, int n, 
     const uint32_t from = float_to_key(least) >> 16;
     uint32_t wanted = 0;
     for (int v = threadIdx.x, i = 0; v < vecs; v += kThreads, ++i) wanted |= (uint32_t)(s.vector_most[v] >= from) << i;
-    for (; wanted; wanted &= wanted - 1) {
-        const int v = threadIdx.x + __builtin_ctz(wanted) * kThreads;
-        const Vec x = ((const Vec*)(row + head))[v];
+    constexpr int kAhead = 4;
+    while (wanted) {
+        Vec x[kAhead];
+        int v[kAhead];
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) one(x[e], head + v * kVec + e);
+        for (int j = 0; j < kAhead; ++j, wanted &= wanted - 1) {
+            v[j] = wanted ? threadIdx.x + __builtin_ctz(wanted) * kThreads : -1;
+            if (wanted) x[j] = ((const Vec*)(row + head))[v[j]];
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+            if (v[j] >= 0)
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) one(x[j][e], head + v[j] * kVec + e);
     }
 }
 struct Range {
@@ -166,7 +178,12 @@ struct Weights {
         const float d = ((float)first - 0.01f) / bins_per_logit;
         return most - d + (d * 0x1p-16f + fabsf(most) * 0x1p-20f);
     }
+    // 2^(-f / 64) for a place f from 0 to 1 in a bin: 1 + f (c1 + f c2), off by 2^-26.8 at most (the best such polynomial)
+    __device__ __forceinline__ uint32_t units_of_place(float f) const {
+        return (uint32_t)fmaf(f, fmaf(f, 0x1.e984d6p-15f, -0x1.62e36cp-7f) * unit, unit + 0.5f);
+    }
     __device__ __forceinline__ uint32_t units(float depth, uint32_t bin) const {
+        if (bin < kBins - 1) return units_of_place(depth - (float)bin);
         return (uint32_t)fmaf(__builtin_amdgcn_exp2f(((float)bin - depth) * (1.0f / kBinsPerLog2)), unit, 0.5f);
     }
     __device__ __forceinline__ double of_bin(uint64_t units, uint32_t bin) const {
@@ -509,11 +526,12 @@ __device__ __forceinline__ int choose(Shared& s, const Weights& w, const uint64_
 }
 
 // A workgroup per row: it reads the row once for its largest logits (256 rows of 128256 in bfloat16, 66 MB: greedy choices take 14 us, where the bytes need
-// 11), and again what it cannot leave out.  The same rows with top_k 50 22 us (of the second reading only the vectors whose largest logit
-// counts; 28 with all of it), 1000 51, without a limit 56, top_p 0.9 59: the histogram of a whole row, 20 us of vector instructions and LDS
-// additions on its compute unit, and a third reading.  Two rows of 32000: 4.8, 11.5, 25, 20, 22 us, a chain of some 20 barriers and as many
-// exchanges.  A row to a workgroup, not to several: with as many rows as compute units nothing is gained, and few rows would pay a launch
-// (3 us) for each reading.
+// 11), and again what it cannot leave out.  The same rows with top_k 50 21 us (of the second reading only the vectors whose largest logit
+// counts; 28 with all of it), 1000 32 (51 from the threads' largest logits, of which the 1000th is no limit), without a limit 54, top_p 0.9 55, at a
+// temperature of 0.7 50 (65 with every element that falls to the last bin added there): the histogram of a whole row, some 18 us of vector instructions and
+// LDS additions on its compute unit (20 with an exponential for every element), and a third reading.  Two rows of 32000: 4.5, 11, 17, 19, 21, 20 us, a chain
+// of some 20 barriers and as many exchanges.  A row to a workgroup, not to several: with as many rows as compute units nothing is gained, and few
+// rows would pay a launch (3 us) for each reading.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     __shared__ Shared s;
@@ -564,27 +582,32 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     lim.depth = min_p > 0.0f ? fmaxf(-kBinsPerLog2 * log2f(min_p), 0.0f) : -1.0f;
     lim.u = fminf(fmaxf(a.u[r], 0.0f), 0x1.fffffep-1f);
 
-    if (lim.count <= kThreads) {
-        // the bin of the count-th largest of the threads' own largest; the least of those up to there
+    const bool by_vector = lim.count > kFewMaxima && n / kVec <= kTable;
+    if (lim.count <= (by_vector ? kMostByMaxima : kThreads / 2)) {
         clear_bins(s);
-        const uint32_t own_bin = w.bin_of(w.depth(own_most));
-        if (own_most > -INFINITY) atomicAdd((unsigned long long*)&s.bins[own_bin], 1ull << a.count_shift);
-        __syncthreads();
-        uint32_t before_count = 0;
+        uint32_t before_count = 0, end = kBins;
         double before_mass = 0.0;
+        float least = -INFINITY;
         const Target last{true, false, lim.count, 0.0};
-        const uint32_t bin = find_bin<false>(s, sum_bins<false>(s, w, a.count_shift, -1), last, before_count, before_mass);
-        if (own_most > -INFINITY && own_bin <= bin) atomicMax(&s.key_high, descending_key(own_most));
-        __syncthreads();
-        const float least = bin == kBins ? -INFINITY : logit_of_key(s.key_high);
-        uint32_t end = kBins;
-        if (lim.count > kThreads * 3 / 4) {
-            // many more than count are not below that: their histogram first
-            clear_bins(s);
-            each_from(s, row, n, least, [&](float l, int) { atomicAdd((unsigned long long*)&s.bins[w.bin_of(w.depth(l))], 1ull << a.count_shift); });
+        if (!by_vector) {
+            // the bin of the count-th largest of the threads' own largest; the least of those up to there
+            const uint32_t own_bin = w.bin_of(w.depth(own_most));
+            if (own_most > -INFINITY) atomicAdd((unsigned long long*)&s.bins[own_bin], 1ull << a.count_shift);
             __syncthreads();
-            before_count = 0;
+            const uint32_t bin = find_bin<false>(s, sum_bins<false>(s, w, a.count_shift, -1), last, before_count, before_mass);
+            if (own_most > -INFINITY && own_bin <= bin) atomicMax(&s.key_high, descending_key(own_most));
+            __syncthreads();
+            if (bin < kBins) least = logit_of_key(s.key_high);
+        } else {
+            // the bin of the count-th largest of the vectors' largest, each taken for what is surely not above it
+            const int head = min(n, (int)((16 - (uintptr_t)row % 16) % 16 / sizeof(T)));
+            for (int v = threadIdx.x; v < (n - head) / kVec; v += kThreads) {
+                const float l = logit_of_key(~((uint32_t)(s.vector_most[v] - 1) << 16));
+                if (l > -INFINITY) atomicAdd((unsigned long long*)&s.bins[w.bin_of(w.depth(l))], 1ull << a.count_shift);
+            }
+            __syncthreads();
             end = find_bin<false>(s, sum_bins<false>(s, w, a.count_shift, -1), last, before_count, before_mass);
+            if (end < kBins) least = w.below(end);
         }
         each_from(s, row, n, least, [&](float l, int i) {
             if (w.bin_of(w.depth(l)) <= end) list_one(s, l, i);
@@ -600,15 +623,31 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
 
     const auto histogram = [&]() {
         clear_bins(s);
-        // without branches: what is not allowed is counted where nobody looks
+        // The last bin takes many of a row where the temperature is low, so every thread sums its own there (and a row whose largest logit is
+        // infinite has all but those); without branches else: what is not of the other bins is added where nobody looks.
+        const uint64_t one = (uint64_t)(1u << (a.count_shift - 32)) << 32;
+        uint64_t light = 0;
         each_vector(row, n, [&](const auto& x, int, int elements, int) {
+            bool rest = false;
 #pragma unroll
             for (int e = 0; e < kVec; ++e) {
-                const float l = logit_of(x[e]), d = w.depth(l);
-                const uint32_t bin = w.bin_of(d), place = l > -INFINITY && e < elements ? bin : kBins + threadIdx.x % 64;
-                atomicAdd((unsigned long long*)&s.bins[place], 1ull << a.count_shift | w.units(d, bin));
+                const float d = (w.most - logit_of(x[e])) * w.bins_per_logit;
+                const bool in = d < kBins - 1.0f && e < elements;
+                rest |= !in;
+                atomicAdd((unsigned long long*)&s.bins[in ? (uint32_t)d : kBins + threadIdx.x % 64], one | w.units_of_place(__builtin_amdgcn_fractf(d)));
             }
+            if (rest)
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) {
+                    const float l = logit_of(x[e]), d = w.depth(l);
+                    if (!((w.most - l) * w.bins_per_logit < kBins - 1.0f) && l > -INFINITY && e < elements) {
+                        if (d < kBins - 1.0f) atomicAdd((unsigned long long*)&s.bins[0], one | w.units(d, 0));   // (infinite)
+                        else light += one | w.units(d, kBins - 1);
+                    }
+                }
         });
+        for (int d = 32; d; d /= 2) light += __shfl_xor((unsigned long long)light, d);
+        if (threadIdx.x % 64 == 0 && light) atomicAdd((unsigned long long*)&s.bins[kBins - 1], (unsigned long long)light);
         __syncthreads();
     };
     histogram();
@@ -778,7 +817,7 @@ int specache_sample(const specache_sample_config* cfg, const void* logits, const
     int bits = 0;
     while ((1 << bits) < cfg->vocab) ++bits;
     a.unit_log2 = 62 - 2 * bits < 28 ? 62 - 2 * bits : 28;
-    a.count_shift = bits + a.unit_log2 + 1;
+    a.count_shift = bits + a.unit_log2 + 1 > 32 ? bits + a.unit_log2 + 1 : 32;   // (the upper word's, for a cheap sum of the two)
     const auto kernel = cfg->dtype == SPECACHE_FP32 ? sample_kernel<float> : cfg->dtype == SPECACHE_BF16 ? sample_kernel<__bf16> : sample_kernel<_Float16>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)cfg->rows), dim3(kThreads), 0, (hipStream_t)stream, a);
     return launched();
