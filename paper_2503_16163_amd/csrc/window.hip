@@ -42,6 +42,7 @@ struct WindowArgs {
     float* part_o;                    // [item][chunk][item_rows][kD], not divided by the sum
     float* part_ml;                   // [item][chunk][item_rows][2]: maximum (in powers of two), sum
     int n_kv_heads, G, q_tokens, kv_tokens, window, sinks;
+    int merge_rows;                   // items * item_rows
     int row_tiles, item_rows, chunks; // an item is a tile of item_rows rows of a KV head of a sequence
     float scale;                      // sm_scale in powers of two
 };
@@ -497,13 +498,17 @@ __global__ __launch_bounds__(64 * WAVES) void step_kernel(WindowArgs a) {
 // The chunks of a row, joined: two channels per lane, the chunks dealt to the waves of a workgroup.  What it takes is latency, so every load of a
 // wave's first chunks is asked for at once, and each wave goes by its own chunks' maximum (4.9 us of a step of one short sequence
 // with the loads behind the row's maximum, 4.5 so).
-constexpr int kMergeWaves = 4;
-template <bool BF16>
+// Up to kFewChunks a wave takes a row by itself, without LDS: 4 chunks of 16384 rows, 34 MB, 9.8 us (3.4 TB/s) against 39 with four waves to a
+// row, three of them for one chunk each.
+constexpr int kMergeWaves = 4, kFewChunks = 4;
+template <bool BF16, int WAVES>
 __global__ __launch_bounds__(64 * kMergeWaves) void merge_kernel(WindowArgs a) {
-    __shared__ float part[kMergeWaves][kD];
-    __shared__ float2 joined[kMergeWaves];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int row = blockIdx.x % a.item_rows, item = blockIdx.x / a.item_rows;
+    __shared__ float part[WAVES][kD];
+    __shared__ float2 joined[WAVES];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64 % WAVES;
+    const int place_of_row = blockIdx.x * (kMergeWaves / WAVES) + threadIdx.x / (64 * WAVES);
+    const int row = place_of_row % a.item_rows, item = place_of_row / a.item_rows;
+    if (WAVES < kMergeWaves && place_of_row >= a.merge_rows) return;
     const int b = item / a.row_tiles / a.n_kv_heads, h = item / a.row_tiles % a.n_kv_heads;
     const int r = (a.row_tiles - 1 - item % a.row_tiles) * a.item_rows + row;
     const int n = length_of(a.q_lengths, b, a.q_tokens);
@@ -511,12 +516,12 @@ __global__ __launch_bounds__(64 * kMergeWaves) void merge_kernel(WindowArgs a) {
     const float2* ml = (const float2*)a.part_ml + place;
     const float* po = a.part_o + place * kD + 2 * lane;
     float m = kNever, l = 0.0f, x = 0.0f, y = 0.0f;
-    constexpr int kAhead = 8;
-    for (int c0 = wave; c0 < a.chunks; c0 += kAhead * kMergeWaves) {
+    constexpr int kAhead = WAVES == 1 ? kFewChunks : 8;
+    for (int c0 = wave; c0 < a.chunks; c0 += kAhead * WAVES) {
         float2 one[kAhead], oc[kAhead];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            const int64_t at = (int64_t)min(c0 + i * kMergeWaves, a.chunks - 1) * a.item_rows;
+            const int64_t at = (int64_t)min(c0 + i * WAVES, a.chunks - 1) * a.item_rows;
             one[i] = ml[at];
             oc[i] = *(const float2*)(po + at * kD);
         }
@@ -529,27 +534,29 @@ __global__ __launch_bounds__(64 * kMergeWaves) void merge_kernel(WindowArgs a) {
         m = most;
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            if (c0 + i * kMergeWaves >= a.chunks || one[i].y == 0.0f) continue;   // (an empty chunk stored no sums)
+            if (c0 + i * WAVES >= a.chunks || one[i].y == 0.0f) continue;   // (an empty chunk stored no sums)
             const float w = __builtin_amdgcn_exp2f(one[i].x - m);
             l = fmaf(w, one[i].y, l);
             x = fmaf(w, oc[i].x, x);
             y = fmaf(w, oc[i].y, y);
         }
     }
-    *(float2*)&part[wave][2 * lane] = float2{x, y};
-    if (lane == 0) joined[wave] = float2{m, l};
-    __syncthreads();
-    if (wave || r >= n * a.G) return;
+    if constexpr (WAVES > 1) {
+        *(float2*)&part[wave][2 * lane] = float2{x, y};
+        if (lane == 0) joined[wave] = float2{m, l};
+        __syncthreads();
+        if (wave || r >= n * a.G) return;
 #pragma unroll
-    for (int w = 0; w < kMergeWaves; ++w) m = fmaxf(m, joined[w].x);
-    l = x = y = 0.0f;
+        for (int w = 0; w < WAVES; ++w) m = fmaxf(m, joined[w].x);
+        l = x = y = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kMergeWaves; ++w) {
-        const float f = __builtin_amdgcn_exp2f(joined[w].x - m);
-        const float2 o = *(const float2*)&part[w][2 * lane];
-        l = fmaf(f, joined[w].y, l);
-        x = fmaf(f, o.x, x);
-        y = fmaf(f, o.y, y);
+        for (int w = 0; w < WAVES; ++w) {
+            const float f = __builtin_amdgcn_exp2f(joined[w].x - m);
+            const float2 o = *(const float2*)&part[w][2 * lane];
+            l = fmaf(f, joined[w].y, l);
+            x = fmaf(f, o.x, x);
+            y = fmaf(f, o.y, y);
+        }
     }
     const float by = l == 0.0f ? 0.0f : 1.0f / l;
     uint16_t* to = (uint16_t*)a.out.data + b * a.out.batch + (h * a.G + r % a.G) * a.out.head + r / a.G * a.out.token;
@@ -626,7 +633,8 @@ void launch(const Plan& p, const WindowArgs& a, hipStream_t stream) {
     if (p.kernel == kStep) hipLaunchKernelGGL((split ? step_kernel<BF16, true, kStepWaves> : step_kernel<BF16, false, kStepWaves>), grid, dim3(64 * kStepWaves), 0, stream, a);
     else if (p.kernel == kTile4) hipLaunchKernelGGL((split ? tile_kernel<BF16, true, 4> : tile_kernel<BF16, false, 4>), grid, dim3(256), 0, stream, a);
     else hipLaunchKernelGGL((split ? tile_kernel<BF16, true, 8> : tile_kernel<BF16, false, 8>), grid, dim3(512), 0, stream, a);
-    if (split) hipLaunchKernelGGL(merge_kernel<BF16>, dim3((unsigned)(p.items * p.item_rows)), dim3(64 * kMergeWaves), 0, stream, a);
+    if (split && p.chunks <= kFewChunks) hipLaunchKernelGGL((merge_kernel<BF16, 1>), dim3((unsigned)((a.merge_rows + kMergeWaves - 1) / kMergeWaves)), dim3(64 * kMergeWaves), 0, stream, a);
+    else if (split) hipLaunchKernelGGL((merge_kernel<BF16, kMergeWaves>), dim3((unsigned)a.merge_rows), dim3(64 * kMergeWaves), 0, stream, a);
 }
 
 }  // namespace
@@ -676,6 +684,7 @@ int specache_window_attend(const specache_window_config* cfg, const specache_vie
     a.kv_tokens = cfg->kv_tokens;
     a.window = window_of(*cfg);
     a.sinks = std::min(cfg->sinks, cfg->kv_tokens);
+    a.merge_rows = (int)(p.items * p.item_rows);
     a.row_tiles = p.row_tiles;
     a.item_rows = p.item_rows;
     a.chunks = p.chunks;
