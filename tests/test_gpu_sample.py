@@ -134,6 +134,47 @@ def test_rows_that_lie_apart_and_odd_addresses(dtype):
     assert _call(x, u) == _call(x.contiguous(), u)
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V,allowed", [(1537, 1.0), (9001, 1.0), (50021, 1.0), (50021, 0.03), (128256, 0.3)])
+def test_top_k_of_some_hundred(V, allowed, dtype):
+    """Around what is found from the row's vectors alone; masked rows, stretches of NaN of either sign, an odd address."""
+    ks = [255, 256, 257, 400, 1023, 1024, 1025, 1535, 1536, 1537]
+    rng = np.random.default_rng(V)
+    wide = _logits(V, len(ks), V + 1, dtype)
+    if allowed < 1:
+        wide.masked_fill_(torch.rand(wide.shape, generator=torch.Generator(device="cuda").manual_seed(V), device="cuda") >= allowed, -math.inf)
+    wide[:, 64:193] = math.nan
+    wide[:, 300:500] = -wide[:, 64:65]
+    for x in (wide[:, :V], wide[:, 1:]):
+        _check(x, rng.random(len(ks), dtype=np.float32).tolist(), t=[3.0] * len(ks), k=ks)
+        _check(x, [1 - 2.0 ** -24] * len(ks), t=[30.0] * len(ks), k=ks, p=[0.999] * len(ks))
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+def test_low_temperatures(dtype):
+    """Most of a row far below its largest logits."""
+    x = _logits(12, 6, 50021, dtype)
+    x[3:, 1000:1200] = 14.0
+    u = [0.0, 0.4, 0.9, 0.2, 0.7, 0.95]
+    for t in (0.5, 0.1, 0.01):
+        _check(x, u, t=[t] * 6)
+        _check(x, u, t=[t] * 6, k=[0, 300, 5000, 100, 40000, 0], p=[0.9, 1.0, 0.999, 0.5, 0.9, 1.0], m=[0.0, 0.0, 0.0, 0.0, 0.0, 1e-12])
+
+
+@pytest.mark.parametrize("V", [3000, 40000])
+def test_many_infinite_logits(V):
+    """Of 700 infinite logits every one weighs the same, and all others nothing."""
+    x = _logits(13, 4, V, torch.float32)
+    at = torch.arange(700) * 3 + 11
+    x[:, at.cuda()] = math.inf
+    u = [0.0, 0.3, 0.77, 1 - 2.0 ** -24]
+    place = lambda n: [int(at[int(n * np.float64(np.float32(a)))]) for a in u]
+    assert _call(x, u) == place(700)
+    assert _call(x, u, k=[50] * 4) == place(50)
+    assert _call(x, u, k=[500] * 4) == place(500)
+    assert _call(x, u, k=[1400] * 4, m=[0.5] * 4) == place(700)
+
+
 def test_frequencies_follow_the_weights():
     """4096 evenly spread numbers over one row: every token as often as its share, to one number at either of its borders."""
     x = torch.tensor([0.0, 2.0, 1.0, -1.0, 2.0, -math.inf, 0.5], device="cuda").repeat(4096, 1)
