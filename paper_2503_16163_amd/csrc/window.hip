@@ -289,7 +289,8 @@ __device__ __forceinline__ int on_one_xcd(int per_head) {
 }
 
 // Tiles of 64 positions travel to LDS while the one before is worked on; a wave takes 1/WAVES of a tile's keys and values.
-// us, 32 heads over a prompt of 16k tokens: 2157 (1.02 PFLOP/s), 8 heads of 4 queries over 32k through a window of 4096 2060.
+// us, 32 heads over a prompt of 16k tokens: 2165 (1.02 PFLOP/s, the matrix cores busy 0.52 of the time at the clock that random inputs leave), 8 heads of 4
+// queries over 32k through a window of 4096 1980 to 2040, 256 tokens of 8 heads of 8 behind 32k 253.
 template <bool BF16, bool SPLIT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void tile_kernel(WindowArgs a) {
     constexpr int TILE = 64, ROWS = WAVES * kWaveRows, FETCHES = 16 / WAVES;
@@ -601,7 +602,8 @@ int window_of(const specache_window_config& c) { return c.window < c.kv_tokens ?
 // 261; 1 head, 100000 positions, 128 chunks 28, 256 26, 512 33.  Up to 4 tiles per wave no chunks at all, as a merge is a launch more: 256
 // positions 7.8 us against 9.0 with them, 512 positions 12.0 against 9.5.
 // Prompts: 8 waves to a workgroup where a row tile walks 2048 positions or more (8 waves / 4: a prompt of 16k tokens 2148 / 2225 us, through a
-// window of 4096 1974 / 2014, but ragged ones of up to 3001 tokens through 512 189 / 172: its first tiles and edges are then most of a walk);
+// window of 4096 1974 / 2014, but ragged ones of up to 3001 tokens through 512 145 / 134, 8 prompts of 1000 tokens
+// 106 / 98: first tiles and edges are then most of a walk);
 // row tiles that are too few for the chip have their positions split, at least four tiles to a chunk.
 constexpr int64_t kStepsAtOnce = 512;
 int plan_of(const specache_window_config& c, Plan& p) {
