@@ -84,7 +84,14 @@ __device__ __forceinline__ void each_vector(const T* row, int n, F&& f) {
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) f(x[i], head + (v + i * kThreads) * kVec, kVec, v + i * kThreads);
     }
-    for (; v < vecs; v += kThreads) f(body[v], head + v * kVec, kVec, v);
+    if (v < vecs) {
+        Vec x[kAhead - 1];
+#pragma unroll
+        for (int i = 0; i < kAhead - 1; ++i) x[i] = body[min(v + i * kThreads, vecs - 1)];
+#pragma unroll
+        for (int i = 0; i < kAhead - 1; ++i)
+            if (v + i * kThreads < vecs) f(x[i], head + (v + i * kThreads) * kVec, kVec, v + i * kThreads);
+    }
     if (tail + (int)threadIdx.x < n) {
         Vec x{};
         x[0] = row[tail + threadIdx.x];

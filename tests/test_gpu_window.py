@@ -97,6 +97,7 @@ SHAPES = [  # B, Hq, Hkv, n, N, window, sinks
     (1, 1, 1, 2, 2, 0, 0), (1, 2, 2, 31, 31, 0, 0), (2, 4, 2, 64, 64, 0, 0), (1, 5, 5, 65, 65, 0, 0), (1, 6, 2, 129, 129, 1, 0), (1, 2, 1, 200, 200, 64, 0),
     (2, 3, 3, 257, 257, 65, 1), (1, 4, 1, 300, 300, 100, 64), (1, 2, 2, 513, 513, 200, 600), (1, 7, 1, 150, 150, 0, 0), (1, 8, 4, 700, 700, 33, 130),
     (1, 4, 2, 20, 500, 0, 0), (2, 2, 2, 100, 1000, 300, 5), (1, 8, 1, 33, 3000, 0, 0), (1, 8, 2, 256, 4096, 0, 0), (1, 2, 2, 40, 7, 0, 0), (1, 2, 1, 200, 100, 30, 2), (1, 2, 2, 70, 70, 2 ** 31 - 1, 3), (2, 2, 1, 2, 900, 900, 2 ** 31 - 1), (1, 2, 2, 3, 900, 899, 900),
+    (2, 9, 9, 130, 130, 0, 0), (3, 6, 3, 150, 2500, 0, 0), (1, 8, 8, 520, 520, 100, 3),
 ]
 
 
