@@ -532,11 +532,11 @@ __device__ __forceinline__ int choose(Shared& s, const Weights& w, const uint64_
     return (int)(uint32_t)list[s.mark_count[2]];
 }
 
-// A workgroup per row: it reads the row once for its largest logits (256 rows of 128256 in bfloat16, 66 MB: greedy choices take 14 us, where the bytes need
+// A workgroup per row: it reads the row once for its largest logits (256 rows of 128256 in bfloat16, 66 MB: greedy choices take 13.5 us, where the bytes need
 // 11), and again what it cannot leave out.  The same rows with top_k 50 21 us (of the second reading only the vectors whose largest logit
-// counts; 28 with all of it), 1000 32 (51 from the threads' largest logits, of which the 1000th is no limit), without a limit 54, top_p 0.9 55, at a
-// temperature of 0.7 50 (65 with every element that falls to the last bin added there): the histogram of a whole row, some 18 us of vector instructions and
-// LDS additions on its compute unit (20 with an exponential for every element), and a third reading.  Two rows of 32000: 4.5, 11, 17, 19, 21, 20 us, a chain
+// counts; 28 with all of it), 1000 31 (51 from the threads' largest logits, of which the 1000th is no limit), without a limit 51, top_p 0.9 53, at a
+// temperature of 0.7 49 (65 with every element that falls to the last bin added there): the histogram of a whole row, some 18 us of vector instructions and
+// LDS additions on its compute unit (20 with an exponential for every element), and a third reading.  Two rows of 32000: 4.3, 11, 17, 19, 20, 19 us, a chain
 // of some 20 barriers and as many exchanges.  A row to a workgroup, not to several: with as many rows as compute units nothing is gained, and few
 // rows would pay a launch (3 us) for each reading.
 template <typename T>
