@@ -496,7 +496,7 @@ int specache_rotary_plan(const specache_rotary_config* cfg, specache_rotary* out
  * address and strides) or shares no memory with any input.
  * positions: device int32 [batch, tokens], contiguous; any int32 (a negative one turns the other way).  NULL: token t of
  * every sequence is at first_position + t.  first_position + tokens stays below 2^31.
- * batch = 0, tokens = 0 or n_q_heads = 0 are allowed.
+ * batch = 0, tokens = 0 or n_q_heads = 0 are allowed; tokens goes up to 2^30.
  * Errors: EINVAL (null, misaligned or in-place-but-different views, counts, dtype, a plan that specache_rotary_plan did not write), EHIP.
  */
 int specache_rotate(const specache_rotary* plan, int32_t dtype, int32_t batch, int32_t tokens, int32_t n_q_heads,

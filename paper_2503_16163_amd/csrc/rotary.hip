@@ -179,6 +179,7 @@ int specache_rotate(const specache_rotary* plan, int32_t dtype, int32_t batch, i
         return fail_without_context(SPECACHE_EINVAL, "plan is not one that specache_rotary_plan wrote");
     if (dtype != SPECACHE_FP16 && dtype != SPECACHE_BF16) return fail_without_context(SPECACHE_EINVAL, "dtype must be SPECACHE_FP16 or SPECACHE_BF16");
     if (batch < 0 || tokens < 0 || n_q_heads < 0 || n_kv_heads < 0) return fail_without_context(SPECACHE_EINVAL, "counts must not be negative");
+    if (tokens > (1 << 30)) return fail_without_context(SPECACHE_EINVAL, "too many tokens");
     if (!positions && (int64_t)first_position + tokens > INT32_MAX) return fail_without_context(SPECACHE_EINVAL, "positions pass 2^31");
     if ((k == nullptr) != (k_out == nullptr) || (v == nullptr) != (v_out == nullptr))
         return fail_without_context(SPECACHE_EINVAL, "a tensor and its output are given or left out together");

@@ -80,7 +80,7 @@ def test_rotate_refuses():
     for change in (dict(plan=Rotary()), dict(dtype=2), dict(batch=-1), dict(tokens=-1), dict(n_q=-1), dict(n_kv=-1), dict(q=None), dict(q_out=None),
                    dict(q=View(A + 8, 512, 256, 128)), dict(q=View(A, 512, 256, 132)), dict(q=View(A, 512, -256, 128)), dict(q=View(None, 512, 256, 128)),
                    dict(k=good), dict(v_out=good), dict(q_out=View(A, 512, 128, 256)), dict(q_out=View(2 * A, 512, 256, 0)),
-                   dict(first=2 ** 31 - 2), dict(n_q=1 << 21)):
+                   dict(first=2 ** 31 - 2), dict(n_q=1 << 21), dict(tokens=(1 << 30) + 1)):
         assert _rotate(**change) == binding.EINVAL, change
         assert binding.lib().specache_last_error(None)
     for nothing in (dict(batch=0), dict(tokens=0), dict(n_q=0)):
