@@ -13,6 +13,7 @@
 #include "operators.h"
 #include "wave_ops.h"
 
+#include <algorithm>
 #include <cmath>
 
 namespace specache {
@@ -826,8 +827,19 @@ int specache_sample(const specache_sample_config* cfg, const void* logits, const
     a.unit_log2 = 62 - 2 * bits < 28 ? 62 - 2 * bits : 28;
     a.count_shift = bits + a.unit_log2 + 1 > 32 ? bits + a.unit_log2 + 1 : 32;   // (the upper word's, for a cheap sum of the two)
     const auto kernel = cfg->dtype == SPECACHE_FP32 ? sample_kernel<float> : cfg->dtype == SPECACHE_BF16 ? sample_kernel<__bf16> : sample_kernel<_Float16>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)cfg->rows), dim3(kThreads), 0, (hipStream_t)stream, a);
-    return launched();
+    // (a launch's threads are counted in 32 bits)
+    for (int64_t first = 0, at_once = (1ll << 31) / kThreads; first < cfg->rows; first += at_once) {
+        SampleArgs some = a;
+        some.logits = (const char*)logits + first * cfg->row_stride * (int64_t)size;
+        some.u += first, some.tokens += first;
+        if (temperature) some.temperature += first;
+        if (top_k) some.top_k += first;
+        if (top_p) some.top_p += first;
+        if (min_p) some.min_p += first;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(at_once, cfg->rows - first)), dim3(kThreads), 0, (hipStream_t)stream, some);
+        if (int rc = launched()) return rc;
+    }
+    return SPECACHE_OK;
 }
 
 }  // extern "C"

@@ -175,6 +175,19 @@ def test_many_infinite_logits(V):
     assert _call(x, u, k=[1400] * 4, m=[0.5] * 4) == place(700)
 
 
+def test_more_rows_than_one_launch_takes():
+    """2^21 + 3 rows of two tokens, every parameter a row's own: the last rows choose by theirs."""
+    R = (1 << 21) + 3
+    x = torch.tensor([[0.0, 1.0]], device="cuda").expand(R, -1)
+    u, t = torch.zeros(R, device="cuda"), torch.full((R,), 1.0, device="cuda")
+    k, p, m = torch.zeros(R, dtype=torch.int32, device="cuda"), torch.ones(R, device="cuda"), torch.zeros(R, device="cuda")
+    u[-5:] = 0.99
+    t[-4], k[-3], p[-2], m[-1] = 0.0, 1, 0.5, 0.9
+    tokens = torch.full((R,), -5, dtype=torch.int32, device="cuda")
+    binding.sample(x, u, tokens, t, k, p, m)
+    assert int((tokens[:-5] != 1).sum()) == 0 and tokens[-5:].tolist() == [0, 1, 1, 1, 1]
+
+
 def test_frequencies_follow_the_weights():
     """4096 evenly spread numbers over one row: every token as often as its share, to one number at either of its borders."""
     x = torch.tensor([0.0, 2.0, 1.0, -1.0, 2.0, -math.inf, 0.5], device="cuda").repeat(4096, 1)
