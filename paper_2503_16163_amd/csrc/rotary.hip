@@ -21,6 +21,7 @@ struct RotateArgs {
 
 constexpr int kThreads = 256, kParts = 8;   // a row is 8 lanes' work: 8 pairs of channels each, two 16-byte accesses
 constexpr int kAhead = 4;                   // rows whose loads a lane has in flight
+constexpr int64_t kMostGroups = (1ll << 32) / kThreads;   // a launch's threads are counted in 32 bits
 constexpr int64_t kCached = 32 << 20;       // bytes that the L2s of the 8 XCDs hold
 
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
@@ -208,8 +209,10 @@ int specache_rotate(const specache_rotary* plan, int32_t dtype, int32_t batch, i
     a.first = first_position;
     a.positions = positions;
     while (a.tile_log2 < 2 && (1 << a.tile_log2) < tokens) ++a.tile_log2;
-    const int64_t tiles = (int64_t)batch * (((int64_t)tokens + (1 << a.tile_log2) - 1) >> a.tile_log2);
-    if (tiles > INT32_MAX) return fail_without_context(SPECACHE_EINVAL, "too many tokens");
+    const auto tiles_of = [&](int log2) { return (int64_t)batch * (((int64_t)tokens + (1 << log2) - 1) >> log2); };
+    while (a.tile_log2 < 5 && tiles_of(a.tile_log2) >= kMostGroups) ++a.tile_log2;
+    const int64_t tiles = tiles_of(a.tile_log2);
+    if (tiles >= kMostGroups) return fail_without_context(SPECACHE_EINVAL, "too many tokens");
     const int64_t passes = (n + (32 >> a.tile_log2) - 1) / (32 >> a.tile_log2);   // of a workgroup that walks all heads
     // 16 workgroups per compute unit, if there are heads to split (32k tokens in tiles of 32: 197 us with 1024 workgroups, 192 with 2048, 184 with 4096)
     int64_t split = (4096 + tiles - 1) / tiles;

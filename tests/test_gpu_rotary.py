@@ -103,6 +103,18 @@ def test_rows_beyond_32_bit_offsets():
     assert torch.equal(near, far)
 
 
+def test_more_tokens_than_small_tiles_take():
+    """2^26 + 5 tokens that share their input row: the output's rows are those of shorter calls at the same positions."""
+    n, plan = (1 << 26) + 5, binding.rotary_plan()
+    x = torch.randn((1, 1, 1, 128), device="cuda").to(torch.bfloat16)
+    out = torch.zeros((1, 1, n, 128), device="cuda", dtype=torch.bfloat16)
+    binding.rotate(plan, x.expand(1, 1, n, 128), out, first_position=11)
+    for at in (0, 1 << 20, (1 << 25) + 3, n - 4099):
+        part = torch.empty((1, 1, 4099, 128), device="cuda", dtype=torch.bfloat16)
+        binding.rotate(plan, x.expand(1, 1, 4099, 128), part, first_position=11 + at)
+        assert torch.equal(out[:, :, at:at + 4099], part)
+
+
 def test_captured_and_on_another_stream():
     plan = binding.rotary_plan(64, layout=binding.ROTARY_INTERLEAVED)
     x = torch.randn((2, 8, 40, 128), device="cuda", dtype=torch.float16)
