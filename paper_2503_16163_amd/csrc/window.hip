@@ -629,6 +629,7 @@ int plan_of(const specache_window_config& c, Plan& p) {
         p.items = heads * p.row_tiles;
         if (p.items) chunks = std::min<int64_t>((p.kernel == kTile8 ? 256 : 512) / p.items, (most + 63) / 64 / 4);
     }
+    if (p.items * p.item_rows >= (1ll << 32) / (64 * kMergeWaves)) chunks = 1;   // (the merge's threads, counted in 32 bits)
     p.chunks = (int)std::max<int64_t>(chunks, 1);
     if (p.items * p.chunks > INT32_MAX / 256) return fail_without_context(SPECACHE_EINVAL, "too many rows");
     p.scratch = p.chunks > 1 ? p.items * p.chunks * p.item_rows * (kD + 2) * (int64_t)sizeof(float) : 0;

@@ -80,7 +80,7 @@ def test_rotate_refuses():
     for change in (dict(plan=Rotary()), dict(dtype=2), dict(batch=-1), dict(tokens=-1), dict(n_q=-1), dict(n_kv=-1), dict(q=None), dict(q_out=None),
                    dict(q=View(A + 8, 512, 256, 128)), dict(q=View(A, 512, 256, 132)), dict(q=View(A, 512, -256, 128)), dict(q=View(None, 512, 256, 128)),
                    dict(k=good), dict(v_out=good), dict(q_out=View(A, 512, 128, 256)), dict(q_out=View(2 * A, 512, 256, 0)),
-                   dict(first=2 ** 31 - 2), dict(n_q=1 << 21), dict(tokens=(1 << 30) + 1)):
+                   dict(first=2 ** 31 - 2), dict(n_q=1 << 21), dict(tokens=(1 << 30) + 1), dict(batch=1 << 24)):
         assert _rotate(**change) == binding.EINVAL, change
         assert binding.lib().specache_last_error(None)
     for nothing in (dict(batch=0), dict(tokens=0), dict(n_q=0)):
@@ -97,6 +97,14 @@ def _config(**change):
 def _window(cfg, q=View(A, 1536, 384, 128), k=View(2 * A, 2560, 1280, 128), v=View(3 * A, 2560, 1280, 128), out=View(4 * A, 1536, 384, 128), scratch=None, size=0):
     ref = lambda x: None if x is None else C.byref(x)
     return binding.lib().specache_window_attend(ref(cfg), ref(q), ref(k), ref(v), ref(out), None, None, scratch, size, None)
+
+
+def test_window_scratch_of_very_many_rows():
+    """A merge of 2^24 rows would have more threads than a launch counts: such calls have no chunks."""
+    size = C.c_int64(-7)
+    for heads, chunks in ((16, 9), (32, 0)):
+        assert binding.lib().specache_window_scratch(C.byref(_config(batch=1 << 19, n_q_heads=heads, n_kv_heads=1, q_tokens=1, kv_tokens=20000)), C.byref(size)) == binding.OK
+        assert size.value == (1 << 19) * heads * chunks * (128 + 2) * 4
 
 
 def test_window_attend_refuses():
