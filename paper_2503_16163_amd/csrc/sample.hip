@@ -675,7 +675,9 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     if (threadIdx.x == end / 2) s.mark_count[1] = end % 2 ? bins.count[2] : bins.count[1];
     if (threadIdx.x == 0) s.list_n = 0;
     __syncthreads();
-    if (s.mark_count[1] <= kList) {
+    const uint32_t candidates = s.mark_count[1];
+    __syncthreads();                   // (thread 0 clears that word further down: all have it before)
+    if (candidates <= kList) {
         each_from(s, row, n, w.below(end), [&](float l, int i) {
             if (w.bin_of(w.depth(l)) <= end) list_one(s, l, i);
         });
