@@ -568,7 +568,8 @@ int specache_sample_scratch(const specache_sample_config* cfg, int64_t* bytes);
 /*
  * logits: device [rows] of vocab elements, row_stride apart, aligned to their type.  u: device float32 [rows], in [0, 1).  temperature, top_p, min_p: device
  * float32 [rows]; top_k: device int32 [rows]; each NULL for 1, no limit, no limit, no limit in every row.  A NaN parameter is taken
- * as that.  tokens: device int32 [rows].  The sums are in binary64 or in whole numbers, so that the choice is the same every time.
+ * as that.  tokens: device int32 [rows].  Weights and running sums have 64 bits, added in a fixed order or as whole numbers, so that the choice is the same
+ * every time; they are off by 2^-41 of the row's sum at most, which decides only where u or top_p lies so near to a border between two tokens.
  * scratch, scratch_bytes: as for specache_window_attend.
  * Errors: EINVAL, ECAPACITY (scratch too small), EHIP.
  */
