@@ -48,6 +48,8 @@ struct SampleArgs {
     double unit, weight[4];            // 2^R, and of 2^R (2^(-f / 64) - 1), a polynomial in f, the coefficients
 };
 
+struct Found { uint32_t place, count; double mass; };   // a place in a row's order with a count and a mass
+
 struct Shared {
     uint64_t bins[kBins + 64];         // the last ones take what is left out, a lane each
     uint64_t list[kList];              // descending_key << 32 | index: ascending is the order of the row
@@ -55,9 +57,9 @@ struct Shared {
     double wave_mass[kWavesPerRow];
     uint32_t wave_count[kWavesPerRow];
     float wave_most[kWavesPerRow];
-    uint32_t list_n, key_low, key_high, found_bin, found_count, found_place;
-    double found_mass;
-    int found_index;
+    uint32_t list_n, key_low, key_high, last_bin, found_index;
+    Found found[kWavesPerRow];
+    uint32_t wave_found[kWavesPerRow];
     double mark_mass[2];
     uint32_t mark_count[3];
     double power[64];                  // 2^(-i / 64) / 2^R
@@ -282,36 +284,47 @@ __device__ __forceinline__ BinSums sum_bins(Shared& s, const Weights& w, bool co
     for (int i = 0; i < kOwn; ++i) b.count[i + 1] = b.count[i] + c[i], b.mass[i + 1] = b.mass[i] + m[i];
     return b;
 }
-// The bin in which the target is reached and what lies before it; where it is not (sums made in another order can fall short at the very end):
-// the last one that holds anything, or kBins.
+// What the first thread with one has found, in the threads' order; false where none has.  (Sums next to a border between two threads are added in different
+// orders, so the one's last can lie below the other's first: a place is the first at whose end the target is reached, whatever its beginning.)
+__device__ __forceinline__ bool first_found(Shared& s, bool here, Found& f) {
+    const uint32_t tid = thread(), lane = tid % 64, wave = tid / 64;
+    const uint64_t lanes = __ballot(here);
+    if (lanes ? lane == (uint32_t)__builtin_ctzll(lanes) : lane == 0) {
+        s.found[wave] = f;
+        s.wave_found[wave] = lanes != 0;
+    }
+    __syncthreads();
+    const uint64_t waves = __ballot(lane < kWavesPerRow && s.wave_found[lane % kWavesPerRow]);
+    if (waves) f = s.found[__builtin_ctzll(waves)];
+    __syncthreads();
+    return waves != 0;
+}
+// The first bin with elements at whose end the target is reached, and what lies before it; where there is none (sums made in another order can fall short at
+// the very end): the last one with elements, or kBins.
 template <bool OR_LAST>
 __device__ __forceinline__ uint32_t find_bin(Shared& s, const BinSums& b, const Target& t, uint32_t& before_count, double& before_mass) {
     const uint32_t tid = thread();
-    if (tid == 0) s.found_bin = kBins;
-    __syncthreads();
+    Found f{kBins, 0, 0.0};
 #pragma unroll
-    for (int i = 0; i < kOwn; ++i)   // (exactly one bin: reached with it and not before it; an empty bin changes nothing)
-        if (!t.reached(before_count + b.count[i], before_mass + b.mass[i]) && t.reached(before_count + b.count[i + 1], before_mass + b.mass[i + 1]))
-            s.found_bin = kOwn * tid + i, s.found_count = before_count + b.count[i], s.found_mass = before_mass + b.mass[i];
-    __syncthreads();
-    uint32_t bin = s.found_bin;
-    if (OR_LAST && bin == kBins) {
-        __syncthreads();
-        if (tid == 0) s.found_bin = 0;
+    for (int i = kOwn - 1; i >= 0; --i)
+        if (b.count[i + 1] > b.count[i] && t.reached(before_count + b.count[i + 1], before_mass + b.mass[i + 1]))
+            f = Found{kOwn * tid + i, before_count + b.count[i], before_mass + b.mass[i]};
+    if (!first_found(s, f.place < kBins, f)) {
+        if (!OR_LAST) return kBins;
+        if (tid == 0) s.last_bin = 0;
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kOwn; ++i)
-            if (b.count[i + 1] > b.count[i]) atomicMax(&s.found_bin, kOwn * tid + i);
+            if (b.count[i + 1] > b.count[i]) atomicMax(&s.last_bin, kOwn * tid + i);
         __syncthreads();
-        bin = s.found_bin;
+        const uint32_t last = s.last_bin;
 #pragma unroll
         for (int i = 0; i < kOwn; ++i)
-            if (bin == kOwn * tid + i) s.found_count = before_count + b.count[i], s.found_mass = before_mass + b.mass[i];
-        __syncthreads();
+            if (last == kOwn * tid + i) f = Found{last, before_count + b.count[i], before_mass + b.mass[i]};
+        first_found(s, tid == last / kOwn, f);
     }
-    before_count = s.found_count, before_mass = s.found_mass;
-    __syncthreads();
-    return bin;
+    before_count = f.count, before_mass = f.mass;
+    return f.place;
 }
 
 template <bool COUNTS, bool MASS>
@@ -441,7 +454,7 @@ __device__ __forceinline__ int index_of_place(Shared& s, int n, uint32_t k, Same
         for (int i = begin; i < end; ++i)
             if (same(i) && ++place == k) s.found_index = i;
     __syncthreads();
-    return s.found_index;
+    return (int)s.found_index;
 }
 
 // The element at which t is reached, from the histogram in s.bins (t by count: and s.places); kept is false where that had to make room.
@@ -514,14 +527,15 @@ __device__ __forceinline__ Place find(Shared& s, const T* row, int n, const Weig
     double mass[3];
     sum_list(s, w, list, have, before_mass, mass);
     // the first that reaches it, or the last one
+    Found f{0, 0, 0.0};
+    bool here_too = false;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint32_t at = 2 * tid + i, c = before_count + at;
-        if (at < have && !t.reached(c, mass[i]) && (t.reached(c + 1, mass[i + 1]) || at + 1 == have))
-            s.found_mass = mass[i + 1], s.found_index = (int)(uint32_t)list[at];
+    for (int i = 1; i >= 0; --i) {
+        const uint32_t at = 2 * tid + i;
+        if (at < have && (at + 1 == have || t.reached(before_count + at + 1, mass[i + 1]))) f = Found{at, 0, mass[i + 1]}, here_too = true;
     }
-    __syncthreads();
-    const Place p{s.found_mass, s.found_index};
+    first_found(s, here_too, f);
+    const Place p{f.mass, (int)(uint32_t)list[f.place]};
     __syncthreads();
     return p;
 }
@@ -538,38 +552,39 @@ __device__ __forceinline__ int choose(Shared& s, const Weights& w, const uint64_
     double mass[3];
     sum_list(s, w, list, n, 0.0, mass);
     const uint32_t first = 2 * tid, n_count = min(lim.count, n);
-    if (tid == 0) s.mark_count[0] = s.mark_count[1] = n_count, s.mark_count[2] = 0;
+    if (tid == 0) s.mark_count[1] = 0;
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-        if (first + i + 1 == n_count) s.mark_mass[0] = mass[i + 1];
-    __syncthreads();
-    if (lim.mass_part < 1.0f) {
-        const double need = (double)lim.mass_part * (total < 0.0 ? s.mark_mass[0] : total);
-#pragma unroll
-        for (int i = 0; i < 2; ++i)   // (one place at most)
-            if (first + i < n_count && (first + i == 0 || mass[i] < need) && mass[i + 1] >= need) s.mark_count[0] = first + i + 1;
-    }
 #pragma unroll
     for (int i = 0; i < 2; ++i)
         if (first + i < n) {
+            if (first + i + 1 == n_count) s.mark_mass[0] = mass[i + 1];
             const bool here = listed_logit(list[first + i]) >= lim.least;
             const bool next = first + i + 1 < n && listed_logit(list[first + i + 1]) >= lim.least;
             if (here && !next) s.mark_count[1] = first + i + 1;
         }
     __syncthreads();
-    const uint32_t kept = min(s.mark_count[0], s.mark_count[1]);
+    uint32_t kept = n_count;
+    if (lim.mass_part < 1.0f) {
+        const double need = (double)lim.mass_part * (total < 0.0 ? s.mark_mass[0] : total);
+        Found f{kBins, 0, 0.0};
+#pragma unroll
+        for (int i = 1; i >= 0; --i)
+            if (first + i < n_count && (first + i + 1 == n_count || mass[i + 1] >= need)) f.place = first + i;
+        first_found(s, f.place < kBins, f);
+        kept = f.place + 1;
+    }
+    kept = max(1u, min(kept, s.mark_count[1]));
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-        if (first + i + 1 == kept) s.mark_mass[1] = mass[i + 1], s.mark_count[2] = first + i;
+        if (first + i + 1 == kept) s.mark_mass[1] = mass[i + 1];
     __syncthreads();
     const double need = (double)lim.u * s.mark_mass[1];
-    __syncthreads();
+    Found f{kBins, 0, 0.0};
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-        if (first + i < kept && mass[i] <= need && mass[i + 1] > need) s.mark_count[2] = first + i;
-    __syncthreads();
-    return (int)(uint32_t)list[s.mark_count[2]];
+    for (int i = 1; i >= 0; --i)
+        if (first + i < kept && (first + i + 1 == kept || mass[i + 1] > need)) f.place = first + i;
+    first_found(s, f.place < kBins, f);
+    return (int)(uint32_t)list[f.place];
 }
 
 // Of a row with infinite logits those weigh the same, and all others nothing.
@@ -784,7 +799,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
                 bool in_end[3];
 #pragma unroll
                 for (int i = 0; i < 3; ++i) in_end[i] = first + i >= listed || w.bin_of(listed_logit(list[first + i])) > b_high;
-                if (threadIdx.x == 0) s.mark_mass[0] = m_low, s.found_index = -1;
+                if (threadIdx.x == 0) s.mark_mass[0] = m_low;
                 __syncthreads();
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
@@ -792,23 +807,23 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
                 __syncthreads();
                 const double moved = m_end - s.mark_mass[0];
                 double before[2], after[2];
+                Found f{kBins, 0, 0.0};
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                for (int i = 1; i >= 0; --i) {
                     before[i] = sums[i] + (in_end[i] ? moved : 0.0), after[i] = sums[i + 1] + (in_end[i] ? moved : 0.0);
-                    if (first + i < listed && before[i] < need && (after[i] >= need || first + i + 1 == listed)) s.found_place = first + i, s.found_mass = after[i];
+                    if (first + i < listed && (first + i + 1 == listed || after[i] >= need)) f = Found{first + i, 0, after[i]};
                 }
-                __syncthreads();
-                const uint32_t last_kept = s.found_place;
-                const double aim = (double)lim.u * s.found_mass;
+                first_found(s, f.place < kBins, f);
+                const uint32_t last_kept = f.place;
+                const double aim = (double)lim.u * f.mass;
+                f.place = kBins;
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    if (first + i < listed && before[i] <= aim && after[i] > aim && first + i <= last_kept) s.found_index = (int)(uint32_t)list[first + i];
-                __syncthreads();
-                if (s.found_index >= 0) {
-                    if (threadIdx.x == 0) a.tokens[r] = s.found_index;
+                for (int i = 1; i >= 0; --i)   // (what lies between the two groups is not listed)
+                    if (first + i < listed && first + i <= last_kept && after[i] > aim && (!in_end[i] || before[i] <= aim)) f.place = first + i;
+                if (first_found(s, f.place < kBins, f)) {
+                    if (threadIdx.x == 0) a.tokens[r] = (int)(uint32_t)list[f.place];
                     return;
                 }
-                __syncthreads();
             }
         }
     }
