@@ -651,7 +651,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     }
     Limits lim;
     lim.count = top_k > 0 && top_k < n ? top_k : 0xFFFFFFFFu;
-    if (top_p <= 0.0f) lim.count = 1;
+    if (top_p <= 0.0f || min_p > 1.0f) lim.count = 1;   // (no token reaches either: one at least is kept)
     lim.mass_part = top_p > 0.0f && top_p < 1.0f ? top_p : 1.0f;
     lim.u = fminf(fmaxf(u, 0.0f), 0x1.fffffep-1f);
     lim.least = -INFINITY;
