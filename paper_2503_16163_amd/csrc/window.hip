@@ -17,6 +17,7 @@
 #include "operators.h"
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 
 namespace specache {
@@ -31,7 +32,8 @@ typedef _Float16 half8v __attribute__((ext_vector_type(8)));
 
 constexpr int kWaveRows = 32;
 constexpr int kRowBytes16 = kD * 2;   // a position's keys, or its values
-constexpr float kNever = -1e30f;      // a maximum below every score: nothing seen yet
+constexpr float kNever = -FLT_MAX;    // a maximum that no finite score is below: nothing seen yet
+constexpr float kFar = 0x1p20f;       // of maxima beyond it, products are rounded before the maximum is taken off
 constexpr float kLazy = 8.0f;         // the maximum moves when a score exceeds it by more than this (in powers of two)
 constexpr float kLog2e = 1.44269504088896340736f;
 
@@ -131,6 +133,9 @@ __device__ __forceinline__ bool drop_odd_values(char* values, int part, int lane
     return dropped;
 }
 
+// What a row's sums are divided by.  No weight at all: a row that sees nothing gives zeros; one that sees scores of -infinity alone has no softmax.
+__device__ __forceinline__ float divisor_of(float l, bool sees) { return l != 0.0f ? 1.0f / l : sees ? NAN : 0.0f; }
+
 // What a row of queries sees: positions up to `last`, of these the sinks and those from `low` on.
 struct Seen {
     int last, low, sinks;
@@ -162,11 +167,13 @@ struct Rows {
     uint4v q[8];
     float16v s[BLOCKS], o[4];
     float m, l;                       // l: of this lane's half of the positions
+    float by, less;                   // a weight is 2^(score by - less)
+    bool far, any_far;                // the row's maximum is beyond kFar; some row's of the wave
     uint4v p[2 * BLOCKS];
     Seen seen;
     int lane, half;
 
-    __device__ __forceinline__ void start(const uint16_t* row, int lane_) {
+    __device__ __forceinline__ void start(const uint16_t* row, int lane_, float scale) {
         lane = lane_, half = lane / 32;
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk) q[kk] = *(const uint4v*)(row + 16 * kk + 8 * half);
@@ -174,7 +181,7 @@ struct Rows {
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[dt][i] = 0.0f;
-        m = kNever, l = 0.0f;
+        m = kNever, l = 0.0f, by = scale, less = 0.0f, far = any_far = false;
     }
     __device__ __forceinline__ void scores(const char* keys) {
 #pragma unroll
@@ -197,26 +204,34 @@ struct Rows {
             if (i % 2) __builtin_amdgcn_sched_barrier(0);   // few conditions at a time: they live in scalar registers
         }
     }
-    // The maximum moves rarely, so that the sums do: weights up to 2^kLazy of a row's own maximum keep all their bits.
+    // The maximum moves rarely, so that the sums do (each row's by its own scores alone): weights up to 2^kLazy of a row's own maximum keep all their bits.
+    // A weight's exponent is the exact product of score and scale less the rounded one that the maximum is: half a step of the maximum is a factor of all of a
+    // row's weights, which does not count while the maximum is small; of one beyond kFar the products are rounded as the maximum was.
     __device__ __forceinline__ void move_maximum(float scale) {
         float most = s[0][0];
 #pragma unroll
         for (int i = 1; i < 16 * BLOCKS; ++i) most = fmaxf(most, s[i / 16][i % 16]);
         most = fmaxf(most, other_half(most)) * scale;
         if (__ballot(most > m + kLazy)) {
-            const float to = fmaxf(m, most), factor = __builtin_amdgcn_exp2f(m - to);
+            const float to = most > m + kLazy ? most : m, factor = __builtin_amdgcn_exp2f(m - to);
             m = to;
             l *= factor;
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[dt][i] *= factor;
+            far = fabsf(m) > kFar && m != kNever;
+            any_far = __ballot(far);
+            by = far ? 1.0f : scale, less = far || m == kNever ? 0.0f : m;
         }
+        if (any_far)
+#pragma unroll
+            for (int i = 0; i < 16 * BLOCKS; ++i) s[i / 16][i % 16] = far ? s[i / 16][i % 16] * scale - m : s[i / 16][i % 16];
     }
-    __device__ __forceinline__ void weights(float scale) {
+    __device__ __forceinline__ void weights() {
 #pragma unroll
         for (int i = 0; i < 16 * BLOCKS; i += 2) {
-            const float x = __builtin_amdgcn_exp2f(fmaf(s[i / 16][i % 16], scale, -m)), y = __builtin_amdgcn_exp2f(fmaf(s[i / 16][i % 16 + 1], scale, -m));
+            const float x = __builtin_amdgcn_exp2f(fmaf(s[i / 16][i % 16], by, -less)), y = __builtin_amdgcn_exp2f(fmaf(s[i / 16][i % 16 + 1], by, -less));
             l += x;
             l += y;
             p[i / 8][i % 8 / 2] = pack16<BF16>(x, y);
@@ -253,7 +268,7 @@ struct Rows {
                 }
     }
     __device__ __forceinline__ void store(uint16_t* to) {
-        const float by = l == 0.0f ? 0.0f : 1.0f / l;
+        const float by = divisor_of(l, seen.last >= 0);
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
@@ -323,7 +338,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tile_kernel(WindowArgs a) {
 
     Rows<BF16, TILE / 32> rs;
     rs.seen = Seen{N - n + token, a.window ? N - n + token - a.window + 1 : 0, a.sinks};
-    rs.start((const uint16_t*)a.q.data + b * a.q.batch + q_head * a.q.head + token * a.q.token, lane);
+    rs.start((const uint16_t*)a.q.data + b * a.q.batch + q_head * a.q.head + token * a.q.token, lane, a.scale);
     const Fetch<true, FETCHES> fetch_keys(a.k, b, h, wave, lane);
     const Fetch<false, FETCHES> fetch_values(a.v, b, h, wave, lane);
 
@@ -355,7 +370,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tile_kernel(WindowArgs a) {
         __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
         if (is_edge<TILE>(tile0, wave_first, wave_last, a.window, a.sinks)) rs.mask(tile0);
         rs.move_maximum(a.scale);
-        rs.weights(a.scale);
+        rs.weights();
         rs.add_values(values);
         // the first step's weights, then the others' beside the products
         __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
@@ -426,7 +441,7 @@ __global__ __launch_bounds__(64 * WAVES) void step_kernel(WindowArgs a) {
         fetch_keys(walk.position(i_first), TILE, N - 1, keys_even + wave * BYTES);
         fetch_values(walk.position(i_first), TILE, N - 1, values_even + wave * BYTES);
     }
-    rs.start((const uint16_t*)a.q.data + b * a.q.batch + q_head * a.q.head + token * a.q.token, lane);
+    rs.start((const uint16_t*)a.q.data + b * a.q.batch + q_head * a.q.head + token * a.q.token, lane, a.scale);
     const auto step = [&](int it, char* keys, char* values, char* next_keys, char* next_values) __attribute__((always_inline)) {
         const int tile0 = walk.position(it);
         const bool more = it + WAVES < i_end;
@@ -444,7 +459,7 @@ __global__ __launch_bounds__(64 * WAVES) void step_kernel(WindowArgs a) {
         const bool edge = is_edge<TILE>(tile0, first, last, a.window, a.sinks);
         if (edge) rs.mask(tile0);
         rs.move_maximum(a.scale);
-        rs.weights(a.scale);
+        rs.weights();
         asm volatile("" ::: "memory");
         if (more) __builtin_amdgcn_s_waitcnt(0x4F70);   // vmcnt(16): and its values
         else __builtin_amdgcn_s_waitcnt(0x0F70);
@@ -496,7 +511,7 @@ __global__ __launch_bounds__(64 * WAVES) void step_kernel(WindowArgs a) {
             if (c == 0) *(float2*)(a.part_ml + 2 * place) = float2{m, l};
             *(float4*)(a.part_o + place * kD + c) = o;
         } else {
-            const float by = l == 0.0f ? 0.0f : 1.0f / l;
+            const float by = divisor_of(l, first + row / a.G >= 0);
             uint16_t* to = (uint16_t*)a.out.data + b * a.out.batch + (h * a.G + row % a.G) * a.out.head + row / a.G * a.out.token;
             *(uint2v*)(to + c) = uint2v{pack16<BF16>(o.x * by, o.y * by), pack16<BF16>(o.z * by, o.w * by)};
         }
@@ -566,7 +581,7 @@ __global__ __launch_bounds__(64 * kMergeWaves) void merge_kernel(WindowArgs a) {
             y = fmaf(f, o.y, y);
         }
     }
-    const float by = l == 0.0f ? 0.0f : 1.0f / l;
+    const float by = divisor_of(l, length_of(a.kv_lengths, b, a.kv_tokens) - n + r / a.G >= 0);
     uint16_t* to = (uint16_t*)a.out.data + b * a.out.batch + (h * a.G + r % a.G) * a.out.head + r / a.G * a.out.token;
     *(uint32_t*)(to + 2 * lane) = pack16<BF16>(x * by, y * by);
 }
