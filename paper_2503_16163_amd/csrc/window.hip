@@ -35,6 +35,9 @@ constexpr int kRowBytes16 = kD * 2;   // a position's keys, or its values
 constexpr float kNever = -FLT_MAX;    // a maximum that no finite score is below: nothing seen yet
 constexpr float kFar = 0x1p20f;       // of maxima beyond it, products are rounded before the maximum is taken off
 constexpr float kLazy = 8.0f;         // the maximum moves when a score exceeds it by more than this (in powers of two)
+// binary16 holds all bits of numbers down to 2^-14 only, so that its weights are taken 2^7 times: up to 2^15, and those below 2^-21 of the largest lose bits, below
+// 2^-32 all.  The factor is one of sums and weights alike.
+template <bool BF16> constexpr float kLift = BF16 ? 0.0f : 7.0f;
 constexpr float kLog2e = 1.44269504088896340736f;
 
 struct WindowArgs {
@@ -181,7 +184,7 @@ struct Rows {
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[dt][i] = 0.0f;
-        m = kNever, l = 0.0f, by = scale, less = 0.0f, far = any_far = false;
+        m = kNever, l = 0.0f, by = scale, less = -kLift<BF16>, far = any_far = false;
     }
     __device__ __forceinline__ void scores(const char* keys) {
 #pragma unroll
@@ -222,7 +225,7 @@ struct Rows {
                 for (int i = 0; i < 16; ++i) o[dt][i] *= factor;
             far = fabsf(m) > kFar && m != kNever;
             any_far = __ballot(far);
-            by = far ? 1.0f : scale, less = far || m == kNever ? 0.0f : m;
+            by = far ? 1.0f : scale, less = (far || m == kNever ? 0.0f : m) - kLift<BF16>;
         }
         if (any_far)
 #pragma unroll
