@@ -195,6 +195,8 @@ def measure_link(nbytes=256 << 20, reps=5):
 
 
 # ---- calls without a context: torch tensors, strided where the C call takes views ------------------------------------
+# Without a stream they go to torch's current one.  They have no backward pass: inputs that require gradients are read like any others, and
+# the outputs carry none.
 
 def _done(rc):
     if rc != OK:
@@ -220,6 +222,10 @@ def _with_torch():
 
 def _here():
     return _with_torch().cuda.current_device()
+
+
+def _current(stream):
+    return _torch.cuda.current_stream().cuda_stream if stream is None else _stream(stream)
 
 
 def _type_of(t):
@@ -300,7 +306,7 @@ def rotate(plan, q, q_out, k=None, k_out=None, v=None, v_out=None, positions=Non
                (shape, shape, kv_shape, kv_shape, kv_shape, kv_shape))
     _done(lib().specache_rotate(C.byref(plan), _type_of(q), B, n, Hq, a[0], a[1], 0 if kv is None else kv_shape[1],
                                 None if k is None else a[2], None if k is None else a[3], None if v is None else a[4], None if v is None else a[5],
-                                _flat(positions, (B, n), _torch.int32, device, "positions"), first_position, _stream(stream)))
+                                _flat(positions, (B, n), _torch.int32, device, "positions"), first_position, _current(stream)))
 
 
 def window_scratch(batch, n_q_heads, n_kv_heads, q_tokens, kv_tokens, window=0, sinks=0):
@@ -322,7 +328,7 @@ def window_attend(q, k, v, out, window=0, sinks=0, q_lengths=None, kv_lengths=No
     cfg = WindowConfig(B, Hq, pairs[1], D, n, pairs[2], window, sinks, _type_of(q), sm_scale)
     address, size = _scratch(scratch, device)
     _done(lib().specache_window_attend(C.byref(cfg), a[0], a[1], a[2], a[3], _flat(q_lengths, (B,), _torch.int32, device, "q_lengths"),
-                                       _flat(kv_lengths, (B,), _torch.int32, device, "kv_lengths"), address, size, _stream(stream)))
+                                       _flat(kv_lengths, (B,), _torch.int32, device, "kv_lengths"), address, size, _current(stream)))
 
 
 def sample_scratch(rows, vocab, dtype):
@@ -347,7 +353,7 @@ def sample(logits, u, tokens, temperature=None, top_k=None, top_p=None, min_p=No
     _done(lib().specache_sample(C.byref(cfg), logits.data_ptr(), _flat(u, shape, f32, device, "u"),
                                 _flat(temperature, shape, f32, device, "temperature"), _flat(top_k, shape, i32, device, "top_k"),
                                 _flat(top_p, shape, f32, device, "top_p"), _flat(min_p, shape, f32, device, "min_p"),
-                                _flat(tokens, shape, i32, device, "tokens"), address, size, _stream(stream)))
+                                _flat(tokens, shape, i32, device, "tokens"), address, size, _current(stream)))
 
 
 class SpeCache:
