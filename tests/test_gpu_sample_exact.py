@@ -88,3 +88,18 @@ def test_logits_and_temperatures_over_the_whole_range():
     for t in (2.0 ** -22, 2.0 ** -12, 1.0e-3):
         for k, p, m in ((0, 1.0, 0.0), (100, 0.9, 0.0), (0, 0.97, 0.0), (2500, 0.99, 0.0)):
             _check(x, t, k, p, m, rng.random(256, dtype=np.float32))
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [3, 2000, 40000])
+def test_rows_of_the_lowest_number(V, dtype):
+    """Masked by the type's lowest number instead of -infinity: it is a logit like others, beside larger ones of no weight, alone of equal weight."""
+    rng = np.random.default_rng(V)
+    u = rng.random(64, dtype=np.float32)
+    x = torch.full((V,), torch.finfo(dtype).min, dtype=dtype, device="cuda")
+    for k, p, m in ((0, 1.0, 0.0), (2, 1.0, 0.0), (300, 0.5, 0.0), (0, 0.7, 0.5), (1900, 0.9, 1.0)):
+        _check(x, 1.0, k, p, m, u)
+    x[V // 2] = -5.0
+    x[V // 3] = -6.0
+    for k, p, m in ((0, 1.0, 0.0), (1, 1.0, 0.0), (300, 0.5, 0.0), (0, 0.9, 0.1), (1900, 0.99, 0.0)):
+        _check(x, 1.0, k, p, m, u)
