@@ -534,7 +534,7 @@ int specache_window_scratch(const specache_window_config* cfg, int64_t* bytes);
  * NULL: q_tokens and kv_tokens.  Rows of q and out from n on and rows of k and v from N on are neither read nor written.
  * Scores, softmax and sums are binary32; the weights are rounded to dtype for their product with v (in binary16 those below 2^-21 of a row's largest
  * keep fewer bits, those below 2^-32 none), the output once.  A value
- * that is not finite reaches the rows that see it and no others.  Without `window` and `sinks` this is a prompt's causal
+ * that is not finite reaches the rows that see it and no others; a row that sees scores of -infinity alone is NaN.  Without `window` and `sinks` this is a prompt's causal
  * attention, with q_tokens = 1 or 2 a step's.  Results do not depend on what else runs, and are the same every time.
  * scratch: device, 16-byte aligned, scratch_bytes >= specache_window_scratch; written before it is read.  Calls that may
  * overlap need scratch memory of their own.  NULL where the size is 0.

@@ -32,8 +32,8 @@ constexpr int kList = 2048;            // elements that are sorted at once
 constexpr int kFew = 256;              // a list so short is sorted by comparing each with all the others,
 constexpr int kRanked = 1024;          // of a bin's so many each is compared with all the others
 constexpr int kTable = 32768;          // vectors of a row whose largest logits are kept (32 of each thread)
-// top_k by the threads' largest logits, by the vectors': us, 256 rows of 128256 / 17 of 49999 in fp32, top_k 100 by the one 22.3 / 13.0, by the other 23.8 / 14.4;
-// 200 24.6 / 15.7 and 25.7 / 16.3; 400 25.9 / 15.7 by the vectors', 1400 36 / 20.
+// top_k by the threads' largest logits, by the vectors': us, 256 rows of 128256 / 17 of 49999 in fp32, top_k 100 by the one 23.3 / 15.1, by the other 24.9 / 16.2;
+// 200 25.5 / 17.3 and 26.3 / 18.0; 400 26.6 / 18.1 by either, 1400 36.8 / 21.9 by the vectors'.
 constexpr int kFewMaxima = 256, kMostByMaxima = 1536;
 constexpr int kMostVocab = 1 << 20;
 constexpr double kRounder = 0x1.8p52;  // added to a number below 2^31: the sum's lower word is its nearest whole number
@@ -346,8 +346,8 @@ __device__ __forceinline__ void list_one(Shared& s, float l, int i) {
 __device__ __forceinline__ float listed_logit(uint64_t x) { return logit_of_key((uint32_t)(x >> 32)); }
 
 // The listed elements (n of them, at most kList), sorted: few are compared with each other, more put to their bins' places and there compared
-// with their bin's others; where a bin holds very many, by exchanges (66 steps for 2048).  us, a row of 32000 by exchanges / so: top_k 1000 33 / 25, top_p 0.9 29 /
-// 22; 50 by their bins' places 11.9, compared with each other 11.
+// with their bin's others; where a bin holds very many, by exchanges (66 steps for 2048).  us, two rows of 32000 by exchanges / so: top_k 1000 31.1 / 17.9, top_p 0.9 26.4 /
+// 20.0; 50 by their bins' places 12.7, compared with each other 11.5, 200 (longer lists) 14.5 and 15.5.
 __device__ __forceinline__ const uint64_t* sort_list(Shared& s, const Weights& w, uint32_t n) {
     const uint32_t tid = thread();
     if (n <= kFew) {
@@ -600,11 +600,11 @@ __device__ __forceinline__ int choose_infinite(Shared& s, const T* row, int n, c
     return index_of_place(s, n, (uint32_t)((double)lim.u * kept) + 1, [&](int i) { return infinite(logit_of(row[i])); });
 }
 
-// A workgroup per row: it reads the row once for its largest logits (256 rows of 128256 in bfloat16, 66 MB: greedy choices take 14.1 us, where the bytes need
-// 11), and again what it cannot leave out.  The same rows with top_k 50 21.4 us (of the second reading only the vectors whose largest logit
-// counts), 1000 31.7, without a limit 58.8, top_p 0.9 55.7, at a temperature of 0.7 49.5: the histogram of a whole row, some 19 us of vector
+// A workgroup per row: it reads the row once for its largest logits (256 rows of 128256 in bfloat16, 66 MB: greedy choices take 14.0 us, where the bytes need
+// 11), and again what it cannot leave out.  The same rows with top_k 50 22.0 us (of the second reading only the vectors whose largest logit
+// counts), 1000 32.1, without a limit 59.0, top_p 0.9 57.0, at a temperature of 0.7 48.9: the histogram of a whole row, some 19 us of vector
 // instructions and LDS additions on its compute unit (16 with binary32 weights, whose sums chose another token once in some thousand draws), and a third reading.  Two rows of
-// 32000: 4.1, 11.0, 17.5, 19.2, 22.2, 19.2 us, a chain of some 20 barriers and as many exchanges.  A row to a workgroup, not to several: where every
+// 32000: 4.0, 11.2, 17.7, 19.3, 22.9, 19.3 us, a chain of some 20 barriers and as many exchanges.  A row to a workgroup, not to several: where every
 // row needs a histogram and there are as many as compute units nothing is gained, and few rows would pay a launch (3 us) for each reading.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {

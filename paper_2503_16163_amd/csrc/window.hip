@@ -307,8 +307,8 @@ __device__ __forceinline__ int on_one_xcd(int per_head) {
 }
 
 // Tiles of 64 positions travel to LDS while the one before is worked on; a wave takes 1/WAVES of a tile's keys and values.
-// us, 32 heads over a prompt of 16k tokens: 2165 (1.02 PFLOP/s, the matrix cores busy 0.52 of the time at the clock that random inputs leave), 8 heads of 4
-// queries over 32k through a window of 4096 1980 to 2040, 256 tokens of 8 heads of 8 behind 32k 253.
+// us, 32 heads over a prompt of 16k tokens: 2165 (1.02 PFLOP/s, the matrix cores busy 0.52 of the time at the clock that random inputs leave; 2130 to 2230 from one card to
+// another), 8 heads of 4 queries over 32k through a window of 4096 1950 to 2140, 256 tokens of 8 heads of 8 behind 32k 250 to 267 and the merge.
 template <bool BF16, bool SPLIT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void tile_kernel(WindowArgs a) {
     constexpr int TILE = 64, ROWS = WAVES * kWaveRows, FETCHES = 16 / WAVES;
@@ -404,7 +404,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tile_kernel(WindowArgs a) {
 }
 
 // Waves by themselves: 32 positions at a time, the next ones on their way while a wave works on these; the waves of a workgroup take a chunk's
-// tiles in turn and join their results in LDS at its end.  Memory is what bounds it, latency where a wave has few tiles (1.1 us each).  By
+// tiles in turn and join their results in LDS at its end.  Memory is what bounds it, latency where a wave has few tiles (1.0 us each: 64, 128, 192
+// and 256 positions of 32 heads without chunks take 5.4, 6.4, 7.4 and 8.4 us, the launch among them).  32 heads and two rows over 2048, 4096 and 8192 positions, not in
+// the caches, take 13.3, 19.0 and 30.0 us: 8 for two launches, their first loads and the join, and the bytes at 6 TB/s.  By
 // workgroups of 1, 2 and 4 waves, with one round of them, us (the time of reading once at 6.2 TB/s): 32 heads over 32768 positions 98, 100, 115
 // (87), 4 of 32 on 8 heads and two rows over 8192 33, 32, 32 (22), one sequence of 1 head over 100000 35, 28, 24 (8), 32 heads and two rows through a
 // window of 4096 22, 23, 23 (11); 16 ragged sequences of 8 heads up to 32768 265, 251, 262 (203), and 236 with workgroups dealt to the XCDs
@@ -617,8 +619,8 @@ int window_of(const specache_window_config& c) { return c.window < c.kv_tokens ?
 // Steps: one round of workgroups (two on a compute unit by their LDS), chunks of at most 64 tiles (2048 positions) so that a ragged batch's lengths
 // even out, a tile for every wave at least, and no more than 256 chunks of a row to merge unless they are that long.  us, by chunks: one sequence of 8
 // KV heads, 131072 positions, 64 chunks 98, 80 chunks (a second round) 116, 128 101; 16 ragged sequences of 8 heads up to 32768 positions, chunks of 64 tiles 236, of 128
-// 261; 1 head, 100000 positions, 128 chunks 28, 256 26, 512 33.  Up to 4 tiles per wave no chunks at all, as a merge is a launch more: 256
-// positions 7.8 us against 9.0 with them, 512 positions 12.0 against 9.5.
+// 261; 1 head, 100000 positions, 128 chunks 28, 256 26, 512 33.  Up to 4 tiles per wave no chunks at all, as a merge is a launch more: 192
+// positions of 32 heads 7.4 us against 8.4 with them, 256 8.4 either way, 320 9.4 against 8.8, 512 12.4 against 8.7.
 // Prompts: 8 waves to a workgroup where a row tile walks 2048 positions or more (8 waves / 4: a prompt of 16k tokens 2148 / 2225 us, through a
 // window of 4096 1974 / 2014, but ragged ones of up to 3001 tokens through 512 145 / 134, 8 prompts of 1000 tokens
 // 106 / 98: first tiles and edges are then most of a walk);
