@@ -578,6 +578,105 @@ int specache_sample(const specache_sample_config* cfg, const void* logits, const
                     const int32_t* top_k, const float* top_p, const float* min_p, int32_t* tokens, void* scratch,
                     int64_t scratch_bytes, void* stream);
 
+/*
+ * A layer's 16-bit keys and values in pages, for batches whose sequences grow and share: row (page, head, place) of k and v is element
+ * page * batch + head * head + place * token (the view's strides) of 128 channels, so that places may follow heads or heads places.
+ * table[b * table_stride + i] is the page of positions i * page_tokens .. of sequence b.  An entry outside 0 .. n_pages - 1 is no page:
+ * nothing is written to its positions, no query sees them and none of its blocks is chosen.  bounds (data NULL: not kept): rows
+ * (page, head, 0) and (page, head, 1) are the least and the largest key of the page, channel by channel.  Plain data: the calls below
+ * read it and keep nothing; pages and tables are the caller's to give out, share and take back.
+ */
+typedef struct specache_pages {
+    specache_view k, v;      /* [n_pages, n_kv_heads, page_tokens]; at most 2^20 elements from place to place */
+    specache_view bounds;    /* [n_pages, n_kv_heads, 2]                                           */
+    const int32_t* table;    /* device, [batch, table_pages]                                       */
+    int64_t table_stride;    /* elements from a sequence's row to the next, >= 0                   */
+    int32_t n_pages;         /* >= 0                                                               */
+    int32_t n_kv_heads;      /* >= 1                                                               */
+    int32_t page_tokens;     /* 16, 32, 64, 128 or 256                                             */
+    int32_t table_pages;     /* >= 0; table_pages * page_tokens up to 2^28                         */
+    int32_t head_dim;        /* must be 128                                                        */
+    int32_t dtype;           /* SPECACHE_FP16 or SPECACHE_BF16: type of k, v and bounds            */
+} specache_pages;
+
+/*
+ * Appends to a paged cache with the rotation on the way, in one launch: token t < n of sequence b goes to position starts[b] + t, its key
+ * (of k [batch, n_kv_heads, tokens]) turned by plan, its value (of v, alike) as it is; q [batch, n_q_heads, tokens] is turned into q_out, which
+ * may be q itself.  Arithmetic as in specache_rotate; plan NULL: nothing is turned.  q and q_out may be NULL with n_q_heads = 0.
+ * starts: device int32 [batch], the positions that the sequences hold already; NULL: 0.  lengths: device int32 [batch], n, held to
+ * 0 .. tokens; NULL: tokens.  Rows of q, k, v and q_out from n on are neither read nor written.  A key or value whose position has no page
+ * (or is negative, or not in the table) is not written.  positions: device int32 [batch, tokens], contiguous: what the
+ * rotation goes by; NULL: a token's position in its sequence.
+ * bounds: a page whose place 0 is among the tokens gets those of the tokens written here, any other the wider of what it has and those; a NaN is passed over.
+ * Two tokens that one call, or two that overlap, write to one page come from one sequence and one call (pages that sequences share are not appended to).
+ * batch = 0 and tokens = 0 are allowed; batch * tokens goes up to 2^30.
+ * Errors: EINVAL (null or misaligned view, counts, a plan that specache_rotary_plan did not write), EHIP.
+ */
+int specache_paged_append(const specache_pages* cache, const specache_rotary* plan, int32_t batch, int32_t tokens,
+                          int32_t n_q_heads, const specache_view* q, const specache_view* q_out, const specache_view* k,
+                          const specache_view* v, const int32_t* starts, const int32_t* lengths, const int32_t* positions,
+                          void* stream);
+
+/*
+ * Attention over a paged cache: of a sequence with n queries and N cached tokens, query row i stands at position p = N - n + i and sees the
+ * positions j <= p that have a page.  A row that sees nothing gives zeros.
+ * shared_tokens: the table's rows agree over the first shared_tokens / page_tokens pages (those of row 0 are read).  Their keys and values are then read
+ * once for all sequences, which changes the time and the rounding alone.  0: nothing is shared.
+ */
+typedef struct specache_paged_config {
+    int32_t batch;           /* >= 0                                                               */
+    int32_t n_q_heads;       /* a multiple of the cache's n_kv_heads; Hq / Hkv <= 64               */
+    int32_t q_tokens;        /* rows of q and out per sequence and head, >= 0                      */
+    int32_t kv_tokens;       /* most positions of a sequence, 0 .. table_pages * page_tokens       */
+    int32_t shared_tokens;   /* >= 0 (held to kv_tokens)                                           */
+    float sm_scale;          /* logit scale; <= 0 selects 1/sqrt(head_dim)                         */
+} specache_paged_config;
+
+/* Host only: the bytes of scratch memory that specache_paged_attend needs (0: none); it depends on the counts alone.  Errors: EINVAL. */
+int specache_paged_scratch(const specache_pages* cache, const specache_paged_config* cfg, int64_t* bytes);
+
+/*
+ * q, out: [batch, n_q_heads, q_tokens] rows of the cache's type (they may have the same view).  q_lengths, kv_lengths: device int32 [batch], n and N, held to
+ * 0 .. q_tokens and 0 .. kv_tokens; NULL: those.  Rows from n on and places from N on are neither read nor written.
+ * Numerics, values that are not finite, scratch and errors: as for specache_window_attend.
+ */
+int specache_paged_attend(const specache_pages* cache, const specache_paged_config* cfg, const specache_view* q,
+                          const specache_view* out, const int32_t* q_lengths, const int32_t* kv_lengths, void* scratch,
+                          int64_t scratch_bytes, void* stream);
+
+/*
+ * Sparse attention over a paged cache: a block is a page's positions, and every (query row, KV head) sees the blocks of a list of its own.
+ *
+ * specache_block_select makes the lists by a cheap score, from the cache's bounds.  For row i at position p (as above) the candidates are the blocks
+ * c <= p / page_tokens that have a page.  Listed are of these c < first, c > p / page_tokens - recent, and the `top` others of the largest
+ *   score(c) = max over the KV head's query heads of  sum over channels of  max(q, 0) * bounds[1] + min(q, 0) * bounds[0],
+ * which no q . k of the block exceeds; the lower block first among equals.  Products and sums have 64 bits, so that the choice is the definition's; a
+ * sum that is NaN counts as -infinity.
+ * specache_block_attend: as specache_paged_attend, but a row sees the positions j <= p of its listed blocks alone.  An entry
+ * that is negative or no block of the sequence's N tokens is passed over; one that is listed twice counts twice.
+ */
+typedef struct specache_block_config {
+    int32_t batch, n_q_heads, q_tokens, kv_tokens;   /* as in specache_paged_config                */
+    int32_t top;             /* >= 0                                                               */
+    int32_t first;           /* >= 0                                                               */
+    int32_t recent;          /* >= 0; first + top + recent from 1 to 2^20: the entries of a list   */
+    float sm_scale;          /* specache_block_attend's; <= 0 selects 1/sqrt(head_dim)             */
+} specache_block_config;
+
+/* Host only: the bytes of scratch memory that either call needs (0: none).  Errors: EINVAL. */
+int specache_block_scratch(const specache_pages* cache, const specache_block_config* cfg, int64_t* bytes);
+
+/*
+ * blocks: device int32 [batch, n_kv_heads, q_tokens, first + top + recent], contiguous: a row's list in ascending order, then -1.  Rows from n on are neither
+ * read nor written.  The cache needs bounds here, in specache_block_attend only k and v.
+ * Errors: EINVAL (null or misaligned view, configuration, scratch), ECAPACITY (scratch too small; nothing is launched), EHIP.
+ */
+int specache_block_select(const specache_pages* cache, const specache_block_config* cfg, const specache_view* q, int32_t* blocks,
+                          const int32_t* q_lengths, const int32_t* kv_lengths, void* scratch, int64_t scratch_bytes, void* stream);
+int specache_block_attend(const specache_pages* cache, const specache_block_config* cfg, const specache_view* q,
+                          const specache_view* out, const int32_t* blocks, const int32_t* q_lengths, const int32_t* kv_lengths,
+                          void* scratch, int64_t scratch_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

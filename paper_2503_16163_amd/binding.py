@@ -23,7 +23,9 @@ EXPORTS = ["specache_create", "specache_destroy", "specache_last_error", "specac
            "specache_attend", "specache_score_attend", "specache_append_score_attend", "specache_decode_step", "specache_attend_static", "specache_debug_poison_slot", "specache_debug_fail_alloc", "specache_debug_scored_by_word", "specache_order_by_events", "specache_debug_kernel_choice", "specache_debug_merger_polls", "specache_export_quantized", "specache_export_rows", "specache_debug_logits",
            "specache_timing", "specache_measure_hbm_read", "specache_measure_link",
            "specache_rotary_plan", "specache_rotate", "specache_window_scratch", "specache_window_attend",
-           "specache_sample_scratch", "specache_sample"]
+           "specache_sample_scratch", "specache_sample",
+           "specache_paged_append", "specache_paged_scratch", "specache_paged_attend",
+           "specache_block_scratch", "specache_block_select", "specache_block_attend"]
 
 
 class Config(C.Structure):
@@ -58,6 +60,19 @@ class WindowConfig(C.Structure):
 
 class SampleConfig(C.Structure):
     _fields_ = [("rows", C.c_int32), ("vocab", C.c_int32), ("dtype", C.c_int32), ("row_stride", C.c_int64)]
+
+
+class PagesConfig(C.Structure):
+    _fields_ = [("k", View), ("v", View), ("bounds", View), ("table", C.c_void_p), ("table_stride", C.c_int64)] + \
+               [(n, C.c_int32) for n in ("n_pages", "n_kv_heads", "page_tokens", "table_pages", "head_dim", "dtype")]
+
+
+class PagedConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "n_q_heads", "q_tokens", "kv_tokens", "shared_tokens")] + [("sm_scale", C.c_float)]
+
+
+class BlockConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "n_q_heads", "q_tokens", "kv_tokens", "top", "first", "recent")] + [("sm_scale", C.c_float)]
 
 
 class SpeCacheError(RuntimeError):
@@ -118,6 +133,13 @@ def lib():
         L.specache_window_attend.argtypes = [C.POINTER(WindowConfig), view, view, view, view, vp, vp, vp, i64, vp]
         L.specache_sample_scratch.argtypes = [C.POINTER(SampleConfig), C.POINTER(i64)]
         L.specache_sample.argtypes = [C.POINTER(SampleConfig), vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+        pages = C.POINTER(PagesConfig)
+        L.specache_paged_append.argtypes = [pages, C.POINTER(Rotary), i32, i32, i32, view, view, view, view, vp, vp, vp, vp]
+        L.specache_paged_scratch.argtypes = [pages, C.POINTER(PagedConfig), C.POINTER(i64)]
+        L.specache_paged_attend.argtypes = [pages, C.POINTER(PagedConfig), view, view, vp, vp, vp, i64, vp]
+        L.specache_block_scratch.argtypes = [pages, C.POINTER(BlockConfig), C.POINTER(i64)]
+        L.specache_block_select.argtypes = [pages, C.POINTER(BlockConfig), view, vp, vp, vp, vp, i64, vp]
+        L.specache_block_attend.argtypes = [pages, C.POINTER(BlockConfig), view, view, vp, vp, vp, vp, i64, vp]
         for name in EXPORTS:
             if name != "specache_last_error":
                 getattr(L, name).restype = C.c_int
@@ -243,7 +265,7 @@ class _Views(threading.local):
 
 
 _room = _Views()
-_PACK = {n: struct.Struct(f"{4 * n}q").pack_into for n in (4, 6)}
+_PACK = {n: struct.Struct(f"{4 * n}q").pack_into for n in (1, 2, 3, 4, 6)}
 
 
 def _views(device, dtype, names, tensors, shapes):
@@ -354,6 +376,100 @@ def sample(logits, u, tokens, temperature=None, top_k=None, top_p=None, min_p=No
                                 _flat(temperature, shape, f32, device, "temperature"), _flat(top_k, shape, i32, device, "top_k"),
                                 _flat(top_p, shape, f32, device, "top_p"), _flat(min_p, shape, f32, device, "min_p"),
                                 _flat(tokens, shape, i32, device, "tokens"), address, size, _current(stream)))
+
+
+class Pages:
+    """A layer's paged cache for the calls below: k, v [pages, Hkv, page_tokens, 128] and bounds [pages, Hkv, 2, 128] (views as they are), table [B, table_pages]
+    int32 (a row's entries side by side).  It keeps the tensors; what is in them may change between calls."""
+
+    def __init__(self, k, v, table, bounds=None):
+        self.device, self.kind, self.k, self.v, self.table, self.bounds = _here(), k.dtype, k, v, table, bounds
+        if k.dim() != 4 or k.shape[3] != 128 or _type_of(k) not in (FP16, BF16):
+            _refuse("k must be a [pages, KV heads, page_tokens, 128] tensor of a 16-bit type")
+        P, H, T, _ = k.shape
+        views = _views(self.device, k.dtype, ("k", "v", "bounds"), (k, v, bounds), (k.shape, k.shape, (P, H, 2, 128)))
+        if table.dim() != 2 or table.dtype is not _torch.int32 or table.get_device() != self.device or (table.shape[1] > 1 and table.stride(1) != 1):
+            _refuse("table must be a [batch, pages] tensor of int32 on the current device, a row's entries side by side")
+        self.batch, self.places = table.shape[0], table.shape[1] * T
+        self.config = PagesConfig(*(View.from_address(at) for at in views[:3]), table.data_ptr(), table.stride(0) if table.shape[0] > 1 else table.shape[1],
+                                  P, H, T, table.shape[1], 128, _type_of(k))
+        self.at = C.byref(self.config)
+
+    def _take(self, q, *others):
+        """Addresses of q's and the others' views, which have q's shape [B, Hq, n, 128]; and the counts."""
+        shape, device = q.shape, _here()
+        if device != self.device:
+            _refuse("the cache is not on the current device")
+        if len(shape) != 4 or shape[3] != 128 or shape[0] != self.batch:
+            _refuse("q is [B, Hq, n, 128], with as many sequences as the table has")
+        tensors = (q,) + others
+        return device, shape, _views(device, self.kind, ("q", "out")[:len(tensors)], tensors, (shape,) * len(tensors))
+
+
+def paged_append(cache, plan, k, v, q=None, q_out=None, starts=None, lengths=None, positions=None, stream=None):
+    """k, v [B, Hkv, n, 128] to positions starts[b] .. of the cache, k turned by plan (None: as it is); q [B, Hq, n, 128] turned into q_out."""
+    B, _, n, _ = k.shape
+    H = cache.config.n_kv_heads
+    device = _here()
+    if device != cache.device or B != cache.batch:
+        _refuse("the cache is not on the current device, or has other sequences")
+    if (q is None) != (q_out is None):
+        _refuse("a tensor and its output are given or left out together")
+    heads = 0 if q is None else q.shape[1]
+    a = _views(device, cache.kind, ("q", "q_out", "k", "v"), (q, q_out, k, v), ((B, heads, n, 128), (B, heads, n, 128), (B, H, n, 128), (B, H, n, 128)))
+    i32 = _torch.int32
+    _done(lib().specache_paged_append(cache.at, None if plan is None else C.byref(plan), B, n, heads, a[0], a[1], a[2], a[3],
+                                      _flat(starts, (B,), i32, device, "starts"), _flat(lengths, (B,), i32, device, "lengths"),
+                                      _flat(positions, (B, n), i32, device, "positions"), _current(stream)))
+
+
+def paged_scratch(cache, batch, n_q_heads, q_tokens, kv_tokens, shared_tokens=0):
+    """Bytes of scratch memory that paged_attend needs for these counts (0: none)."""
+    out = C.c_int64()
+    _done(lib().specache_paged_scratch(cache.at, C.byref(PagedConfig(batch, n_q_heads, q_tokens, kv_tokens, shared_tokens)), C.byref(out)))
+    return out.value
+
+
+def paged_attend(cache, q, out, kv_tokens=None, shared_tokens=0, q_lengths=None, kv_lengths=None, sm_scale=0.0, scratch=None, stream=None):
+    """Attention of q [B, Hq, n, 128] over the cache's positions (kv_tokens at most; None: what the table holds), whose first shared_tokens the sequences
+    share, into out (q's shape)."""
+    device, (B, Hq, n, _), a = cache._take(q, out)
+    cfg = PagedConfig(B, Hq, n, cache.places if kv_tokens is None else kv_tokens, shared_tokens, sm_scale)
+    address, size = _scratch(scratch, device)
+    _done(lib().specache_paged_attend(cache.at, C.byref(cfg), a[0], a[1], _flat(q_lengths, (B,), _torch.int32, device, "q_lengths"),
+                                      _flat(kv_lengths, (B,), _torch.int32, device, "kv_lengths"), address, size, _current(stream)))
+
+
+def block_scratch(cache, batch, n_q_heads, q_tokens, kv_tokens, top, first=0, recent=0):
+    """Bytes of scratch memory that block_select and block_attend need for these counts (0: none)."""
+    out = C.c_int64()
+    _done(lib().specache_block_scratch(cache.at, C.byref(BlockConfig(batch, n_q_heads, q_tokens, kv_tokens, top, first, recent)), C.byref(out)))
+    return out.value
+
+
+def block_select(cache, q, blocks, kv_tokens=None, top=0, first=0, recent=0, q_lengths=None, kv_lengths=None, scratch=None, stream=None):
+    """blocks [B, Hkv, n, first + top + recent] of int32: the blocks of the cache (its pages) that the rows of q [B, Hq, n, 128] see."""
+    device, (B, Hq, n, _), a = cache._take(q)
+    cfg = BlockConfig(B, Hq, n, cache.places if kv_tokens is None else kv_tokens, top, first, recent)
+    address, size = _scratch(scratch, device)
+    lists = _flat(blocks, (B, cache.config.n_kv_heads, n, first + top + recent), _torch.int32, device, "blocks")
+    if cache.bounds is None and top > 0:
+        _refuse("the cache keeps no bounds")
+    _done(lib().specache_block_select(cache.at, C.byref(cfg), a[0], lists, _flat(q_lengths, (B,), _torch.int32, device, "q_lengths"),
+                                      _flat(kv_lengths, (B,), _torch.int32, device, "kv_lengths"), address, size, _current(stream)))
+
+
+def block_attend(cache, q, out, blocks, kv_tokens=None, q_lengths=None, kv_lengths=None, sm_scale=0.0, scratch=None, stream=None):
+    """Attention of q [B, Hq, n, 128] over the listed blocks [B, Hkv, n, entries] of the cache, into out (q's shape)."""
+    device, (B, Hq, n, _), a = cache._take(q, out)
+    if blocks.dim() != 4:
+        _refuse("blocks is [B, Hkv, n, entries]")
+    slots = blocks.shape[3]
+    cfg = BlockConfig(B, Hq, n, cache.places if kv_tokens is None else kv_tokens, slots, 0, 0, sm_scale)
+    address, size = _scratch(scratch, device)
+    lists = _flat(blocks, (B, cache.config.n_kv_heads, n, slots), _torch.int32, device, "blocks")
+    _done(lib().specache_block_attend(cache.at, C.byref(cfg), a[0], a[1], lists, _flat(q_lengths, (B,), _torch.int32, device, "q_lengths"),
+                                      _flat(kv_lengths, (B,), _torch.int32, device, "kv_lengths"), address, size, _current(stream)))
 
 
 class SpeCache:

@@ -37,6 +37,9 @@ typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef __bf16 bfloat2v __attribute__((ext_vector_type(2)));
 typedef float float2v __attribute__((ext_vector_type(2)));
 
+// a sequence's length, held to 0 .. most (NULL: most)
+__device__ __forceinline__ int length_of(const int32_t* lengths, int b, int most) { return lengths ? min(max(lengths[b], 0), most) : most; }
+
 // two binary32 numbers as two 16-bit ones, each rounded to the nearest (even)
 template <bool BF16>
 __device__ __forceinline__ uint32_t pack16(float lo, float hi) {

@@ -1,0 +1,808 @@
+// Attention over 16-bit keys and values in pages: of a batch whose sequences share a prefix, and over listed blocks.
+//
+// Rows, tiles and softmax are those of rows16.h; what differs from contiguous keys is where a tile's positions are.  A tile is made of granules of 16
+// positions, each inside a page.  The lanes of a wave look up the pages of its next 64 granules at once (entries of the table, and of the list where there
+// is one) and a tile takes its own from there, so that the two dependent reads are paid once for 32 tiles and not for each.
+//
+// A prefix that all sequences share is work of its own: its rows are those of all sequences together, so its keys and values are read once for as many
+// rows as a workgroup holds.  Its partial results, and those of the sequences' own positions, are joined by merge_kernel.
+#include "pages.h"
+#include "rows16.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace specache {
+namespace {
+
+constexpr int kHidden = 1 << 30;      // position of a granule that nobody sees
+
+struct PagedArgs {
+    specache_view q, out;
+    PageArgs pages;
+    const int32_t* q_lengths;
+    const int32_t* kv_lengths;
+    const int32_t* blocks;            // [batch][KV head][token][slots]
+    float* own_o;                     // [unit][row tile][chunk][row][kD], not divided by the sum; a unit is a KV head of a sequence (of a token of it)
+    float* own_ml;                    // [unit][row tile][chunk][row][2]: maximum (in powers of two; -infinity where nothing is seen), sum
+    float* prefix_o;                  // [KV head][row tile][chunk][row][kD]
+    float* prefix_ml;
+    int batch, G, q_tokens, kv_tokens, slots;
+    int shared;                       // positions of the prefix, whole pages
+    int prefix_groups;                // the first workgroups of a launch work on the prefix
+    int own_chunks, own_row_tiles, own_rows, prefix_chunks, prefix_row_tiles, prefix_rows;
+    int parts;                        // results go to the merge
+    int merge_rows;
+    float scale;                      // sm_scale in powers of two
+};
+
+// What a workgroup works on: rows row0 .. row0 + rows - 1 of a unit or of the prefix, positions begin .. end - 1 or a list's.
+struct Job {
+    bool prefix;
+    int b, h, token, row0, rows, n, N, begin, end, tiles, i_begin, i_end;
+    int64_t place;                    // of its first row's partial results
+};
+
+// A lane's row of it.
+struct Row {
+    int b, token, head, last;         // last: the last position seen
+};
+
+template <bool LISTED>
+__device__ __forceinline__ Row row_of(const PagedArgs& a, const Job& j, int i) {
+    const int r = j.row0 + min(i, j.rows - 1);
+    Row o;
+    if (!LISTED && j.prefix) {
+        o.b = r / (a.q_tokens * a.G);
+        const int rest = r - o.b * (a.q_tokens * a.G), n = length_of(a.q_lengths, o.b, a.q_tokens), N = length_of(a.kv_lengths, o.b, a.kv_tokens);
+        o.token = rest / a.G;
+        o.head = j.h * a.G + rest - o.token * a.G;
+        o.last = o.token < n ? min(N - n + o.token, j.end - 1) : j.end - 1;   // (of rows that there are not nothing is kept)
+        o.token = min(o.token, max(n - 1, 0));
+    } else {
+        o.b = j.b;
+        o.token = LISTED ? j.token : r / a.G;
+        o.head = j.h * a.G + r % a.G;
+        o.last = j.N - j.n + o.token;
+    }
+    return o;
+}
+
+// Which work the workgroup has; false: none.
+template <bool LISTED, int TILE, int ROWS>
+__device__ __forceinline__ bool job_of(const PagedArgs& a, Job& j) {
+    int chunk, chunks;
+    j.prefix = !LISTED && (int)blockIdx.x < a.prefix_groups;
+    j.token = 0;
+    if (j.prefix) {
+        const int id = blockIdx.x, tile = id % a.prefix_row_tiles;
+        chunks = a.prefix_chunks;
+        chunk = id / a.prefix_row_tiles % chunks;
+        j.h = id / a.prefix_row_tiles / chunks;
+        j.b = 0;
+        j.row0 = tile * ROWS;
+        j.rows = min(ROWS, a.batch * a.q_tokens * a.G - j.row0);
+        j.n = j.N = 0;
+        j.begin = 0;
+        j.end = a.shared;
+        j.tiles = (j.end + TILE - 1) / TILE;
+        j.place = (((int64_t)j.h * a.prefix_row_tiles + tile) * chunks + chunk) * a.prefix_rows;
+    } else {
+        const int id = blockIdx.x - a.prefix_groups, item = id / a.own_chunks;
+        const int tile = a.own_row_tiles - 1 - item % a.own_row_tiles;   // the longest first
+        int unit = item / a.own_row_tiles;
+        chunks = a.own_chunks;
+        chunk = id % chunks;
+        j.place = (((int64_t)unit * a.own_row_tiles + tile) * chunks + chunk) * a.own_rows;
+        j.h = unit % a.pages.n_kv_heads;
+        unit /= a.pages.n_kv_heads;
+        if (LISTED) {
+            j.token = unit % a.q_tokens;
+            unit /= a.q_tokens;
+        }
+        j.b = unit;
+        j.n = length_of(a.q_lengths, j.b, a.q_tokens);
+        j.N = length_of(a.kv_lengths, j.b, a.kv_tokens);
+        j.row0 = tile * ROWS;
+        const int all = LISTED ? j.token < j.n ? a.G : 0 : j.n * a.G;
+        j.rows = min(ROWS, all - j.row0);
+        if (j.rows <= 0) return false;
+        j.begin = LISTED ? 0 : a.shared;
+        j.end = j.N;
+        if (!LISTED) {
+            const int last = j.N - j.n + (j.row0 + j.rows - 1) / a.G;
+            j.tiles = max(0, (min(j.N, last + 1) - j.begin + TILE - 1) / TILE);
+        } else {
+            const int32_t* list = a.blocks + (((int64_t)j.b * a.pages.n_kv_heads + j.h) * a.q_tokens + j.token) * a.slots;
+            const int lane = threadIdx.x % 64;
+            int used = 0;                                                // of its entries: up to the last block that there is
+            for (int at = (a.slots - 1) / 64 * 64; at >= 0; at -= 64) {
+                const uint64_t some = __ballot(at + lane < a.slots && list[min(at + lane, a.slots - 1)] >= 0);
+                if (some) {
+                    used = at + 64 - __builtin_clzll(some);
+                    break;
+                }
+            }
+            j.tiles = (int)((((int64_t)used << a.pages.log2) + TILE - 1) / TILE);
+        }
+    }
+    j.i_begin = (int)((int64_t)j.tiles * chunk / chunks);
+    j.i_end = (int)((int64_t)j.tiles * (chunk + 1) / chunks);
+    return true;
+}
+
+// Where the positions of tiles are: tile i_first + k * STEP, its GRANULES granules of 16, for the next 64 granules at a time.
+template <int GRANULES>
+struct Granules {
+    int page[GRANULES], pos0[GRANULES];
+    uint32_t edge, wave_edge;         // granules that some row (of the wave) does not see all of
+};
+template <bool LISTED, int GRANULES>
+struct Directory {
+    static constexpr int kTiles = 64 / GRANULES;
+    const int32_t* table;
+    const int32_t* list;
+    int log2, n_pages, slots, begin, end, i_first, step, lane;
+    int first, wave_first;            // the first position that is the last one seen of some row (of the wave)
+    int k0, page, pos0;
+    uint64_t edge, wave_edge;
+
+    __device__ __forceinline__ Directory(const PagedArgs& a, const Job& j, int i_first_, int step_, int lane_, int first_, int wave_first_)
+        : table(a.pages.table + (j.prefix ? 0 : j.b * a.pages.table_stride)),
+          list(LISTED ? a.blocks + (((int64_t)j.b * a.pages.n_kv_heads + j.h) * a.q_tokens + j.token) * a.slots : nullptr),
+          log2(a.pages.log2), n_pages(a.pages.n_pages), slots(a.slots), begin(j.begin), end(j.end), i_first(i_first_), step(step_), lane(lane_),
+          first(first_), wave_first(wave_first_) {}
+    __device__ __forceinline__ void load(int k) {
+        k0 = k;
+        const int64_t place = (int64_t)begin + ((int64_t)(i_first + (k + lane / GRANULES) * step) * GRANULES + lane % GRANULES) * 16;
+        int64_t position = place;
+        bool there = place < end;
+        if constexpr (LISTED) {
+            const int64_t entry = place >> log2;
+            const int block = entry < slots ? list[entry] : -1;
+            position = ((int64_t)block << log2) + (place & ((1 << log2) - 1));
+            there = block >= 0 && position < end;
+        }
+        page = -1;
+        if (there) page = table[position >> log2];
+        there = (uint32_t)page < (uint32_t)n_pages;
+        page = there ? page : 0;
+        pos0 = there ? (int)position : kHidden;
+        edge = __ballot(pos0 + 15 > first);
+        wave_edge = __ballot(pos0 + 15 > wave_first);
+    }
+    __device__ __forceinline__ Granules<GRANULES> at(int k) {
+        if (k - k0 >= kTiles) load(k);
+        Granules<GRANULES> g;
+        const int l = (k - k0) * GRANULES;
+#pragma unroll
+        for (int i = 0; i < GRANULES; ++i) {
+            g.page[i] = __builtin_amdgcn_readlane(page, l + i);
+            g.pos0[i] = __builtin_amdgcn_readlane(pos0, l + i);
+        }
+        g.edge = (uint32_t)(edge >> l) & ((1u << GRANULES) - 1);
+        g.wave_edge = (uint32_t)(wave_edge >> l) & ((1u << GRANULES) - 1);
+        return g;
+    }
+};
+
+// One wave's loads of keys or values of a granule: LOADS times 4 positions from position 4 * LOADS * part of it on, to LDS in the order that Rows reads.
+template <bool KEYS, int LOADS>
+struct PageFetch {
+    const char* base;                 // the head's first place of page 0
+    int64_t page_bytes;
+    uint32_t place_bytes;
+    int part, lane, log2;
+    uint32_t at[LOADS];
+    __device__ __forceinline__ int position(int i) const { return 4 * (LOADS * part + i) + lane / 16; }
+    __device__ __forceinline__ uint32_t piece(int i) const {
+        const int r = position(i);
+        return ((lane % 16) ^ (KEYS ? key_swizzle(r) : value_swizzle(r))) * 16;
+    }
+    __device__ __forceinline__ PageFetch(const specache_view& v, int h, int log2_, int part_, int lane_)
+        : base((const char*)v.data + h * v.head * 2), page_bytes(v.batch * 2), place_bytes((uint32_t)v.token * 2), part(part_), lane(lane_), log2(log2_) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) at[i] = (uint32_t)position(i) * place_bytes + piece(i);
+    }
+    __device__ __forceinline__ const char* granule(int page, int pos0) const {
+        return base + page * page_bytes + (int64_t)((pos0 & ((1 << log2) - 1)) * (uint64_t)place_bytes);
+    }
+    // Positions from `end` on are the last one before it again (no row sees them, but they are finite if it is).
+    __device__ __forceinline__ void operator()(int page, int pos0, int end, char* lds) const {
+        const char* from = granule(page, pos0);
+        char* to = lds + 4 * LOADS * part * kRowBytes16;
+        if (pos0 + 16 <= end || pos0 == kHidden) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i)
+                __builtin_amdgcn_global_load_lds((global_void*)(from + at[i]), (lds_void*)(to + 4 * i * kRowBytes16), 16, 0, 0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const uint32_t r = min(position(i), end - 1 - pos0);
+                __builtin_amdgcn_global_load_lds((global_void*)(from + (r * place_bytes + piece(i))), (lds_void*)(to + 4 * i * kRowBytes16), 16, 0, 0);
+            }
+        }
+    }
+};
+
+template <bool BF16, int BLOCKS>
+struct PagedRows : Rows<BF16, BLOCKS> {
+    using Base = Rows<BF16, BLOCKS>;
+    bool saw = false;                 // some position (of this lane's half)
+    // hides what the row does not see
+    __device__ __forceinline__ void hide(const int (&pos0)[2 * BLOCKS]) {
+#pragma unroll
+        for (int g = 0; g < 2 * BLOCKS; ++g) {
+            const int most = Base::seen.last - pos0[g] - 4 * Base::half;
+            saw |= most >= 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (8 * (e / 4) + e % 4 > most) Base::s[g / 2][8 * (g % 2) + e] = -INFINITY;
+                if (e % 2) __builtin_amdgcn_sched_barrier(0);   // few conditions at a time: they live in scalar registers
+            }
+        }
+    }
+    // what drop_odd_values dropped of a granule
+    __device__ void give_odd_granule(const char* values, uint32_t place_bytes, int pos0, int end) {
+        for (int j = 0; j < 16 && pos0 + j < end; ++j)
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const uint32_t x = ((const uint16_t*)(values + (uint64_t)j * place_bytes))[32 * dt + 8 * (i / 4) + 4 * Base::half + i % 4];
+                    if ((x & kExponents<BF16> & 0xFFFFu) == (kExponents<BF16> & 0xFFFFu) && pos0 + j <= Base::seen.last) Base::o[dt][i] += widen16<BF16>(x);
+                }
+    }
+    // the two halves' sums and what they saw, together
+    __device__ __forceinline__ void finish() {
+        Base::l += other_half(Base::l);
+        if (!saw && other_half(saw ? 1.0f : 0.0f) == 0.0f) Base::m = -INFINITY;
+    }
+};
+
+template <int LANES>
+__device__ __forceinline__ int least_of_wave(int v) {
+#pragma unroll
+    for (int d = 1; d < LANES; d *= 2) v = min(v, __shfl_xor(v, d));
+    return __builtin_amdgcn_readfirstlane(v);
+}
+
+// Rows of more than a wave: the waves of a workgroup have rows of their own and share tiles of 64 positions, which travel to LDS while the one before is worked on.
+template <bool BF16, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void paged_tile_kernel(PagedArgs a) {
+    constexpr int TILE = 64, ROWS = WAVES * kWaveRows, LOADS = 16 / WAVES, PARTS = 4 / LOADS;
+    __shared__ __align__(1024) char keys_even[TILE * kRowBytes16];
+    __shared__ __align__(1024) char keys_odd[TILE * kRowBytes16];
+    __shared__ __align__(1024) char values_even[TILE * kRowBytes16];
+    __shared__ __align__(1024) char values_odd[TILE * kRowBytes16];
+    __shared__ int any_dropped, least[WAVES];
+
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    Job j;
+    if (!job_of<false, TILE, ROWS>(a, j)) return;
+    const int i_row = wave * kWaveRows + lane % 32;
+    const Row row = row_of<false>(a, j, i_row);
+    int first, wave_first, wave_last;
+    if (threadIdx.x == 0) any_dropped = 0;
+    if (j.prefix) {
+        wave_first = least_of_wave<32>(row.last);
+        wave_last = j.end;
+        if (lane == 0) least[wave] = wave_first;
+        __syncthreads();
+        first = least[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) first = min(first, least[w]);
+        first = __builtin_amdgcn_readfirstlane(first);
+    } else {
+        first = j.N - j.n + j.row0 / a.G;
+        wave_first = j.N - j.n + (j.row0 + min(wave * kWaveRows, j.rows - 1)) / a.G;
+        wave_last = j.N - j.n + (j.row0 + min(wave * kWaveRows + kWaveRows - 1, j.rows - 1)) / a.G;
+        __syncthreads();
+    }
+
+    PagedRows<BF16, TILE / 32> rs;
+    rs.seen = Seen{row.last, 0, 0};
+    const int granule = wave / PARTS;      // of a tile, whose keys and values the wave fetches (a part of)
+    Directory<false, 4> directory(a, j, j.i_begin, 1, lane, first, wave_first);
+    const PageFetch<true, LOADS> fetch_keys(a.pages.k, j.h, a.pages.log2, wave % PARTS, lane);
+    const PageFetch<false, LOADS> fetch_values(a.pages.v, j.h, a.pages.log2, wave % PARTS, lane);
+    rs.start((const uint16_t*)a.q.data + row.b * a.q.batch + row.head * a.q.head + row.token * a.q.token, lane, a.scale);
+    const int n = j.i_end - j.i_begin;
+    Granules<4> here;
+    const auto fetch = [&](const Granules<4>& g, char* keys, char* values) __attribute__((always_inline)) {
+        const int page = granule == 0 ? g.page[0] : granule == 1 ? g.page[1] : granule == 2 ? g.page[2] : g.page[3];
+        const int pos0 = granule == 0 ? g.pos0[0] : granule == 1 ? g.pos0[1] : granule == 2 ? g.pos0[2] : g.pos0[3];
+        fetch_keys(page, pos0, j.end, keys + granule * 16 * kRowBytes16);
+        fetch_values(page, pos0, j.end, values + granule * 16 * kRowBytes16);
+    };
+    if (n > 0) {
+        directory.load(0);
+        here = directory.at(0);
+        fetch(here, keys_even, values_even);
+    }
+    const auto step = [&](int k, char* keys, char* values, char* next_keys, char* next_values) __attribute__((always_inline)) {
+        Granules<4> next = here;
+        __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+        if (here.edge && drop_odd_values<BF16, LOADS>(values, wave, lane)) any_dropped = 1;
+        __syncthreads();
+        if (k + 1 < n) {
+            next = directory.at(k + 1);
+            fetch(next, next_keys, next_values);
+        }
+        if (j.begin + (j.i_begin + k) * TILE <= wave_last) {   // some of the wave's rows see the tile
+            rs.scores(keys);
+            // the first reads ahead of the products, then one beside each
+            __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+            for (int i = 0; i < 10; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
+            if (here.wave_edge) rs.hide(here.pos0);
+            else rs.saw = true;
+            rs.move_maximum(a.scale);
+            rs.weights();
+            rs.add_values(values);
+            // the first step's weights, then the others' beside the products
+            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 28, 0);
+#pragma unroll
+            for (int i = 0; i < 12; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 7, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+        }
+        here = next;
+    };
+    for (int k = 0; k < n; k += 2) {
+        step(k, keys_even, values_even, keys_odd, values_odd);
+        if (k + 1 < n) step(k + 1, keys_odd, values_odd, keys_even, values_even);
+    }
+    __syncthreads();
+    if (any_dropped) {
+        directory.load(0);
+        for (int k = 0; k < n; ++k) {
+            const Granules<4> g = directory.at(k);
+            if (g.edge)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (g.pos0[i] != kHidden) rs.give_odd_granule(fetch_values.granule(g.page[i], g.pos0[i]), fetch_values.place_bytes, g.pos0[i], j.end);
+        }
+    }
+    rs.finish();
+    if (i_row >= j.rows) return;
+    if (j.prefix || a.parts) rs.store_part(j.prefix ? a.prefix_o : a.own_o, j.prefix ? a.prefix_ml : a.own_ml, j.place + i_row, n > 0);
+    else {
+        rs.seen.last = rs.m != -INFINITY ? 0 : -1;   // (whether the row saw anything)
+        rs.store((uint16_t*)a.out.data + row.b * a.out.batch + row.head * a.out.head + row.token * a.out.token);
+    }
+}
+
+// Waves by themselves: up to 32 rows, 32 positions at a time, the next ones on their way while a wave works on these; the waves of a workgroup take a
+// chunk's tiles in turn and join their results in LDS at its end.
+template <bool BF16, bool LISTED, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void paged_step_kernel(PagedArgs a) {
+    constexpr int TILE = 32, BYTES = TILE * kRowBytes16, HALF = BYTES / 2;
+    __shared__ __align__(1024) char keys_even[WAVES * BYTES];
+    __shared__ __align__(1024) char keys_odd[WAVES * BYTES];
+    __shared__ __align__(1024) char values_even[WAVES * BYTES];
+    __shared__ __align__(1024) char values_odd[WAVES * BYTES];
+    __shared__ float2 joined[WAVES][kWaveRows];
+
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    Job j;
+    if (!job_of<LISTED, TILE, kWaveRows>(a, j)) return;
+    const Row row = row_of<LISTED>(a, j, lane % 32);
+    const int first = least_of_wave<32>(row.last);
+    const int n = max(0, (j.i_end - j.i_begin - wave + WAVES - 1) / WAVES);   // tiles of this wave
+
+    PagedRows<BF16, 1> rs;
+    rs.seen = Seen{row.last, 0, 0};
+    Directory<LISTED, 2> directory(a, j, j.i_begin + wave, WAVES, lane, first, first);
+    const PageFetch<true, 4> fetch_keys(a.pages.k, j.h, a.pages.log2, 0, lane);
+    const PageFetch<false, 4> fetch_values(a.pages.v, j.h, a.pages.log2, 0, lane);
+    bool dropped = false;
+    Granules<2> here;
+    const auto fetch = [&](const Granules<2>& g, char* keys, char* values) __attribute__((always_inline)) {
+        fetch_keys(g.page[0], g.pos0[0], j.end, keys + wave * BYTES);
+        fetch_keys(g.page[1], g.pos0[1], j.end, keys + wave * BYTES + HALF);
+        fetch_values(g.page[0], g.pos0[0], j.end, values + wave * BYTES);
+        fetch_values(g.page[1], g.pos0[1], j.end, values + wave * BYTES + HALF);
+    };
+    if (n > 0) {
+        directory.load(0);
+        here = directory.at(0);
+        fetch(here, keys_even, values_even);
+    }
+    rs.start((const uint16_t*)a.q.data + row.b * a.q.batch + row.head * a.q.head + row.token * a.q.token, lane, a.scale);
+    const auto step = [&](int k, char* keys, char* values, char* next_keys, char* next_values) __attribute__((always_inline)) {
+        const bool more = k + 1 < n;
+        Granules<2> next = here;
+        if (more) next = directory.at(k + 1);
+        asm volatile("" ::: "memory");        // (the buffers' last reads are behind)
+        __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+        if (more) {
+            fetch(next, next_keys, next_values);
+            __builtin_amdgcn_s_waitcnt(0x4F78);   // vmcnt(24): this tile's keys are there
+        } else {
+            __builtin_amdgcn_s_waitcnt(0x0F78);   // vmcnt(8)
+        }
+        asm volatile("" ::: "memory");
+        rs.scores(keys + wave * BYTES);
+        if (here.edge) rs.hide(here.pos0);
+        else rs.saw = true;
+        rs.move_maximum(a.scale);
+        rs.weights();
+        asm volatile("" ::: "memory");
+        if (more) __builtin_amdgcn_s_waitcnt(0x4F70);   // vmcnt(16): and its values
+        else __builtin_amdgcn_s_waitcnt(0x0F70);
+        asm volatile("" ::: "memory");
+        if (here.edge) dropped |= drop_odd_values<BF16, 8>(values + wave * BYTES, 0, lane);
+        rs.add_values(values + wave * BYTES);
+        here = next;
+    };
+    for (int k = 0; k < n; k += 2) {
+        step(k, keys_even, values_even, keys_odd, values_odd);
+        if (k + 1 < n) step(k + 1, keys_odd, values_odd, keys_even, values_even);
+    }
+    if (__ballot(dropped)) {
+        directory.load(0);
+        for (int k = 0; k < n; ++k) {
+            const Granules<2> g = directory.at(k);
+            if (g.edge)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (g.pos0[i] != kHidden) rs.give_odd_granule(fetch_values.granule(g.page[i], g.pos0[i]), fetch_values.place_bytes, g.pos0[i], j.end);
+        }
+    }
+    rs.finish();
+
+    // every wave's sums to LDS (a row's channels turned by 4 per row: no two rows of a group of lanes meet in a bank), then four channels per thread
+    __syncthreads();
+    char* const room = wave == 0 ? keys_even : wave == 1 ? keys_odd : wave == 2 ? values_even : values_odd;
+    const int mine = lane % 32;
+    if (mine < j.rows) {
+        if (lane < 32) joined[wave][mine] = float2{rs.m, rs.l};
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *(float4*)(room + (mine * kD + (32 * dt + 8 * i + 4 * rs.half + 4 * mine) % kD) * 4) =
+                    float4{rs.o[dt][4 * i], rs.o[dt][4 * i + 1], rs.o[dt][4 * i + 2], rs.o[dt][4 * i + 3]};
+    }
+    __syncthreads();
+    for (int at = threadIdx.x; at < j.rows * (kD / 4); at += 64 * WAVES) {
+        const int r = at / (kD / 4), c = at % (kD / 4) * 4;
+        float m = -INFINITY, l = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) m = fmaxf(m, joined[w][r].x);
+        float4 o{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float2 ml = joined[w][r];
+            const float f = __builtin_amdgcn_exp2f(ml.x - fmaxf(m, kNever));
+            const char* from = w == 0 ? keys_even : w == 1 ? keys_odd : w == 2 ? values_even : values_odd;
+            const float4 x = *(const float4*)(from + (r * kD + (c + 4 * r) % kD) * 4);
+            l = fmaf(f, ml.y, l);
+            o.x = fmaf(f, x.x, o.x), o.y = fmaf(f, x.y, o.y), o.z = fmaf(f, x.z, o.z), o.w = fmaf(f, x.w, o.w);
+        }
+        if (j.prefix || a.parts) {
+            float* po = j.prefix ? a.prefix_o : a.own_o;
+            float* pm = j.prefix ? a.prefix_ml : a.own_ml;
+            if (c == 0) *(float2*)(pm + 2 * (j.place + r)) = float2{m, l};
+            *(float4*)(po + (j.place + r) * kD + c) = o;
+        } else {
+            const float by = divisor_of(l, m != -INFINITY);
+            const Row to = row_of<LISTED>(a, j, r);
+            uint16_t* out = (uint16_t*)a.out.data + to.b * a.out.batch + to.head * a.out.head + to.token * a.out.token;
+            *(uint2v*)(out + c) = uint2v{pack16<BF16>(o.x * by, o.y * by), pack16<BF16>(o.z * by, o.w * by)};
+        }
+    }
+}
+
+// The partial results of a row, joined: those of the prefix, then those of its own positions; two channels per lane, the parts dealt to the waves of a
+// workgroup (a wave by itself where there are few), every load of a wave's first parts asked for at once.
+constexpr int kMergeWaves = 4, kFewParts = 4;
+template <bool BF16, bool LISTED, int WAVES>
+__global__ __launch_bounds__(64 * kMergeWaves) void paged_merge_kernel(PagedArgs a) {
+    __shared__ float part[WAVES][kD];
+    __shared__ float3 joined[WAVES];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64 % WAVES;
+    const int r = blockIdx.x * (kMergeWaves / WAVES) + threadIdx.x / (64 * WAVES);   // [batch][token][query head]
+    if (WAVES < kMergeWaves && r >= a.merge_rows) return;
+    const int Hkv = a.pages.n_kv_heads, head = r % (Hkv * a.G), token = r / (Hkv * a.G) % a.q_tokens, b = r / (Hkv * a.G) / a.q_tokens;
+    const int h = head / a.G, g = head % a.G;
+    const int n = length_of(a.q_lengths, b, a.q_tokens);
+    if (token >= n) return;
+    const int n_prefix = a.prefix_chunks, parts = n_prefix + a.own_chunks;
+    const int prefix_row = (b * a.q_tokens + token) * a.G + g, own_row = LISTED ? g : token * a.G + g;
+    const int64_t unit = LISTED ? ((int64_t)b * a.q_tokens + token) * Hkv + h : (int64_t)b * Hkv + h;
+    const int64_t prefix0 = n_prefix ? ((int64_t)h * a.prefix_row_tiles + prefix_row / a.prefix_rows) * n_prefix * a.prefix_rows + prefix_row % a.prefix_rows : 0;
+    const int64_t own0 = (unit * a.own_row_tiles + own_row / a.own_rows) * a.own_chunks * a.own_rows + own_row % a.own_rows;
+    float m = kNever, l = 0.0f, x = 0.0f, y = 0.0f;
+    bool sees = false;
+    constexpr int kAhead = WAVES == 1 ? kFewParts : 8;
+    for (int c0 = wave; c0 < parts; c0 += kAhead * WAVES) {
+        float2 one[kAhead], oc[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int c = min(c0 + i * WAVES, parts - 1);
+            const bool shared = c < n_prefix;
+            const int64_t at = shared ? prefix0 + (int64_t)c * a.prefix_rows : own0 + (int64_t)(c - n_prefix) * a.own_rows;
+            one[i] = ((const float2*)(shared ? a.prefix_ml : a.own_ml))[at];
+            oc[i] = *(const float2*)((shared ? a.prefix_o : a.own_o) + at * kD + 2 * lane);
+        }
+        float most = m;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            most = fmaxf(most, one[i].x);
+            sees |= one[i].x != -INFINITY;
+        }
+        const float moved = __builtin_amdgcn_exp2f(m - most);
+        l *= moved, x *= moved, y *= moved;
+        m = most;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (c0 + i * WAVES >= parts || one[i].y == 0.0f) continue;   // (an empty part stored no sums)
+            const float w = __builtin_amdgcn_exp2f(one[i].x - m);
+            l = fmaf(w, one[i].y, l);
+            x = fmaf(w, oc[i].x, x);
+            y = fmaf(w, oc[i].y, y);
+        }
+    }
+    if constexpr (WAVES > 1) {
+        *(float2*)&part[wave][2 * lane] = float2{x, y};
+        if (lane == 0) joined[wave] = float3{m, l, sees ? 1.0f : 0.0f};
+        __syncthreads();
+        if (wave) return;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            m = fmaxf(m, joined[w].x);
+            sees |= joined[w].z != 0.0f;
+        }
+        l = x = y = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float f = __builtin_amdgcn_exp2f(joined[w].x - m);
+            const float2 o = *(const float2*)&part[w][2 * lane];
+            l = fmaf(f, joined[w].y, l);
+            x = fmaf(f, o.x, x);
+            y = fmaf(f, o.y, y);
+        }
+    }
+    const float by = divisor_of(l, sees);
+    uint16_t* to = (uint16_t*)a.out.data + b * a.out.batch + head * a.out.head + token * a.out.token;
+    *(uint32_t*)(to + 2 * lane) = pack16<BF16>(x * by, y * by);
+}
+
+constexpr int kStepWaves = 2;
+constexpr int64_t kMostGroups = INT32_MAX / 512;   // a launch's threads are counted in 32 bits
+constexpr int64_t kStepsAtOnce = 512;
+enum { kStep, kTile4, kTile8 };
+// how a kind of work (the prefix's, the sequences' own) is laid out
+struct Part {
+    int kernel = kStep, row_tiles = 1, item_rows = 1, chunks = 0;
+    int64_t items = 0;
+    int64_t groups() const { return items * chunks; }
+    int64_t places() const { return items * chunks * item_rows; }
+};
+struct Plan {
+    Part prefix, own;
+    int shared = 0;
+    bool parts = false;
+    int64_t scratch = 0;
+};
+
+// `units` of `rows` rows each over at most `most` positions
+Part part_of(int64_t units, int64_t rows, int64_t most, bool listed) {
+    Part p;
+    int64_t chunks = 1;
+    if (rows <= kWaveRows || listed) {
+        p.kernel = kStep;
+        p.item_rows = (int)std::min<int64_t>(std::max<int64_t>(rows, 1), kWaveRows);
+        p.row_tiles = (int)((rows + kWaveRows - 1) / kWaveRows);
+        p.items = units * p.row_tiles;
+        const int64_t tiles = (most + 31) / 32;
+        if (p.items && tiles > 4 * kStepWaves) {
+            chunks = std::max(kStepsAtOnce / p.items, tiles / 64);
+            chunks = std::min({chunks, tiles / kStepWaves, std::max<int64_t>(256, tiles / 64)});
+        }
+    } else {
+        p.kernel = most >= 2048 && rows > 128 ? kTile8 : kTile4;
+        p.item_rows = p.kernel == kTile8 ? 256 : 128;
+        p.row_tiles = (int)((rows + p.item_rows - 1) / p.item_rows);
+        p.items = units * p.row_tiles;
+        if (p.items) chunks = std::min<int64_t>((p.kernel == kTile8 ? 256 : 512) / p.items, (most + 63) / 64 / 4);
+    }
+    p.chunks = (int)std::max<int64_t>(chunks, 1);
+    return p;
+}
+
+int finish_plan(Plan& p, int64_t merge_rows) {
+    if (!p.shared && merge_rows >= kMostGroups) p.own.chunks = 1;
+    p.parts = p.shared || p.own.chunks > 1;
+    if (p.prefix.groups() + p.own.groups() > kMostGroups || (p.parts && merge_rows > kMostGroups)) return fail_without_context(SPECACHE_EINVAL, "too many rows");
+    p.scratch = p.parts ? (p.prefix.places() + p.own.places()) * (kD + 2) * (int64_t)sizeof(float) : 0;
+    return SPECACHE_OK;
+}
+
+int check_counts(const specache_pages& c, int batch, int n_q_heads, int q_tokens, int kv_tokens, float sm_scale) {
+    if (batch < 0 || q_tokens < 0 || kv_tokens < 0) return fail_without_context(SPECACHE_EINVAL, "batch, q_tokens and kv_tokens must not be negative");
+    if (n_q_heads < 1 || n_q_heads % c.n_kv_heads || n_q_heads / c.n_kv_heads > 64)
+        return fail_without_context(SPECACHE_EINVAL, "n_q_heads must be a multiple of n_kv_heads, up to 64 of it");
+    if (kv_tokens > (int64_t)c.table_pages * c.page_tokens) return fail_without_context(SPECACHE_EINVAL, "kv_tokens is more than the table holds");
+    if (!std::isfinite(sm_scale)) return fail_without_context(SPECACHE_EINVAL, "sm_scale must be finite");
+    const int64_t rows = (int64_t)batch * q_tokens;
+    if (rows > (1 << 28) || rows * n_q_heads > (1 << 28)) return fail_without_context(SPECACHE_EINVAL, "too many rows");
+    return SPECACHE_OK;
+}
+
+int plan_of(const specache_pages* cache, const specache_paged_config* c, Plan& p) {
+    if (int rc = check_pages(cache)) return rc;
+    if (!c) return fail_without_context(SPECACHE_EINVAL, "null configuration");
+    if (int rc = check_counts(*cache, c->batch, c->n_q_heads, c->q_tokens, c->kv_tokens, c->sm_scale)) return rc;
+    if (c->shared_tokens < 0) return fail_without_context(SPECACHE_EINVAL, "shared_tokens must not be negative");
+    const int G = c->n_q_heads / cache->n_kv_heads;
+    const int64_t rows = (int64_t)c->q_tokens * G;
+    if (c->batch > 1 && rows) p.shared = std::min(c->shared_tokens, c->kv_tokens) / cache->page_tokens * cache->page_tokens;
+    if (p.shared) p.prefix = part_of(cache->n_kv_heads, c->batch * rows, p.shared, false);
+    p.own = part_of(rows ? (int64_t)c->batch * cache->n_kv_heads : 0, rows, c->kv_tokens - p.shared, false);
+    return finish_plan(p, c->batch * rows * cache->n_kv_heads);
+}
+
+}  // namespace
+
+int check_blocks(const specache_pages* cache, const specache_block_config* c) {
+    if (int rc = check_pages(cache)) return rc;
+    if (!c) return fail_without_context(SPECACHE_EINVAL, "null configuration");
+    if (int rc = check_counts(*cache, c->batch, c->n_q_heads, c->q_tokens, c->kv_tokens, c->sm_scale)) return rc;
+    const int64_t slots = (int64_t)c->top + c->first + c->recent;
+    if (c->top < 0 || c->first < 0 || c->recent < 0 || slots < 1 || slots > (1 << 20))
+        return fail_without_context(SPECACHE_EINVAL, "top, first and recent must not be negative, and make up from 1 to 2^20 entries");
+    return SPECACHE_OK;
+}
+
+namespace {
+
+int plan_of_blocks(const specache_pages* cache, const specache_block_config* c, Plan& p) {
+    if (int rc = check_blocks(cache, c)) return rc;
+    const int64_t slots = (int64_t)c->top + c->first + c->recent, blocks = (c->kv_tokens + cache->page_tokens - 1) / cache->page_tokens;
+    const int64_t units = (int64_t)c->batch * c->q_tokens * cache->n_kv_heads;
+    p.own = part_of(units, c->n_q_heads / cache->n_kv_heads, std::min(slots, blocks) * cache->page_tokens, true);
+    return finish_plan(p, units * (c->n_q_heads / cache->n_kv_heads));
+}
+
+}  // namespace
+
+int block_attend_scratch(const specache_pages& cache, const specache_block_config& c, int64_t* bytes) {
+    Plan p;
+    if (int rc = plan_of_blocks(&cache, &c, p)) return rc;
+    *bytes = p.scratch;
+    return SPECACHE_OK;
+}
+
+namespace {
+
+PagedArgs args_of(const specache_pages& cache, const Plan& p, int batch, int n_q_heads, int q_tokens, int kv_tokens, float sm_scale, const specache_view* q,
+                  const specache_view* out, const int32_t* q_lengths, const int32_t* kv_lengths, void* scratch) {
+    PagedArgs a{};
+    a.q = *q;
+    a.out = *out;
+    a.pages = page_args(cache);
+    a.q_lengths = q_lengths;
+    a.kv_lengths = kv_lengths;
+    a.prefix_o = (float*)scratch;
+    a.own_o = a.prefix_o + p.prefix.places() * kD;
+    a.prefix_ml = a.own_o + p.own.places() * kD;
+    a.own_ml = a.prefix_ml + p.prefix.places() * 2;
+    a.batch = batch;
+    a.G = n_q_heads / cache.n_kv_heads;
+    a.q_tokens = q_tokens;
+    a.kv_tokens = cache.n_pages ? kv_tokens : 0;
+    a.shared = cache.n_pages ? p.shared : 0;
+    a.own_chunks = p.own.chunks;
+    a.own_row_tiles = p.own.row_tiles;
+    a.own_rows = p.own.item_rows;
+    a.prefix_chunks = p.prefix.chunks;
+    a.prefix_row_tiles = p.prefix.row_tiles;
+    a.prefix_rows = p.prefix.item_rows;
+    a.parts = p.parts;
+    a.merge_rows = batch * q_tokens * n_q_heads;
+    a.scale = (sm_scale > 0.0f ? sm_scale : 0.08838834764831845f) * kLog2e;
+    return a;
+}
+
+template <bool BF16>
+void launch_part(int kernel, int64_t groups, const PagedArgs& a, hipStream_t stream) {
+    const dim3 grid((unsigned)groups);
+    if (kernel == kStep) hipLaunchKernelGGL((paged_step_kernel<BF16, false, kStepWaves>), grid, dim3(64 * kStepWaves), 0, stream, a);
+    else if (kernel == kTile4) hipLaunchKernelGGL((paged_tile_kernel<BF16, 4>), grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((paged_tile_kernel<BF16, 8>), grid, dim3(512), 0, stream, a);
+}
+
+template <bool BF16, bool LISTED>
+void launch_merge(const Plan& p, const PagedArgs& a, hipStream_t stream) {
+    if (!p.parts) return;
+    if (a.prefix_chunks + a.own_chunks <= kFewParts)
+        hipLaunchKernelGGL((paged_merge_kernel<BF16, LISTED, 1>), dim3((unsigned)((a.merge_rows + kMergeWaves - 1) / kMergeWaves)), dim3(64 * kMergeWaves), 0, stream, a);
+    else hipLaunchKernelGGL((paged_merge_kernel<BF16, LISTED, kMergeWaves>), dim3((unsigned)a.merge_rows), dim3(64 * kMergeWaves), 0, stream, a);
+}
+
+template <bool BF16>
+void launch(const Plan& p, PagedArgs a, hipStream_t stream) {
+    if (p.shared) {
+        a.prefix_groups = (int)p.prefix.groups();
+        launch_part<BF16>(p.prefix.kernel, p.prefix.groups(), a, stream);
+        a.prefix_groups = 0;
+    }
+    launch_part<BF16>(p.own.kernel, p.own.groups(), a, stream);
+    launch_merge<BF16, false>(p, a, stream);
+}
+
+template <bool BF16>
+void launch_listed(const Plan& p, const PagedArgs& a, hipStream_t stream) {
+    hipLaunchKernelGGL((paged_step_kernel<BF16, true, kStepWaves>), dim3((unsigned)p.own.groups()), dim3(64 * kStepWaves), 0, stream, a);
+    launch_merge<BF16, true>(p, a, stream);
+}
+
+int check_call(const specache_pages& cache, const Plan& p, const specache_view* q, const specache_view* out, int batch, int n_q_heads, int q_tokens,
+               int kv_tokens, const int32_t* q_lengths, const int32_t* kv_lengths, void* scratch, int64_t scratch_bytes) {
+    if (!q || !out) return fail_without_context(SPECACHE_EINVAL, "null view");
+    if (!view_fits(*q) || !view_fits(*out)) return fail_without_context(SPECACHE_EINVAL, "a view's address must be 16-byte aligned, its strides multiples of 8");
+    if (!rows_apart(*out, batch, n_q_heads, q_tokens)) return fail_without_context(SPECACHE_EINVAL, "the output's rows share memory");
+    if ((uintptr_t)q_lengths % 4 || (uintptr_t)kv_lengths % 4) return fail_without_context(SPECACHE_EINVAL, "misaligned lengths");
+    if (kv_tokens)
+        if (int rc = check_page_views(cache, true, false)) return rc;
+    if (p.scratch) {
+        if (!scratch || (uintptr_t)scratch % 16) return fail_without_context(SPECACHE_EINVAL, "scratch must be 16-byte aligned");
+        if (scratch_bytes < p.scratch) return fail_without_context(SPECACHE_ECAPACITY, "scratch is smaller than the call needs");
+    }
+    return SPECACHE_OK;
+}
+
+}  // namespace
+}  // namespace specache
+
+using namespace specache;
+
+extern "C" {
+
+int specache_paged_scratch(const specache_pages* cache, const specache_paged_config* cfg, int64_t* bytes) {
+    Plan p;
+    if (int rc = plan_of(cache, cfg, p)) return rc;
+    if (!bytes) return fail_without_context(SPECACHE_EINVAL, "null output");
+    *bytes = p.scratch;
+    return SPECACHE_OK;
+}
+
+int specache_paged_attend(const specache_pages* cache, const specache_paged_config* cfg, const specache_view* q, const specache_view* out,
+                          const int32_t* q_lengths, const int32_t* kv_lengths, void* scratch, int64_t scratch_bytes, void* stream) {
+    Plan p;
+    if (int rc = plan_of(cache, cfg, p)) return rc;
+    if (!p.own.items) return SPECACHE_OK;
+    if (int rc = check_call(*cache, p, q, out, cfg->batch, cfg->n_q_heads, cfg->q_tokens, cfg->kv_tokens, q_lengths, kv_lengths, scratch, scratch_bytes)) return rc;
+    const PagedArgs a = args_of(*cache, p, cfg->batch, cfg->n_q_heads, cfg->q_tokens, cfg->kv_tokens, cfg->sm_scale, q, out, q_lengths, kv_lengths, scratch);
+    if (cache->dtype == SPECACHE_BF16) launch<true>(p, a, (hipStream_t)stream);
+    else launch<false>(p, a, (hipStream_t)stream);
+    return launched();
+}
+
+int specache_block_attend(const specache_pages* cache, const specache_block_config* cfg, const specache_view* q, const specache_view* out,
+                          const int32_t* blocks, const int32_t* q_lengths, const int32_t* kv_lengths, void* scratch, int64_t scratch_bytes, void* stream) {
+    Plan p;
+    if (int rc = plan_of_blocks(cache, cfg, p)) return rc;
+    if (!p.own.items) return SPECACHE_OK;
+    if (int rc = check_call(*cache, p, q, out, cfg->batch, cfg->n_q_heads, cfg->q_tokens, cfg->kv_tokens, q_lengths, kv_lengths, scratch, scratch_bytes)) return rc;
+    if (!blocks || (uintptr_t)blocks % 4) return fail_without_context(SPECACHE_EINVAL, "null or misaligned blocks");
+    PagedArgs a = args_of(*cache, p, cfg->batch, cfg->n_q_heads, cfg->q_tokens, cfg->kv_tokens, cfg->sm_scale, q, out, q_lengths, kv_lengths, scratch);
+    a.blocks = blocks;
+    a.slots = cfg->top + cfg->first + cfg->recent;
+    if (cache->dtype == SPECACHE_BF16) launch_listed<true>(p, a, (hipStream_t)stream);
+    else launch_listed<false>(p, a, (hipStream_t)stream);
+    return launched();
+}
+
+}  // extern "C"

@@ -5,7 +5,7 @@
 // Far positions cost no more than near ones, and no table is read.
 #include <cmath>
 
-#include "operators.h"
+#include "rotate16.h"
 
 namespace specache {
 namespace {
@@ -19,30 +19,9 @@ struct RotateArgs {
     int tile_log2;                 // tokens of a workgroup's tile
 };
 
-constexpr int kThreads = 256, kParts = 8;   // a row is 8 lanes' work: 8 pairs of channels each, two 16-byte accesses
+constexpr int kThreads = 256;
 constexpr int kAhead = 4;                   // rows whose loads a lane has in flight
 constexpr int64_t kMostGroups = (1ll << 32) / kThreads;   // a launch's threads are counted in 32 bits
-constexpr int64_t kCached = 32 << 20;       // bytes that the L2s of the 8 XCDs hold
-
-typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
-template <bool STREAM>
-__device__ __forceinline__ void store16(uint16_t* to, const uint4& v) {
-    if constexpr (STREAM) __builtin_nontemporal_store(__builtin_bit_cast(uint4v, v), (uint4v*)to);
-    else *(uint4*)to = v;
-}
-template <bool BF16>
-__device__ __forceinline__ void unpack8(const uint4& u, float (&x)[8]) {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[2 * i] = widen16<BF16>(w[i] & 0xFFFFu);
-        x[2 * i + 1] = widen16<BF16>(w[i] >> 16);
-    }
-}
-template <bool BF16>
-__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
-    return uint4{pack16<BF16>(x[0], x[1]), pack16<BF16>(x[2], x[3]), pack16<BF16>(x[4], x[5]), pack16<BF16>(x[6], x[7])};
-}
 
 // A workgroup holds a tile of up to 4 tokens times the other factor of 32 in heads at a time and walks the heads: a lane works out its 8
 // angles once for all of them.  Memory is what bounds it.  The tile weighs reads, in which a token's heads lie side by side, against writes, in
@@ -59,22 +38,12 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a) {
     const int d = a.plan.rotary_dim, heads_here = (kThreads / kParts) >> a.tile_log2;
     if (t >= a.tokens) return;
 
-    // Halves: pair e of this part joins element e of both accesses.  Neighbours: pairs 0 to 3 are the first access's, 4 to 7 the second's.  Channels that
-    // stay are dealt like the others, so that an access of neighbouring lanes is in few pieces.
-    const bool turns[2] = {(HALF ? 16 : 8) * part < d, HALF ? 16 * part < d : 8 * part + kD / 2 < d};
-    const int c0 = HALF && !turns[0] ? d / 2 + 8 * part : 8 * part;
-    const int c1 = c0 + (!HALF ? kD / 2 : turns[0] ? d / 2 : (kD - d) / 2);
-    float cosine[8], sine[8];
-    if (turns[0]) {
+    const RowParts<HALF> parts(part, d);
+    const int c0 = parts.c0, c1 = parts.c1;
+    Turn<BF16, HALF> turn;
+    if (parts.turns[0]) {
         const int64_t p = a.positions ? a.positions[(int64_t)b * a.tokens + t] : a.first + t;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int pair = HALF ? 8 * part + e : 4 * part + e % 4 + e / 4 * (kD / 4);
-            const uint64_t angle = (uint64_t)p * a.plan.turns[pair];   // (0 for pairs that there are not)
-            const float x = (float)(int32_t)(angle >> 32) * 0x1p-32f;
-            cosine[e] = __builtin_amdgcn_cosf(x) * a.plan.gain;
-            sine[e] = __builtin_amdgcn_sinf(x) * a.plan.gain;
-        }
+        turn.set(a.plan, part, p);
     }
     const int n_q = a.heads[0], n_k = a.heads[1], n = n_q + n_k + a.heads[2];
     const int step = heads_here * gridDim.y;
@@ -100,27 +69,12 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a) {
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             if (!to[i]) continue;
-            if (turns[0] && !is_v[i]) {
-                float x[2][8], y[2][8];
-                unpack8<BF16>(u[i][0], x[0]);
-                unpack8<BF16>(u[i][1], x[1]);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int r0 = HALF ? 0 : e / 4, e0 = HALF ? e : 2 * (e % 4), r1 = HALF ? 1 : r0, e1 = HALF ? e : e0 + 1;
-                    const float p = x[r0][e0], q = x[r1][e1];
-                    y[r0][e0] = fmaf(p, cosine[e], -(q * sine[e]));
-                    y[r1][e1] = fmaf(q, cosine[e], p * sine[e]);
-                }
-                u[i][0] = pack8<BF16>(y[0]);
-                if (turns[1]) u[i][1] = pack8<BF16>(y[1]);
-            }
+            if (parts.turns[0] && !is_v[i]) turn.apply(u[i][0], u[i][1], parts.turns[1]);
             store16<STREAM>(to[i] + c0, u[i][0]);
             store16<STREAM>(to[i] + c1, u[i][1]);
         }
     }
 }
-
-bool in_place_or_apart(const specache_view& in, const specache_view& out) { return in.data != out.data || same_view(in, out); }
 
 }  // namespace
 }  // namespace specache
@@ -175,9 +129,7 @@ int specache_rotate(const specache_rotary* plan, int32_t dtype, int32_t batch, i
                     const specache_view* q, const specache_view* q_out, int32_t n_kv_heads, const specache_view* k,
                     const specache_view* k_out, const specache_view* v, const specache_view* v_out, const int32_t* positions,
                     int32_t first_position, void* stream) {
-    if (!plan || plan->rotary_dim < 16 || plan->rotary_dim > kD || plan->rotary_dim % 16 ||
-        (plan->layout != SPECACHE_ROTARY_HALF && plan->layout != SPECACHE_ROTARY_INTERLEAVED))
-        return fail_without_context(SPECACHE_EINVAL, "plan is not one that specache_rotary_plan wrote");
+    if (!plan || !is_plan(*plan)) return fail_without_context(SPECACHE_EINVAL, "plan is not one that specache_rotary_plan wrote");
     if (dtype != SPECACHE_FP16 && dtype != SPECACHE_BF16) return fail_without_context(SPECACHE_EINVAL, "dtype must be SPECACHE_FP16 or SPECACHE_BF16");
     if (batch < 0 || tokens < 0 || n_q_heads < 0 || n_kv_heads < 0) return fail_without_context(SPECACHE_EINVAL, "counts must not be negative");
     if (tokens > (1 << 30)) return fail_without_context(SPECACHE_EINVAL, "too many tokens");

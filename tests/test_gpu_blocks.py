@@ -1,0 +1,238 @@
+"""specache_block_select and specache_block_attend: lists equal to the definition's in 64 bits, attention within its tolerance."""
+import math
+
+import pytest
+import torch
+
+from paper_2503_16163_amd import binding
+from tests.paged import compare, generator, ints, pool, reference, scratch_of, table_of
+
+pytestmark = pytest.mark.gpu
+SCALE = 1 / math.sqrt(128)
+
+
+def bounds_of(k):
+    return torch.stack([k.amin(dim=2), k.amax(dim=2)], dim=2).contiguous()
+
+
+def lists(q, bounds, table, n_of, N_of, page, top, first, recent):
+    """The definition, a row at a time, in 64 bits."""
+    B, Hq, n_all, _ = q.shape
+    P, Hkv = bounds.shape[:2]
+    G = Hq // Hkv
+    out = torch.full((B, Hkv, n_all, top + first + recent), -1, dtype=torch.int32)
+    for b in range(B):
+        n, N = n_of[b], N_of[b]
+        for h in range(Hkv):
+            for i in range(n):
+                p = N - n + i
+                if p < 0:
+                    continue
+                row = table[b, :p // page + 1].long()
+                there = ((row >= 0) & (row < P)).cpu()
+                low, high = (bounds[row.clamp(0, max(P - 1, 0)), h, x].double() for x in (0, 1))
+                score = torch.full((len(row),), -math.inf, dtype=torch.float64, device=q.device)
+                for g in range(h * G, h * G + G):
+                    x = q[b, g, i].double()
+                    one = (x.clamp(min=0) * high + x.clamp(max=0) * low).sum(dim=1)
+                    score = torch.maximum(score, torch.where(torch.isnan(one), -math.inf, one))
+                score = score.cpu()
+                always = [c for c in range(len(row)) if there[c] and (c < first or c > p // page - recent)]
+                rest = sorted((c for c in range(len(row)) if there[c] and c not in set(always)), key=lambda c: (-score[c].item(), c))[:top]
+                ids = sorted(always + rest)
+                out[b, h, i, :len(ids)] = torch.tensor(ids, dtype=torch.int32)
+    return out.cuda()
+
+
+def select(cache, q, kv_tokens, top, first, recent, n_of=None, N_of=None, stream=None):
+    B, Hq, n, _ = q.shape
+    blocks = torch.full((B, cache.config.n_kv_heads, n, top + first + recent), -9, dtype=torch.int32, device="cuda")
+    scratch = scratch_of(binding.block_scratch(cache, B, Hq, n, kv_tokens, top, first, recent))
+    binding.block_select(cache, q, blocks, kv_tokens, top, first, recent, ints(n_of), ints(N_of), scratch, stream)
+    return blocks
+
+
+def attend(cache, q, blocks, kv_tokens, n_of=None, N_of=None, sm_scale=0.0, out=None):
+    B, Hq, n, _ = q.shape
+    out = torch.full(q.shape, 7.0, device="cuda", dtype=q.dtype) if out is None else out
+    scratch = scratch_of(binding.block_scratch(cache, B, Hq, n, kv_tokens, blocks.shape[3]))
+    binding.block_attend(cache, q, out, blocks, kv_tokens, ints(n_of), ints(N_of), sm_scale, scratch)
+    return out
+
+
+def _seen(blocks, page, N_of):
+    def of(b, h):
+        N = N_of[b]
+        seen = torch.zeros((blocks.shape[2], -(-N // page) + 1), dtype=torch.bool, device="cuda")
+        l = blocks[b, h].long()
+        seen.scatter_(1, torch.where((l >= 0) & (l < seen.shape[1]), l, seen.shape[1] - 1), True)
+        seen[:, -1] = False
+        return seen[:, :-1].repeat_interleave(page, dim=1)[:, :N]
+    return of
+
+
+def _make(seed, B, Hq, Hkv, n, N_of, page, dtype, order="heads"):
+    gen = generator(seed)
+    table, pages = table_of(gen, N_of, page, max(-(-max(N_of) // page), 1))
+    k, v = pool(gen, pages, Hkv, page, dtype, order)
+    k = k + torch.randn((pages, Hkv, 1, 128), generator=gen, device="cuda").to(dtype) * 0.5
+    q = torch.randn((B, Hq, n, 128), generator=gen, device="cuda").to(dtype)
+    return q, k, v, bounds_of(k), table
+
+
+SHAPES = [  # B, Hq, Hkv, n, N_of, page, top, first, recent
+    (1, 1, 1, 1, [1], 16, 1, 0, 0), (2, 4, 1, 1, [300, 17], 16, 4, 1, 2), (1, 32, 32, 2, [2000], 16, 20, 1, 4), (3, 8, 2, 1, [5000, 4999, 64], 64, 8, 0, 1),
+    (1, 64, 1, 3, [1000], 32, 5, 2, 0), (2, 20, 1, 2, [700, 555], 128, 2, 1, 1), (1, 3, 3, 20, [900], 16, 7, 1, 2), (2, 8, 2, 33, [600, 40], 32, 3, 0, 0),
+    (1, 8, 4, 1, [20000], 16, 64, 4, 8), (1, 2, 1, 1, [70000], 16, 100, 1, 1), (1, 4, 2, 2, [3000], 256, 1, 0, 0), (2, 4, 2, 1, [800, 90], 16, 0, 2, 3), (1, 2, 2, 1, [500], 16, 200, 3, 3),
+    (1, 16, 1, 17, [333], 64, 2, 0, 1), (1, 48, 2, 2, [900], 16, 9, 1, 1), (1, 2, 1, 1, [150000], 16, 30, 1, 1),
+]
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("B,Hq,Hkv,n,N_of,page,top,first,recent", SHAPES)
+def test_blocks(B, Hq, Hkv, n, N_of, page, top, first, recent, dtype):
+    q, k, v, bounds, table = _make(N_of[0] + n, B, Hq, Hkv, n, N_of, page, dtype, "places" if n % 2 else "heads")
+    cache = binding.Pages(k, v, table, bounds)
+    got = select(cache, q, max(N_of), top, first, recent, None, N_of)
+    assert torch.equal(got, lists(q, bounds, table, [n] * B, N_of, page, top, first, recent))
+    exact, tol = reference(q, k, v, table, [n] * B, N_of, SCALE, _seen(got, page, N_of))
+    compare(attend(cache, q, got, max(N_of), None, N_of), exact, tol, [n] * B)
+
+
+def test_scores_bound_what_the_blocks_hold():
+    """A block that is not chosen holds no score above the bound of the worst one chosen."""
+    q, k, v, bounds, table = _make(4, 1, 4, 1, 1, [1600], 16, torch.bfloat16)
+    got = select(binding.Pages(k, v, table, bounds), q, 1600, 10, 0, 0)[0, 0, 0].tolist()
+    b = bounds[table[0].long(), 0].double()
+    bound = torch.stack([(q[0, g, 0].double().clamp(min=0) * b[:, 1] + q[0, g, 0].double().clamp(max=0) * b[:, 0]).sum(1) for g in range(4)]).amax(0)
+    real = torch.einsum("gc,pjc->pgj", q[0, :, 0].double().cpu(), k[table[0].long(), 0].double().cpu()).amax(dim=(1, 2)).cuda()
+    assert bool((real <= bound).all())
+    worst = bound[got].min()
+    assert all(real[c] <= worst for c in range(100) if c not in got)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_equal_scores_take_the_lower_block(dtype):
+    q, k, v, bounds, table = _make(6, 2, 4, 2, 2, [1600, 1599], 16, dtype)
+    for level in (0, 3, 40):       # all alike, a few above the others, all of either sign
+        some = bounds.clone()
+        some[:] = bounds[:1]
+        some[table[:, :level].long()] = bounds[1]
+        cache = binding.Pages(k, v, table, some)
+        got = select(cache, q, 1600, 11, 1, 2, None, [1600, 1599])
+        assert torch.equal(got, lists(q, some, table, [2, 2], [1600, 1599], 16, 11, 1, 2))
+    zero = torch.zeros_like(bounds)
+    zero[::2] *= -1.0
+    cache = binding.Pages(k, v, table, zero)
+    assert torch.equal(select(cache, q, 1600, 5, 0, 1, None, [1600, 1599]), lists(q, zero, table, [2, 2], [1600, 1599], 16, 5, 0, 1))
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_neighbouring_scores(dtype):
+    """Blocks that differ in the last bit of one channel, and sums whose addends differ by 2^20: what binary32 sums would confuse."""
+    q, k, v, bounds, table = _make(7, 1, 2, 1, 1, [3200], 16, dtype)
+    some = bounds[:1].repeat(bounds.shape[0], 1, 1, 1)
+    some[:, :, :, 5] = 512.0
+    some[:, :, :, 6] = -512.0
+    q[:, :, :, 5] = q[:, :, :, 6] = 100.0
+    q[:, :, :, 9] = 2.0 ** -10
+    steps = torch.randint(0, 100, (bounds.shape[0], 1), generator=generator(1), device="cuda")
+    some[:, :, 0, 9] = some[:, :, 1, 9] = (1 + steps * 2.0 ** -7).to(dtype)
+    got = select(binding.Pages(k, v, table, some), q, 3200, 40, 0, 0)
+    assert torch.equal(got, lists(q, some, table, [1], [3200], 16, 40, 0, 0))
+
+
+@pytest.mark.parametrize("n,n_of,N_of", [(1, [1, 0, 1, 1], [700, 5, 0, 1]), (3, [3, 3, 2, 0], [2, 1, 900, 77]), (40, [40, 1, 39, 20], [30, 900, 39, 500])])
+def test_ragged_batches_and_missing_pages(n, n_of, N_of):
+    q, k, v, bounds, table = _make(n, 4, 8, 2, n, [912] * 4, 16, torch.bfloat16)
+    table[:, 4] = -1
+    table[1, 20:23] = 2 ** 31 - 1
+    table[2, 0] = k.shape[0]
+    for b in range(4):             # behind a sequence's tokens, anything
+        q[b, :, n_of[b]:] = math.nan
+        for i in range(-(-N_of[b] // 16), 57):
+            if i != 4 and 0 <= table[b, i] < k.shape[0]:
+                k[table[b, i].item()] = math.nan
+                bounds[table[b, i].item()] = math.nan
+    cache = binding.Pages(k, v, table, bounds)
+    for top, first, recent in ((6, 1, 2), (3, 6, 0), (60, 0, 0)):
+        got = select(cache, q, 912, top, first, recent, n_of, N_of)
+        want = lists(q, bounds, table, n_of, N_of, 16, top, first, recent)
+        for b in range(4):
+            assert torch.equal(got[b, :, :n_of[b]], want[b, :, :n_of[b]]) and bool((got[b, :, n_of[b]:] == -9).all())
+        exact, tol = reference(q, k, v, table, n_of, N_of, SCALE, lambda b, h: _seen(want, 16, N_of)(b, h)[:n_of[b]])
+        compare(attend(cache, q, got.clamp(min=-1), 912, n_of, N_of), exact, tol, n_of)
+
+
+def test_bounds_that_are_not_finite():
+    q, k, v, bounds, table = _make(9, 1, 4, 2, 2, [800], 16, torch.float16)
+    bounds[table[0, 3].item(), :, 1, 7] = math.nan
+    bounds[table[0, 5].item(), 0] = math.inf
+    bounds[table[0, 8].item(), :, 0] = -math.inf
+    bounds[table[0, 9].item(), :, 1] = -math.inf
+    q[0, 1, 1, 3] = math.nan
+    for top in (5, 46, 60):
+        assert torch.equal(select(binding.Pages(k, v, table, bounds), q, 800, top, 1, 1), lists(q, bounds, table, [2], [800], 16, top, 1, 1))
+
+
+def test_lists_of_the_callers_own():
+    """In any order, with entries that are no block, a block that is later than the row, and one that counts twice."""
+    q, k, v, bounds, table = _make(10, 2, 4, 2, 2, [500, 77], 16, torch.bfloat16)
+    cache = binding.Pages(k, v, table)
+    blocks = torch.full((2, 2, 2, 9), -1, dtype=torch.int32, device="cuda")
+    blocks[..., 0], blocks[..., 2], blocks[..., 3], blocks[..., 5], blocks[..., 6] = 4, 2, 0, 2 ** 31 - 1, 31
+    blocks[..., 7] = -(2 ** 31)
+    exact, tol = reference(q, k, v, table, [2, 2], [500, 77], SCALE, _seen(blocks, 16, [500, 77]))
+    compare(attend(cache, q, blocks, 500, None, [500, 77]), exact, tol, [2, 2])
+    # twice: as if the block's positions stood there twice
+    twice = torch.tensor([1, 3, 1], dtype=torch.int32, device="cuda").expand(2, 2, 2, 3).contiguous()
+    again = table.clone()
+    again[:, 0] = table[:, 1]      # the same page as a block of its own
+    other = torch.tensor([0, 1, 3], dtype=torch.int32, device="cuda").expand(2, 2, 2, 3).contiguous()
+    got, want = attend(cache, q, twice, 500, None, [500, 77]), attend(binding.Pages(k, v, again), q, other, 500, None, [500, 77])
+    exact, tol = reference(q, k, v, again, [2, 2], [500, 77], SCALE, _seen(other, 16, [500, 77]))
+    compare(got, exact, tol, [2, 2])
+    compare(want, exact, tol, [2, 2])
+    assert bool((attend(cache, q, torch.full_like(twice, -1), 500, None, [500, 77]) == 0).all())
+
+
+def test_all_blocks_are_paged_attention():
+    from tests.paged import attend as whole
+    q, k, v, bounds, table = _make(12, 2, 8, 2, 5, [1000, 300], 32, torch.float16)
+    cache = binding.Pages(k, v, table, bounds)
+    got = select(cache, q, 1000, 32, 0, 0, None, [1000, 300])
+    a, b = attend(cache, q, got, 1000, None, [1000, 300]), whole(cache, q, 1000, 0, None, [1000, 300])
+    exact, tol = reference(q, k, v, table, [5, 5], [1000, 300], SCALE)
+    compare(a, exact, tol, [5, 5])
+    compare(b, exact, tol, [5, 5])
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,n,N,page,top", [(2, 8, 2, 2, 9000, 16, 40), (1, 4, 4, 30, 700, 32, 5)])
+def test_captured_overlapping_and_the_same_every_time(B, Hq, Hkv, n, N, page, top):
+    sets = []
+    for i in range(2):
+        q, k, v, bounds, table = _make(20 + i, B, Hq, Hkv, n, [N] * B, page, torch.bfloat16)
+        cache = binding.Pages(k, v, table, bounds)
+        s = dict(q=q, cache=cache, out=torch.zeros_like(q), scratch=scratch_of(binding.block_scratch(cache, B, Hq, n, N, top, 1, 2)),
+                 blocks=torch.zeros((B, Hkv, n, top + 3), dtype=torch.int32, device="cuda"), N=torch.full((B,), N, dtype=torch.int32, device="cuda"),
+                 stream=torch.cuda.Stream(), graph=torch.cuda.CUDAGraph())
+        torch.cuda.synchronize()
+        with torch.cuda.graph(s["graph"], stream=s["stream"]):
+            binding.block_select(cache, q, s["blocks"], N, top, 1, 2, kv_lengths=s["N"], scratch=s["scratch"])
+            binding.block_attend(cache, q, s["out"], s["blocks"], N, kv_lengths=s["N"], scratch=s["scratch"])
+        sets.append(s)
+    for turn in range(3):
+        for s in sets:
+            s["q"].copy_(torch.randn_like(s["q"]))
+            s["N"].fill_(N - 13 * turn)
+        want = []
+        for s in sets:
+            blocks = select(s["cache"], s["q"], N, top, 1, 2, N_of=s["N"].tolist())
+            want.append((blocks, attend(s["cache"], s["q"], blocks, N, N_of=s["N"].tolist())))
+        torch.cuda.synchronize()
+        for s in sets:
+            with torch.cuda.stream(s["stream"]):
+                s["graph"].replay()
+        torch.cuda.synchronize()
+        for s, (blocks, out) in zip(sets, want):
+            assert torch.equal(s["blocks"], blocks) and torch.equal(s["out"], out)
