@@ -70,9 +70,9 @@ __device__ __forceinline__ Row row_of(const PagedArgs& a, const Job& j, int i) {
 
 // Which work the workgroup has; false: none.
 template <bool LISTED, int TILE, int ROWS>
-__device__ __forceinline__ bool job_of(const PagedArgs& a, Job& j) {
+__device__ __forceinline__ bool job_of(const PagedArgs& a, bool prefix, Job& j) {
     int chunk, chunks;
-    j.prefix = !LISTED && (int)blockIdx.x < a.prefix_groups;
+    j.prefix = prefix;
     j.token = 0;
     if (j.prefix) {
         const int id = blockIdx.x, tile = id % a.prefix_row_tiles;
@@ -132,14 +132,12 @@ __device__ __forceinline__ bool job_of(const PagedArgs& a, Job& j) {
 }
 
 // Where the positions of tiles are: tile i_first + k * STEP, its GRANULES granules of 16, for the next 64 granules at a time.
-template <int GRANULES>
-struct Granules {
-    int page[GRANULES], pos0[GRANULES];
-    uint32_t edge, wave_edge;         // granules that some row (of the wave) does not see all of
+struct Edges {
+    uint32_t edge, wave_edge;         // of a tile's granules those that some row (of the wave) does not see all of
 };
 template <bool LISTED, int GRANULES>
 struct Directory {
-    static constexpr int kTiles = 64 / GRANULES;
+    static constexpr int kTiles = 64 / GRANULES, kGranules = GRANULES;
     const int32_t* table;
     const int32_t* list;
     int log2, n_pages, slots, begin, end, i_first, step, lane;
@@ -171,20 +169,50 @@ struct Directory {
         edge = __ballot(pos0 + 15 > first);
         wave_edge = __ballot(pos0 + 15 > wave_first);
     }
-    __device__ __forceinline__ Granules<GRANULES> at(int k) {
-        if (k - k0 >= kTiles) load(k);
-        Granules<GRANULES> g;
-        const int l = (k - k0) * GRANULES;
+    __device__ __forceinline__ void one(int k, int granule, int& p, int& x) const {
+        const int l = (k - k0) * GRANULES + granule;
+        p = __builtin_amdgcn_readlane(page, l);
+        x = __builtin_amdgcn_readlane(pos0, l);
+    }
+    __device__ __forceinline__ void positions(int k, int (&x)[GRANULES]) const {
 #pragma unroll
-        for (int i = 0; i < GRANULES; ++i) {
-            g.page[i] = __builtin_amdgcn_readlane(page, l + i);
-            g.pos0[i] = __builtin_amdgcn_readlane(pos0, l + i);
-        }
-        g.edge = (uint32_t)(edge >> l) & ((1u << GRANULES) - 1);
-        g.wave_edge = (uint32_t)(wave_edge >> l) & ((1u << GRANULES) - 1);
-        return g;
+        for (int i = 0; i < GRANULES; ++i) x[i] = __builtin_amdgcn_readlane(pos0, (k - k0) * GRANULES + i);
+    }
+    __device__ __forceinline__ void tile(int k, int (&p)[GRANULES], int (&x)[GRANULES]) const {
+#pragma unroll
+        for (int i = 0; i < GRANULES; ++i) one(k, i, p[i], x[i]);
+    }
+    __device__ __forceinline__ Edges edges(int k) const {
+        const int l = (k - k0) * GRANULES;
+        constexpr uint32_t kAll = (1u << GRANULES) - 1;
+        return Edges{(uint32_t)(edge >> l) & kAll, (uint32_t)(wave_edge >> l) & kAll};
     }
 };
+
+// LOADS times 16 bytes to each lane's place (1024 bytes in order of lanes) from `lds` on, from base + at[i].  The compiler is not told which part of LDS this
+// writes: it would wait for all that travels in front of some reads of what is there already.  So the kernels wait themselves, and tell it where memory may
+// have changed.  (M0, the place in LDS, is left as it was.)
+template <int LOADS>
+__device__ __forceinline__ void load_to_lds(uint32_t lds, const uint32_t (&at)[LOADS], const char* base) {
+    uint32_t m0;
+    if constexpr (LOADS == 4)
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %6\n\t"
+                     "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %6\n\t"
+                     "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, %6\n\t"
+                     "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %5, %6\n\ts_mov_b32 m0, %0"
+                     : "=&s"(m0) : "s"(lds), "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "s"(base) : "memory", "scc");
+    else {
+        static_assert(LOADS == 2, "two or four loads");
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %4\n\t"
+                     "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %4\n\ts_mov_b32 m0, %0"
+                     : "=&s"(m0) : "s"(lds), "v"(at[0]), "v"(at[1]), "s"(base) : "memory", "scc");
+    }
+}
+template <int COUNT>
+__device__ __forceinline__ void wait_loads() {   // until no more than COUNT loads are on their way
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COUNT) : "memory");
+}
+__device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }   // of LDS
 
 // One wave's loads of keys or values of a granule: LOADS times 4 positions from position 4 * LOADS * part of it on, to LDS in the order that Rows reads.
 template <bool KEYS, int LOADS>
@@ -208,19 +236,16 @@ struct PageFetch {
         return base + page * page_bytes + (int64_t)((pos0 & ((1 << log2) - 1)) * (uint64_t)place_bytes);
     }
     // Positions from `end` on are the last one before it again (no row sees them, but they are finite if it is).
-    __device__ __forceinline__ void operator()(int page, int pos0, int end, char* lds) const {
+    __device__ __forceinline__ void operator()(int page, int pos0, int end, uint32_t lds) const {
         const char* from = granule(page, pos0);
-        char* to = lds + 4 * LOADS * part * kRowBytes16;
+        const uint32_t to = lds + 4 * LOADS * part * kRowBytes16;
         if (pos0 + 16 <= end || pos0 == kHidden) {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i)
-                __builtin_amdgcn_global_load_lds((global_void*)(from + at[i]), (lds_void*)(to + 4 * i * kRowBytes16), 16, 0, 0);
+            load_to_lds(to, at, from);
         } else {
+            uint32_t held[LOADS];
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const uint32_t r = min(position(i), end - 1 - pos0);
-                __builtin_amdgcn_global_load_lds((global_void*)(from + (r * place_bytes + piece(i))), (lds_void*)(to + 4 * i * kRowBytes16), 16, 0, 0);
-            }
+            for (int i = 0; i < LOADS; ++i) held[i] = min(position(i), end - 1 - pos0) * place_bytes + piece(i);
+            load_to_lds(to, held, from);
         }
     }
 };
@@ -253,6 +278,19 @@ struct PagedRows : Rows<BF16, BLOCKS> {
                     if ((x & kExponents<BF16> & 0xFFFFu) == (kExponents<BF16> & 0xFFFFu) && pos0 + j <= Base::seen.last) Base::o[dt][i] += widen16<BF16>(x);
                 }
     }
+    template <class D, class F>
+    __device__ void give_odd_values(D& directory, const F& fetch_values, int n, int end) {
+        directory.load(0);
+        for (int k = 0; k < n; ++k) {
+            if (k - directory.k0 >= D::kTiles) directory.load(k);
+            if (!directory.edges(k).edge) continue;
+            for (int i = 0; i < D::kGranules; ++i) {
+                int page, pos0;
+                directory.one(k, i, page, pos0);
+                if (pos0 != kHidden) give_odd_granule(fetch_values.granule(page, pos0), fetch_values.place_bytes, pos0, end);
+            }
+        }
+    }
     // the two halves' sums and what they saw, together
     __device__ __forceinline__ void finish() {
         Base::l += other_half(Base::l);
@@ -267,24 +305,28 @@ __device__ __forceinline__ int least_of_wave(int v) {
     return __builtin_amdgcn_readfirstlane(v);
 }
 
+constexpr int kTileBytes = 64 * kRowBytes16;   // of keys, or of values
+constexpr int kLds = 4 * kTileBytes;
+
+__device__ __forceinline__ uint32_t lds_address(const char* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }
+
+template <bool BF16>
+__device__ __forceinline__ const uint16_t* query_of(const PagedArgs& a, const Row& row) {
+    return (const uint16_t*)a.q.data + row.b * a.q.batch + row.head * a.q.head + row.token * a.q.token;
+}
+
 // Rows of more than a wave: the waves of a workgroup have rows of their own and share tiles of 64 positions, which travel to LDS while the one before is worked on.
 template <bool BF16, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void paged_tile_kernel(PagedArgs a) {
+__device__ __forceinline__ void tile_job(const PagedArgs& a, bool prefix, char* lds, int* least, int* any_dropped) {
     constexpr int TILE = 64, ROWS = WAVES * kWaveRows, LOADS = 16 / WAVES, PARTS = 4 / LOADS;
-    __shared__ __align__(1024) char keys_even[TILE * kRowBytes16];
-    __shared__ __align__(1024) char keys_odd[TILE * kRowBytes16];
-    __shared__ __align__(1024) char values_even[TILE * kRowBytes16];
-    __shared__ __align__(1024) char values_odd[TILE * kRowBytes16];
-    __shared__ int any_dropped, least[WAVES];
-
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     Job j;
-    if (!job_of<false, TILE, ROWS>(a, j)) return;
+    if (!job_of<false, TILE, ROWS>(a, prefix, j)) return;
     const int i_row = wave * kWaveRows + lane % 32;
     const Row row = row_of<false>(a, j, i_row);
     int first, wave_first, wave_last;
-    if (threadIdx.x == 0) any_dropped = 0;
-    if (j.prefix) {
+    if (threadIdx.x == 0) *any_dropped = 0;
+    if (prefix) {
         wave_first = least_of_wave<32>(row.last);
         wave_last = j.end;
         if (lane == 0) least[wave] = wave_first;
@@ -303,98 +345,90 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_tile_kernel(PagedArgs a) 
     PagedRows<BF16, TILE / 32> rs;
     rs.seen = Seen{row.last, 0, 0};
     const int granule = wave / PARTS;      // of a tile, whose keys and values the wave fetches (a part of)
+    const uint32_t room = lds_address(lds) + granule * 16 * kRowBytes16;
     Directory<false, 4> directory(a, j, j.i_begin, 1, lane, first, wave_first);
     const PageFetch<true, LOADS> fetch_keys(a.pages.k, j.h, a.pages.log2, wave % PARTS, lane);
     const PageFetch<false, LOADS> fetch_values(a.pages.v, j.h, a.pages.log2, wave % PARTS, lane);
-    rs.start((const uint16_t*)a.q.data + row.b * a.q.batch + row.head * a.q.head + row.token * a.q.token, lane, a.scale);
+    rs.start(query_of<BF16>(a, row), lane, a.scale);
     const int n = j.i_end - j.i_begin;
-    Granules<4> here;
-    const auto fetch = [&](const Granules<4>& g, char* keys, char* values) __attribute__((always_inline)) {
-        const int page = granule == 0 ? g.page[0] : granule == 1 ? g.page[1] : granule == 2 ? g.page[2] : g.page[3];
-        const int pos0 = granule == 0 ? g.pos0[0] : granule == 1 ? g.pos0[1] : granule == 2 ? g.pos0[2] : g.pos0[3];
-        fetch_keys(page, pos0, j.end, keys + granule * 16 * kRowBytes16);
-        fetch_values(page, pos0, j.end, values + granule * 16 * kRowBytes16);
+    const auto fetch = [&](int k, int buffer) __attribute__((always_inline)) {
+        int page, pos0;
+        directory.one(k, granule, page, pos0);
+        fetch_keys(page, pos0, j.end, room + buffer * kTileBytes);
+        fetch_values(page, pos0, j.end, room + (2 + buffer) * kTileBytes);
     };
+    Edges here;
+    directory.load(0);                     // (and the queries are there when it is)
     if (n > 0) {
-        directory.load(0);
-        here = directory.at(0);
-        fetch(here, keys_even, values_even);
+        here = directory.edges(0);
+        fetch(0, 0);
     }
-    const auto step = [&](int k, char* keys, char* values, char* next_keys, char* next_values) __attribute__((always_inline)) {
-        Granules<4> next = here;
-        __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
-        if (here.edge && drop_odd_values<BF16, LOADS>(values, wave, lane)) any_dropped = 1;
+    const auto step = [&](int k, int buffer) __attribute__((always_inline)) {
+        char* keys = lds + buffer * kTileBytes;
+        char* values = lds + (2 + buffer) * kTileBytes;
+        wait_loads<0>();
+        if (here.edge && drop_odd_values<BF16, LOADS>(values, wave, lane)) *any_dropped = 1;
         __syncthreads();
+        // some of the wave's rows see the tile
+        const bool seen = j.begin + (j.i_begin + k) * TILE <= wave_last;
+        const uint32_t wave_edge = here.wave_edge;
+        int pos0[4];
+        if (wave_edge) directory.positions(k, pos0);
         if (k + 1 < n) {
-            next = directory.at(k + 1);
-            fetch(next, next_keys, next_values);
+            if (k + 1 - directory.k0 >= directory.kTiles) directory.load(k + 1);
+            here = directory.edges(k + 1);
+            fetch(k + 1, buffer ^ 1);
         }
-        if (j.begin + (j.i_begin + k) * TILE <= wave_last) {   // some of the wave's rows see the tile
-            rs.scores(keys);
-            // the first reads ahead of the products, then one beside each
-            __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+        if (!seen) return;
+        rs.scores(keys);
+        // the first reads ahead of the products, then one beside each
+        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
 #pragma unroll
-            for (int i = 0; i < 10; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            }
-            __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
-            if (here.wave_edge) rs.hide(here.pos0);
-            else rs.saw = true;
-            rs.move_maximum(a.scale);
-            rs.weights();
-            rs.add_values(values);
-            // the first step's weights, then the others' beside the products
-            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-            __builtin_amdgcn_sched_group_barrier(0x002, 28, 0);
-#pragma unroll
-            for (int i = 0; i < 12; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-                __builtin_amdgcn_sched_group_barrier(0x002, 7, 0);
-            }
-            __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+        for (int i = 0; i < 10; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
-        here = next;
+        __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
+        if (wave_edge) rs.hide(pos0);
+        else rs.saw = true;
+        rs.move_maximum(a.scale);
+        rs.weights();
+        rs.add_values(values);
+        // the first step's weights, then the others' beside the products
+        __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 28, 0);
+#pragma unroll
+        for (int i = 0; i < 12; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 7, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
     };
     for (int k = 0; k < n; k += 2) {
-        step(k, keys_even, values_even, keys_odd, values_odd);
-        if (k + 1 < n) step(k + 1, keys_odd, values_odd, keys_even, values_even);
+        step(k, 0);
+        if (k + 1 < n) step(k + 1, 1);
     }
     __syncthreads();
-    if (any_dropped) {
-        directory.load(0);
-        for (int k = 0; k < n; ++k) {
-            const Granules<4> g = directory.at(k);
-            if (g.edge)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (g.pos0[i] != kHidden) rs.give_odd_granule(fetch_values.granule(g.page[i], g.pos0[i]), fetch_values.place_bytes, g.pos0[i], j.end);
-        }
-    }
+    if (*any_dropped) rs.give_odd_values(directory, fetch_values, n, j.end);
     rs.finish();
     if (i_row >= j.rows) return;
-    if (j.prefix || a.parts) rs.store_part(j.prefix ? a.prefix_o : a.own_o, j.prefix ? a.prefix_ml : a.own_ml, j.place + i_row, n > 0);
+    if (prefix || a.parts) rs.store_part(prefix ? a.prefix_o : a.own_o, prefix ? a.prefix_ml : a.own_ml, j.place + i_row, n > 0);
     else {
         rs.seen.last = rs.m != -INFINITY ? 0 : -1;   // (whether the row saw anything)
         rs.store((uint16_t*)a.out.data + row.b * a.out.batch + row.head * a.out.head + row.token * a.out.token);
     }
 }
 
-// Waves by themselves: up to 32 rows, 32 positions at a time, the next ones on their way while a wave works on these; the waves of a workgroup take a
-// chunk's tiles in turn and join their results in LDS at its end.
+// Waves by themselves: up to 32 rows, 32 positions at a time; as soon as a tile's keys have been read the next ones travel to their place, and so do the values.
+// The waves of a workgroup take a chunk's tiles in turn and join their results in LDS at its end.
 template <bool BF16, bool LISTED, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void paged_step_kernel(PagedArgs a) {
-    constexpr int TILE = 32, BYTES = TILE * kRowBytes16, HALF = BYTES / 2;
-    __shared__ __align__(1024) char keys_even[WAVES * BYTES];
-    __shared__ __align__(1024) char keys_odd[WAVES * BYTES];
-    __shared__ __align__(1024) char values_even[WAVES * BYTES];
-    __shared__ __align__(1024) char values_odd[WAVES * BYTES];
-    __shared__ float2 joined[WAVES][kWaveRows];
-
+__device__ __forceinline__ void step_job(const PagedArgs& a, bool prefix, char* lds, float2 (*joined)[kWaveRows]) {
+    constexpr int TILE = 32, HALF = TILE / 2 * kRowBytes16, OWN = kLds / WAVES;
+    static_assert(OWN >= 2 * TILE * kRowBytes16 && OWN >= kWaveRows * kD * 4, "a wave's part of LDS holds a tile, and its sums");
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     Job j;
-    if (!job_of<LISTED, TILE, kWaveRows>(a, j)) return;
+    if (!job_of<LISTED, TILE, kWaveRows>(a, prefix, j)) return;
     const Row row = row_of<LISTED>(a, j, lane % 32);
     const int first = least_of_wave<32>(row.last);
     const int n = max(0, (j.i_end - j.i_begin - wave + WAVES - 1) / WAVES);   // tiles of this wave
@@ -404,65 +438,54 @@ __global__ __launch_bounds__(64 * WAVES) void paged_step_kernel(PagedArgs a) {
     Directory<LISTED, 2> directory(a, j, j.i_begin + wave, WAVES, lane, first, first);
     const PageFetch<true, 4> fetch_keys(a.pages.k, j.h, a.pages.log2, 0, lane);
     const PageFetch<false, 4> fetch_values(a.pages.v, j.h, a.pages.log2, 0, lane);
+    char* const keys = lds + wave * OWN;
+    char* const values = keys + TILE * kRowBytes16;
+    const uint32_t keys_at = lds_address(keys), values_at = lds_address(values);
     bool dropped = false;
-    Granules<2> here;
-    const auto fetch = [&](const Granules<2>& g, char* keys, char* values) __attribute__((always_inline)) {
-        fetch_keys(g.page[0], g.pos0[0], j.end, keys + wave * BYTES);
-        fetch_keys(g.page[1], g.pos0[1], j.end, keys + wave * BYTES + HALF);
-        fetch_values(g.page[0], g.pos0[0], j.end, values + wave * BYTES);
-        fetch_values(g.page[1], g.pos0[1], j.end, values + wave * BYTES + HALF);
-    };
+    int page[2], pos0[2];
+    rs.start(query_of<BF16>(a, row), lane, a.scale);   // (there when the directory is)
+    directory.load(0);
     if (n > 0) {
-        directory.load(0);
-        here = directory.at(0);
-        fetch(here, keys_even, values_even);
+        directory.tile(0, page, pos0);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) fetch_keys(page[i], pos0[i], j.end, keys_at + i * HALF);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) fetch_values(page[i], pos0[i], j.end, values_at + i * HALF);
     }
-    rs.start((const uint16_t*)a.q.data + row.b * a.q.batch + row.head * a.q.head + row.token * a.q.token, lane, a.scale);
-    const auto step = [&](int k, char* keys, char* values, char* next_keys, char* next_values) __attribute__((always_inline)) {
+    for (int k = 0; k < n; ++k) {
         const bool more = k + 1 < n;
-        Granules<2> next = here;
-        if (more) next = directory.at(k + 1);
-        asm volatile("" ::: "memory");        // (the buffers' last reads are behind)
-        __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+        const bool edge = directory.edges(k).edge;
+        wait_loads<8>();
+        rs.scores(keys);
+        wait_reads();
+        int next_page[2] = {0, 0}, next_pos0[2] = {0, 0};
         if (more) {
-            fetch(next, next_keys, next_values);
-            __builtin_amdgcn_s_waitcnt(0x4F78);   // vmcnt(24): this tile's keys are there
-        } else {
-            __builtin_amdgcn_s_waitcnt(0x0F78);   // vmcnt(8)
+            if (k + 1 - directory.k0 >= directory.kTiles) directory.load(k + 1);
+            directory.tile(k + 1, next_page, next_pos0);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) fetch_keys(next_page[i], next_pos0[i], j.end, keys_at + i * HALF);
         }
-        asm volatile("" ::: "memory");
-        rs.scores(keys + wave * BYTES);
-        if (here.edge) rs.hide(here.pos0);
+        if (edge) rs.hide(pos0);
         else rs.saw = true;
         rs.move_maximum(a.scale);
         rs.weights();
-        asm volatile("" ::: "memory");
-        if (more) __builtin_amdgcn_s_waitcnt(0x4F70);   // vmcnt(16): and its values
-        else __builtin_amdgcn_s_waitcnt(0x0F70);
-        asm volatile("" ::: "memory");
-        if (here.edge) dropped |= drop_odd_values<BF16, 8>(values + wave * BYTES, 0, lane);
-        rs.add_values(values + wave * BYTES);
-        here = next;
-    };
-    for (int k = 0; k < n; k += 2) {
-        step(k, keys_even, values_even, keys_odd, values_odd);
-        if (k + 1 < n) step(k + 1, keys_odd, values_odd, keys_even, values_even);
-    }
-    if (__ballot(dropped)) {
-        directory.load(0);
-        for (int k = 0; k < n; ++k) {
-            const Granules<2> g = directory.at(k);
-            if (g.edge)
+        if (more) wait_loads<8>();
+        else wait_loads<0>();
+        if (edge) dropped |= drop_odd_values<BF16, 8>(values, 0, lane);
+        rs.add_values(values);
+        wait_reads();
+        if (more) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    if (g.pos0[i] != kHidden) rs.give_odd_granule(fetch_values.granule(g.page[i], g.pos0[i]), fetch_values.place_bytes, g.pos0[i], j.end);
+            for (int i = 0; i < 2; ++i) {
+                page[i] = next_page[i], pos0[i] = next_pos0[i];
+                fetch_values(page[i], pos0[i], j.end, values_at + i * HALF);
+            }
         }
     }
+    if (__ballot(dropped)) rs.give_odd_values(directory, fetch_values, n, j.end);
     rs.finish();
 
-    // every wave's sums to LDS (a row's channels turned by 4 per row: no two rows of a group of lanes meet in a bank), then four channels per thread
-    __syncthreads();
-    char* const room = wave == 0 ? keys_even : wave == 1 ? keys_odd : wave == 2 ? values_even : values_odd;
+    // every wave's sums to its own part of LDS (a row's channels turned by 4 per row: no two rows of a group of lanes meet in a bank), then four channels per thread
     const int mine = lane % 32;
     if (mine < j.rows) {
         if (lane < 32) joined[wave][mine] = float2{rs.m, rs.l};
@@ -470,7 +493,7 @@ __global__ __launch_bounds__(64 * WAVES) void paged_step_kernel(PagedArgs a) {
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                *(float4*)(room + (mine * kD + (32 * dt + 8 * i + 4 * rs.half + 4 * mine) % kD) * 4) =
+                *(float4*)(keys + (mine * kD + (32 * dt + 8 * i + 4 * rs.half + 4 * mine) % kD) * 4) =
                     float4{rs.o[dt][4 * i], rs.o[dt][4 * i + 1], rs.o[dt][4 * i + 2], rs.o[dt][4 * i + 3]};
     }
     __syncthreads();
@@ -484,14 +507,13 @@ __global__ __launch_bounds__(64 * WAVES) void paged_step_kernel(PagedArgs a) {
         for (int w = 0; w < WAVES; ++w) {
             const float2 ml = joined[w][r];
             const float f = __builtin_amdgcn_exp2f(ml.x - fmaxf(m, kNever));
-            const char* from = w == 0 ? keys_even : w == 1 ? keys_odd : w == 2 ? values_even : values_odd;
-            const float4 x = *(const float4*)(from + (r * kD + (c + 4 * r) % kD) * 4);
+            const float4 x = *(const float4*)(lds + w * OWN + (r * kD + (c + 4 * r) % kD) * 4);
             l = fmaf(f, ml.y, l);
             o.x = fmaf(f, x.x, o.x), o.y = fmaf(f, x.y, o.y), o.z = fmaf(f, x.z, o.z), o.w = fmaf(f, x.w, o.w);
         }
-        if (j.prefix || a.parts) {
-            float* po = j.prefix ? a.prefix_o : a.own_o;
-            float* pm = j.prefix ? a.prefix_ml : a.own_ml;
+        if (prefix || a.parts) {
+            float* po = prefix ? a.prefix_o : a.own_o;
+            float* pm = prefix ? a.prefix_ml : a.own_ml;
             if (c == 0) *(float2*)(pm + 2 * (j.place + r)) = float2{m, l};
             *(float4*)(po + (j.place + r) * kD + c) = o;
         } else {
@@ -501,6 +523,22 @@ __global__ __launch_bounds__(64 * WAVES) void paged_step_kernel(PagedArgs a) {
             *(uint2v*)(out + c) = uint2v{pack16<BF16>(o.x * by, o.y * by), pack16<BF16>(o.z * by, o.w * by)};
         }
     }
+}
+
+// The prefix's work and the sequences' own in one launch, so that the one fills what the other leaves of the chip.
+enum { kSteps, kTilesAndSteps, kTiles };      // of the prefix and the own positions
+template <bool BF16, bool LISTED, int KIND, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void paged_kernel(PagedArgs a) {
+    __shared__ __align__(1024) char lds[kLds];
+    __shared__ union {
+        float2 joined[WAVES][kWaveRows];
+        struct {
+            int any_dropped, least[WAVES];
+        };
+    } more;
+    const bool prefix = !LISTED && (int)blockIdx.x < a.prefix_groups;
+    if (KIND == kTiles || (KIND == kTilesAndSteps && prefix)) tile_job<BF16, WAVES>(a, prefix, lds, more.least, &more.any_dropped);
+    else if constexpr (KIND != kTiles) step_job<BF16, LISTED, WAVES>(a, prefix, lds, more.joined);
 }
 
 // The partial results of a row, joined: those of the prefix, then those of its own positions; two channels per lane, the parts dealt to the waves of a
@@ -578,30 +616,28 @@ __global__ __launch_bounds__(64 * kMergeWaves) void paged_merge_kernel(PagedArgs
     *(uint32_t*)(to + 2 * lane) = pack16<BF16>(x * by, y * by);
 }
 
-constexpr int kStepWaves = 2;
+constexpr int kStepWaves = 4;
 constexpr int64_t kMostGroups = INT32_MAX / 512;   // a launch's threads are counted in 32 bits
 constexpr int64_t kStepsAtOnce = 512;
-enum { kStep, kTile4, kTile8 };
 // how a kind of work (the prefix's, the sequences' own) is laid out
 struct Part {
-    int kernel = kStep, row_tiles = 1, item_rows = 1, chunks = 0;
+    int row_tiles = 1, item_rows = 1, chunks = 0;
     int64_t items = 0;
     int64_t groups() const { return items * chunks; }
     int64_t places() const { return items * chunks * item_rows; }
 };
 struct Plan {
     Part prefix, own;
-    int shared = 0;
+    int shared = 0, kind = kSteps, waves = kStepWaves;
     bool parts = false;
     int64_t scratch = 0;
 };
 
-// `units` of `rows` rows each over at most `most` positions
-Part part_of(int64_t units, int64_t rows, int64_t most, bool listed) {
+// `units` of `rows` rows each over at most `most` positions: by waves by themselves, or (waves of a workgroup) in tiles
+Part part_of(int64_t units, int64_t rows, int64_t most, int waves) {
     Part p;
     int64_t chunks = 1;
-    if (rows <= kWaveRows || listed) {
-        p.kernel = kStep;
+    if (!waves) {
         p.item_rows = (int)std::min<int64_t>(std::max<int64_t>(rows, 1), kWaveRows);
         p.row_tiles = (int)((rows + kWaveRows - 1) / kWaveRows);
         p.items = units * p.row_tiles;
@@ -611,11 +647,10 @@ Part part_of(int64_t units, int64_t rows, int64_t most, bool listed) {
             chunks = std::min({chunks, tiles / kStepWaves, std::max<int64_t>(256, tiles / 64)});
         }
     } else {
-        p.kernel = most >= 2048 && rows > 128 ? kTile8 : kTile4;
-        p.item_rows = p.kernel == kTile8 ? 256 : 128;
+        p.item_rows = waves * kWaveRows;
         p.row_tiles = (int)((rows + p.item_rows - 1) / p.item_rows);
         p.items = units * p.row_tiles;
-        if (p.items) chunks = std::min<int64_t>((p.kernel == kTile8 ? 256 : 512) / p.items, (most + 63) / 64 / 4);
+        if (p.items) chunks = std::min<int64_t>((waves == 8 ? 256 : 512) / p.items, (most + 63) / 64 / 4);
     }
     p.chunks = (int)std::max<int64_t>(chunks, 1);
     return p;
@@ -648,8 +683,12 @@ int plan_of(const specache_pages* cache, const specache_paged_config* c, Plan& p
     const int G = c->n_q_heads / cache->n_kv_heads;
     const int64_t rows = (int64_t)c->q_tokens * G;
     if (c->batch > 1 && rows) p.shared = std::min(c->shared_tokens, c->kv_tokens) / cache->page_tokens * cache->page_tokens;
-    if (p.shared) p.prefix = part_of(cache->n_kv_heads, c->batch * rows, p.shared, false);
-    p.own = part_of(rows ? (int64_t)c->batch * cache->n_kv_heads : 0, rows, c->kv_tokens - p.shared, false);
+    if (rows > kWaveRows) {
+        p.kind = kTiles;
+        p.waves = std::max(p.shared, c->kv_tokens - p.shared) >= 2048 && rows > 128 ? 8 : 4;
+    } else if (p.shared && c->batch * rows > kWaveRows) p.kind = kTilesAndSteps;
+    if (p.shared) p.prefix = part_of(cache->n_kv_heads, c->batch * rows, p.shared, p.kind == kSteps ? 0 : p.waves);
+    p.own = part_of(rows ? (int64_t)c->batch * cache->n_kv_heads : 0, rows, c->kv_tokens - p.shared, p.kind == kTiles ? p.waves : 0);
     return finish_plan(p, c->batch * rows * cache->n_kv_heads);
 }
 
@@ -671,7 +710,7 @@ int plan_of_blocks(const specache_pages* cache, const specache_block_config* c, 
     if (int rc = check_blocks(cache, c)) return rc;
     const int64_t slots = (int64_t)c->top + c->first + c->recent, blocks = (c->kv_tokens + cache->page_tokens - 1) / cache->page_tokens;
     const int64_t units = (int64_t)c->batch * c->q_tokens * cache->n_kv_heads;
-    p.own = part_of(units, c->n_q_heads / cache->n_kv_heads, std::min(slots, blocks) * cache->page_tokens, true);
+    p.own = part_of(units, c->n_q_heads / cache->n_kv_heads, std::min(slots, blocks) * cache->page_tokens, 0);
     return finish_plan(p, units * (c->n_q_heads / cache->n_kv_heads));
 }
 
@@ -703,6 +742,7 @@ PagedArgs args_of(const specache_pages& cache, const Plan& p, int batch, int n_q
     a.q_tokens = q_tokens;
     a.kv_tokens = cache.n_pages ? kv_tokens : 0;
     a.shared = cache.n_pages ? p.shared : 0;
+    a.prefix_groups = (int)p.prefix.groups();
     a.own_chunks = p.own.chunks;
     a.own_row_tiles = p.own.row_tiles;
     a.own_rows = p.own.item_rows;
@@ -715,14 +755,6 @@ PagedArgs args_of(const specache_pages& cache, const Plan& p, int batch, int n_q
     return a;
 }
 
-template <bool BF16>
-void launch_part(int kernel, int64_t groups, const PagedArgs& a, hipStream_t stream) {
-    const dim3 grid((unsigned)groups);
-    if (kernel == kStep) hipLaunchKernelGGL((paged_step_kernel<BF16, false, kStepWaves>), grid, dim3(64 * kStepWaves), 0, stream, a);
-    else if (kernel == kTile4) hipLaunchKernelGGL((paged_tile_kernel<BF16, 4>), grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((paged_tile_kernel<BF16, 8>), grid, dim3(512), 0, stream, a);
-}
-
 template <bool BF16, bool LISTED>
 void launch_merge(const Plan& p, const PagedArgs& a, hipStream_t stream) {
     if (!p.parts) return;
@@ -731,21 +763,15 @@ void launch_merge(const Plan& p, const PagedArgs& a, hipStream_t stream) {
     else hipLaunchKernelGGL((paged_merge_kernel<BF16, LISTED, kMergeWaves>), dim3((unsigned)a.merge_rows), dim3(64 * kMergeWaves), 0, stream, a);
 }
 
-template <bool BF16>
-void launch(const Plan& p, PagedArgs a, hipStream_t stream) {
-    if (p.shared) {
-        a.prefix_groups = (int)p.prefix.groups();
-        launch_part<BF16>(p.prefix.kernel, p.prefix.groups(), a, stream);
-        a.prefix_groups = 0;
-    }
-    launch_part<BF16>(p.own.kernel, p.own.groups(), a, stream);
-    launch_merge<BF16, false>(p, a, stream);
-}
-
-template <bool BF16>
-void launch_listed(const Plan& p, const PagedArgs& a, hipStream_t stream) {
-    hipLaunchKernelGGL((paged_step_kernel<BF16, true, kStepWaves>), dim3((unsigned)p.own.groups()), dim3(64 * kStepWaves), 0, stream, a);
-    launch_merge<BF16, true>(p, a, stream);
+template <bool BF16, bool LISTED>
+void launch(const Plan& p, const PagedArgs& a, hipStream_t stream) {
+    const dim3 grid((unsigned)(p.prefix.groups() + p.own.groups()));
+    const auto kernel = LISTED || p.kind == kSteps ? paged_kernel<BF16, LISTED, kSteps, kStepWaves>
+                        : p.kind == kTilesAndSteps ? paged_kernel<BF16, false, kTilesAndSteps, kStepWaves>
+                        : p.waves == 8             ? paged_kernel<BF16, false, kTiles, 8>
+                                                   : paged_kernel<BF16, false, kTiles, 4>;
+    hipLaunchKernelGGL(kernel, grid, dim3(64 * p.waves), 0, stream, a);
+    launch_merge<BF16, LISTED>(p, a, stream);
 }
 
 int check_call(const specache_pages& cache, const Plan& p, const specache_view* q, const specache_view* out, int batch, int n_q_heads, int q_tokens,
@@ -785,8 +811,8 @@ int specache_paged_attend(const specache_pages* cache, const specache_paged_conf
     if (!p.own.items) return SPECACHE_OK;
     if (int rc = check_call(*cache, p, q, out, cfg->batch, cfg->n_q_heads, cfg->q_tokens, cfg->kv_tokens, q_lengths, kv_lengths, scratch, scratch_bytes)) return rc;
     const PagedArgs a = args_of(*cache, p, cfg->batch, cfg->n_q_heads, cfg->q_tokens, cfg->kv_tokens, cfg->sm_scale, q, out, q_lengths, kv_lengths, scratch);
-    if (cache->dtype == SPECACHE_BF16) launch<true>(p, a, (hipStream_t)stream);
-    else launch<false>(p, a, (hipStream_t)stream);
+    if (cache->dtype == SPECACHE_BF16) launch<true, false>(p, a, (hipStream_t)stream);
+    else launch<false, false>(p, a, (hipStream_t)stream);
     return launched();
 }
 
@@ -800,8 +826,8 @@ int specache_block_attend(const specache_pages* cache, const specache_block_conf
     PagedArgs a = args_of(*cache, p, cfg->batch, cfg->n_q_heads, cfg->q_tokens, cfg->kv_tokens, cfg->sm_scale, q, out, q_lengths, kv_lengths, scratch);
     a.blocks = blocks;
     a.slots = cfg->top + cfg->first + cfg->recent;
-    if (cache->dtype == SPECACHE_BF16) launch_listed<true>(p, a, (hipStream_t)stream);
-    else launch_listed<false>(p, a, (hipStream_t)stream);
+    if (cache->dtype == SPECACHE_BF16) launch<true, true>(p, a, (hipStream_t)stream);
+    else launch<false, true>(p, a, (hipStream_t)stream);
     return launched();
 }
 
