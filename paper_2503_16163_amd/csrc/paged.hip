@@ -75,7 +75,7 @@ __device__ __forceinline__ bool job_of(const PagedArgs& a, bool prefix, Job& j) 
     j.prefix = prefix;
     j.token = 0;
     if (j.prefix) {
-        const int id = blockIdx.x, tile = id % a.prefix_row_tiles;
+        const int id = on_one_xcd(blockIdx.x, a.prefix_groups, a.prefix_row_tiles), tile = id % a.prefix_row_tiles;
         chunks = a.prefix_chunks;
         chunk = id / a.prefix_row_tiles % chunks;
         j.h = id / a.prefix_row_tiles / chunks;
@@ -88,7 +88,8 @@ __device__ __forceinline__ bool job_of(const PagedArgs& a, bool prefix, Job& j) 
         j.tiles = (j.end + TILE - 1) / TILE;
         j.place = (((int64_t)j.h * a.prefix_row_tiles + tile) * chunks + chunk) * a.prefix_rows;
     } else {
-        const int id = blockIdx.x - a.prefix_groups, item = id / a.own_chunks;
+        const int index = blockIdx.x - a.prefix_groups;
+        const int id = TILE == 64 ? on_one_xcd(index, gridDim.x - a.prefix_groups, a.own_row_tiles * a.own_chunks) : index, item = id / a.own_chunks;
         const int tile = a.own_row_tiles - 1 - item % a.own_row_tiles;   // the longest first
         int unit = item / a.own_row_tiles;
         chunks = a.own_chunks;
@@ -626,6 +627,7 @@ struct Part {
     int64_t groups() const { return items * chunks; }
     int64_t places() const { return items * chunks * item_rows; }
 };
+constexpr int kMostWaves = 8;
 struct Plan {
     Part prefix, own;
     int shared = 0, kind = kSteps, waves = kStepWaves;
@@ -634,7 +636,7 @@ struct Plan {
 };
 
 // `units` of `rows` rows each over at most `most` positions: by waves by themselves, or (waves of a workgroup) in tiles
-Part part_of(int64_t units, int64_t rows, int64_t most, int waves) {
+Part part_of(int64_t units, int64_t rows, int64_t most, int waves, int64_t at_once = 0) {
     Part p;
     int64_t chunks = 1;
     if (!waves) {
@@ -650,7 +652,7 @@ Part part_of(int64_t units, int64_t rows, int64_t most, int waves) {
         p.item_rows = waves * kWaveRows;
         p.row_tiles = (int)((rows + p.item_rows - 1) / p.item_rows);
         p.items = units * p.row_tiles;
-        if (p.items) chunks = std::min<int64_t>((waves == 8 ? 256 : 512) / p.items, (most + 63) / 64 / 4);
+        if (p.items) chunks = std::min<int64_t>(at_once / p.items, (most + 63) / 64 / 4);
     }
     p.chunks = (int)std::max<int64_t>(chunks, 1);
     return p;
@@ -683,12 +685,14 @@ int plan_of(const specache_pages* cache, const specache_paged_config* c, Plan& p
     const int G = c->n_q_heads / cache->n_kv_heads;
     const int64_t rows = (int64_t)c->q_tokens * G;
     if (c->batch > 1 && rows) p.shared = std::min(c->shared_tokens, c->kv_tokens) / cache->page_tokens * cache->page_tokens;
+    const int64_t tile = kMostWaves * kWaveRows;
+    if (c->batch * ((rows + tile - 1) / tile) * 10 <= (c->batch * rows + tile - 1) / tile * 11) p.shared = 0;
     if (rows > kWaveRows) {
         p.kind = kTiles;
         p.waves = std::max(p.shared, c->kv_tokens - p.shared) >= 2048 && rows > 128 ? 8 : 4;
     } else if (p.shared && c->batch * rows > kWaveRows) p.kind = kTilesAndSteps;
-    if (p.shared) p.prefix = part_of(cache->n_kv_heads, c->batch * rows, p.shared, p.kind == kSteps ? 0 : p.waves);
-    p.own = part_of(rows ? (int64_t)c->batch * cache->n_kv_heads : 0, rows, c->kv_tokens - p.shared, p.kind == kTiles ? p.waves : 0);
+    if (p.shared) p.prefix = part_of(cache->n_kv_heads, c->batch * rows, p.shared, p.kind == kSteps ? 0 : p.waves, p.kind == kTiles ? (p.waves == 8 ? 256 : 512) : 256);
+    p.own = part_of(rows ? (int64_t)c->batch * cache->n_kv_heads : 0, rows, c->kv_tokens - p.shared, p.kind == kTiles ? p.waves : 0, p.waves == 8 ? 256 : 512);
     return finish_plan(p, c->batch * rows * cache->n_kv_heads);
 }
 

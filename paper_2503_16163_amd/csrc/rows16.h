@@ -208,5 +208,18 @@ struct Rows {
     }
 };
 
+// Of `total` workgroups, `per_head` that read the same keys and values (a KV head of a sequence) follow each other on one XCD (workgroups go to the 8 XCDs in
+// turn), whose L2 they share.  Heads are dealt to the XCDs in turn, so that a long sequence of a batch is everybody's (5 prompts of up to 3001 tokens, in
+// stretches of heads 194 us, so 141); of the last ones, fewer than 8, each XCD has a stretch.
+__device__ __forceinline__ int on_one_xcd(int index, int total, int per_head) {
+    const int xcd = index % 8, dealt = total / per_head / 8 * 8 * per_head;
+    if (index < dealt) {
+        const int at = index / 8;
+        return (at / per_head * 8 + xcd) * per_head + at % per_head;
+    }
+    const int left = total - dealt, per_xcd = left / 8, rest = left % 8;
+    return dealt + xcd * per_xcd + min(xcd, rest) + (index - dealt) / 8;
+}
+
 }  // namespace
 }  // namespace specache

@@ -90,19 +90,6 @@ __device__ __forceinline__ bool is_edge(int tile0, int first, int last, int wind
     return tile0 + TILE - 1 > first || (window && tile0 < last - window + 1 && tile0 + TILE > sinks);
 }
 
-// The workgroups of a KV head of a sequence (per_head) follow each other on one XCD (workgroups go to the 8 XCDs in turn), whose L2 they share. Heads
-// are dealt to the XCDs in turn, so that a long sequence of a batch is everybody's (5 prompts of up to 3001 tokens, in stretches of heads 194 us, so 141); of the last ones, fewer
-// than 8, each XCD has a stretch.
-__device__ __forceinline__ int on_one_xcd(int per_head) {
-    const int xcd = blockIdx.x % 8, dealt = gridDim.x / per_head / 8 * 8 * per_head;
-    if ((int)blockIdx.x < dealt) {
-        const int at = blockIdx.x / 8;
-        return (at / per_head * 8 + xcd) * per_head + at % per_head;
-    }
-    const int total = gridDim.x - dealt, per_xcd = total / 8, rest = total % 8;
-    return dealt + xcd * per_xcd + min(xcd, rest) + (blockIdx.x - dealt) / 8;
-}
-
 // Tiles of 64 positions travel to LDS while the one before is worked on; a wave takes 1/WAVES of a tile's keys and values.
 // us, 32 heads over a prompt of 16k tokens: 2165 (1.02 PFLOP/s, the matrix cores busy 0.52 of the time at the clock that random inputs leave; 2130 to 2230 from one card to
 // another), 8 heads of 4 queries over 32k through a window of 4096 1950 to 2140, 256 tokens of 8 heads of 8 behind 32k 250 to 267 and the merge.
@@ -118,7 +105,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tile_kernel(WindowArgs a) {
     __shared__ int any_dropped;
 
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int id = on_one_xcd(SPLIT ? a.row_tiles * a.chunks : a.row_tiles), chunk = SPLIT ? id % a.chunks : 0, item = SPLIT ? id / a.chunks : id;
+    const int id = on_one_xcd(blockIdx.x, gridDim.x, SPLIT ? a.row_tiles * a.chunks : a.row_tiles), chunk = SPLIT ? id % a.chunks : 0, item = SPLIT ? id / a.chunks : id;
     const int b = item / a.row_tiles / a.n_kv_heads, h = item / a.row_tiles % a.n_kv_heads;
     const int row_tile = a.row_tiles - 1 - item % a.row_tiles;   // the longest first
     const int n = length_of(a.q_lengths, b, a.q_tokens), N = length_of(a.kv_lengths, b, a.kv_tokens);
