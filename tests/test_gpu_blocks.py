@@ -142,6 +142,37 @@ def test_neighbouring_scores(dtype):
     assert torch.equal(got, lists(q, some, table, [1], [3200], 16, 40, 0, 0))
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("N,top", [(4000, 30), (9600, 300), (30000, 100), (100000, 600), (300000, 50)])
+def test_many_scores_alike(N, top, dtype):
+    """More blocks near to the last chosen one than are told apart in LDS: all of them equal, in a few steps, or different in their last bits alone."""
+    q, k, v, bounds, table = _make(8, 1, 2, 1, 1, [N], 16, dtype)
+    gen, P = generator(2), bounds.shape[0]
+    one = bounds[:1].repeat(P, 1, 1, 1)
+    steps = one.clone()
+    steps[:, :, :, 4] = torch.randint(-2, 3, (P, 1, 1), generator=gen, device="cuda").to(dtype)
+    close = one.clone()
+    close[:, :, :, 5], close[:, :, :, 6] = 512.0, -512.0
+    close[:, :, :, 9] = (1 + torch.randint(0, 100, (P, 1, 1), generator=gen, device="cuda") * 2.0 ** -7).to(dtype)
+    x = q.clone()
+    x[:, :, :, 5] = x[:, :, :, 6] = 100.0
+    x[:, :, :, 9] = 2.0 ** -10
+    mixed = torch.where((torch.arange(P, device="cuda") % 3 == 0)[:, None, None, None], bounds, one)
+    for queries, some in ((q, one), (q, steps), (x, close), (q, mixed), (q, torch.zeros_like(one))):
+        cache = binding.Pages(k, v, table, some)
+        assert torch.equal(select(cache, queries, N, top, 1, 2), lists(queries, some, table, [1], [N], 16, top, 1, 2))
+
+
+def test_smallest_and_largest_numbers():
+    """Bounds and queries below the smallest normal number, and products beyond the largest of 32 bits."""
+    for dtype, scales in ((torch.float16, (2.0 ** -22, 2.0 ** 14)), (torch.bfloat16, (1e-38, 1e38))):
+        for scale in scales:
+            q, k, v, bounds, table = _make(13, 1, 4, 2, 2, [3200], 16, dtype)
+            some, x = (bounds.double() * scale).to(dtype), (q.double() * scale).to(dtype)
+            for top in (7, 100):
+                assert torch.equal(select(binding.Pages(k, v, table, some), x, 3200, top, 1, 1), lists(x, some, table, [2], [3200], 16, top, 1, 1))
+
+
 @pytest.mark.parametrize("n,n_of,N_of", [(1, [1, 0, 1, 1], [700, 5, 0, 1]), (3, [3, 3, 2, 0], [2, 1, 900, 77]), (40, [40, 1, 39, 20], [30, 900, 39, 500])])
 def test_ragged_batches_and_missing_pages(n, n_of, N_of):
     q, k, v, bounds, table = _make(n, 4, 8, 2, n, [912] * 4, 16, torch.bfloat16)
