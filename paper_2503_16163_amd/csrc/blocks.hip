@@ -3,10 +3,8 @@
 // score(block) = max over the KV head's query heads of  max(q, 0) . most + min(q, 0) . least, where least and most are the block's bounds: a product over 256
 // channels, [max(q, 0), min(q, 0)] by [most, least].  Which block is the last chosen depends on scores next to each other, and a sum in
 // 32 bits would choose differently from one order of additions to another, so the choice is that of sums in 64 bits.  Hardly a block needs them: score_kernel
-// makes all scores on the matrix cores in 32 bits, together with the sums of the addends' magnitudes, which bound their error; select_kernel, a workgroup
-// to a row, finds the last chosen one by its bits from the top, and only where others are nearer to it than the error are those
-// made again in 64 bits.  (All scores in 64 bits on the matrix cores: 19 us instead of 5 for 16 sequences of up to 512 blocks and 8 heads of 4, 52 instead of 12
-// for 256 rows of 313 blocks and 8 heads of 8.)
+// makes all scores on the matrix cores in 32 bits, together with the sums of the addends' magnitudes, which bound their error; select_kernel, a workgroup to a
+// row, counts them in bins and makes those around the last chosen one again in 64 bits.
 #include "pages.h"
 #include "wave_ops.h"
 
@@ -35,7 +33,9 @@ struct BlockArgs {
     uint64_t* keys;                   // [batch][KV head][token][row_blocks]: where a row's scores are all made again
     int batch, G, q_tokens, kv_tokens, top, first, recent;
     int row_blocks;                   // whole tiles
-    int tokens_here, passes, token_groups, splits;
+    int tokens_here;                  // tokens whose heads make a product's rows
+    int passes, token_groups;         // of those to a workgroup; workgroups to a sequence
+    int splits;
 };
 
 template <bool BF16>
@@ -44,88 +44,90 @@ __device__ __forceinline__ float4v mfma16(short8v a, short8v b, float4v c) {
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8v, a), __builtin_bit_cast(half8v, b), c, 0, 0, 0);
 }
 
-// A wave's rows are up to 16 query heads at a time: of as many tokens as fit, or of a part of one token.  It keeps 16 blocks' bounds and walks the rows of its
-// tokens.  Lane l has, of row and of block l % 16, the channels 32 s + 8 (l / 16) + e: 16-byte accesses, four neighbouring lanes' 64 bytes for every s.
-template <bool BF16>
-__global__ __launch_bounds__(64 * kScoreWaves) void score_kernel(BlockArgs a) {
-    __shared__ float2 room[kScoreWaves][kTile][kTile + 1];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int split = blockIdx.x % a.splits, unit = blockIdx.x / a.splits;
-    const int token0 = unit % a.token_groups * a.tokens_here * a.passes, h = unit / a.token_groups % a.pages.n_kv_heads, b = unit / a.token_groups / a.pages.n_kv_heads;
-    const int n = length_of(a.q_lengths, b, a.q_tokens), N = length_of(a.kv_lengths, b, a.kv_tokens);
-    const int tokens = min(a.tokens_here * a.passes, n - token0), last = N - n + token0 + tokens - 1;   // the last row's position
-    if (tokens <= 0 || last < 0) return;
-    const int tiles = (last >> a.pages.log2) / kTile + 1;
-    const int column = lane % 16, quarter = lane / 16;
-    const int32_t* table = a.pages.table + b * a.pages.table_stride;
-    const uint16_t* base = (const uint16_t*)a.pages.bounds.data + h * a.pages.bounds.head + 8 * quarter;
-    const int64_t row0 = ((int64_t)b * a.pages.n_kv_heads + h) * a.q_tokens;
-    for (int tile = split * kScoreWaves + wave; tile < tiles; tile += a.splits * kScoreWaves) {
-        const int block = tile * kTile + column;
-        int page = block < a.pages.table_pages ? table[block] : -1;
-        const bool there = (uint32_t)page < (uint32_t)a.pages.n_pages;
-        if (!there) page = 0;
-        const uint16_t* from = base + page * a.pages.bounds.batch;
-        short8v least[4], most[4];
+// The scores of 16 blocks for the tokens token0 .. token0 + tokens - 1 of a KV head, by a wave.  Its rows are up to 16 query heads at a time: of as many tokens as
+// fit, or of a part of one token.  It keeps the blocks' bounds and walks the rows.  Lane l has, of row and of block l % 16, the channels 32 s + 8 (l / 16) + e:
+// 16-byte accesses, four neighbouring lanes' 64 bytes for every s.  Every s has a sum of its own, so that none has more than 64 addends in a row.
+// emit(token, block, score, the largest sum of magnitudes of these blocks as far as the token's candidates go)
+template <bool BF16, typename Emit>
+__device__ __forceinline__ void tile_scores(const BlockArgs& a, int b, int h, int first_position, int token0, int tokens, int tile, float2 (*room)[kTile + 1], Emit&& emit) {
+    const int lane = threadIdx.x % 64, column = lane % 16, quarter = lane / 16, block = tile * kTile + column;
+    int page = block < a.pages.table_pages ? a.pages.table[b * a.pages.table_stride + block] : -1;
+    const bool there = (uint32_t)page < (uint32_t)a.pages.n_pages;
+    if (!there) page = 0;
+    const uint16_t* from = (const uint16_t*)a.pages.bounds.data + page * a.pages.bounds.batch + h * a.pages.bounds.head + 8 * quarter;
+    short8v least[4], most[4];
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            least[s] = *(const short8v*)(from + 32 * s);
-            most[s] = *(const short8v*)(from + a.pages.bounds.token + 32 * s);
-        }
-        for (int t0 = 0; t0 < tokens; t0 += a.tokens_here) {
-            const int here = min(a.tokens_here, tokens - t0), rows = here * a.G;
-            float best[4], size[4];
+    for (int s = 0; s < 4; ++s) {
+        least[s] = *(const short8v*)(from + 32 * s);
+        most[s] = *(const short8v*)(from + a.pages.bounds.token + 32 * s);
+    }
+    for (int t0 = 0; t0 < tokens; t0 += a.tokens_here) {
+        const int here = min(a.tokens_here, tokens - t0), rows = here * a.G;
+        float best[4], size[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) best[i] = -INFINITY, size[i] = 0.0f;
-            for (int r0 = 0; r0 < rows; r0 += kTile) {
-                const int r = min(r0 + column, rows - 1);
-                const uint16_t* q = (const uint16_t*)a.q.data + b * a.q.batch + (h * a.G + r % a.G) * a.q.head + (token0 + t0 + r / a.G) * a.q.token + 8 * quarter;
-                float4v sum = {0.0f, 0.0f, 0.0f, 0.0f}, magnitude = sum;
-                constexpr short8v kZero = {0, 0, 0, 0, 0, 0, 0, 0}, kNoSign = {0x7FFF, 0x7FFF, 0x7FFF, 0x7FFF, 0x7FFF, 0x7FFF, 0x7FFF, 0x7FFF};
+        for (int i = 0; i < 4; ++i) best[i] = -INFINITY, size[i] = 0.0f;
+        for (int r0 = 0; r0 < rows; r0 += kTile) {
+            const int r = min(r0 + column, rows - 1);
+            const uint16_t* q = (const uint16_t*)a.q.data + b * a.q.batch + (h * a.G + r % a.G) * a.q.head + (token0 + t0 + r / a.G) * a.q.token + 8 * quarter;
+            constexpr float4v kNone = {0.0f, 0.0f, 0.0f, 0.0f};
+            constexpr short8v kZero = {0, 0, 0, 0, 0, 0, 0, 0}, kNoSign = {0x7FFF, 0x7FFF, 0x7FFF, 0x7FFF, 0x7FFF, 0x7FFF, 0x7FFF, 0x7FFF};
+            float4v sum[4], magnitude = kNone;
 #pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    const short8v x = *(const short8v*)(q + 32 * s);
-                    const short8v plus = __builtin_elementwise_max(x, kZero), minus = __builtin_elementwise_min(x, kZero);   // (a negative number's bits are one)
-                    sum = mfma16<BF16>(plus, most[s], sum);
-                    sum = mfma16<BF16>(minus, least[s], sum);
-                    magnitude = mfma16<BF16>(plus, most[s] & kNoSign, magnitude);
-                    magnitude = mfma16<BF16>(minus & kNoSign, least[s] & kNoSign, magnitude);
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) room[wave][4 * quarter + i][column] = float2{sum[i], magnitude[i]};
-                wave_sync();
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int t = quarter + 4 * i, end = min(min((t + 1) * a.G, r0 + kTile), rows);   // the token's heads among these rows
-                    for (int g = max(t * a.G, r0); g < end; ++g) {
-                        const float2 x = room[wave][g - r0][column];
-                        best[i] = fmaxf(best[i], x.x);
-                        size[i] = x.y <= size[i] ? size[i] : x.y == x.y ? x.y : INFINITY;
-                    }
-                }
-                wave_sync();
+            for (int s = 0; s < 4; ++s) {
+                const short8v x = *(const short8v*)(q + 32 * s);
+                const short8v plus = __builtin_elementwise_max(x, kZero), minus = __builtin_elementwise_min(x, kZero);   // (a negative number's bits are one)
+                sum[s] = mfma16<BF16>(minus, least[s], mfma16<BF16>(plus, most[s], kNone));
+                magnitude = mfma16<BF16>(plus, most[s] & kNoSign, magnitude);
+                magnitude = mfma16<BF16>(minus & kNoSign, least[s] & kNoSign, magnitude);
             }
+            sum[0] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) room[4 * quarter + i][column] = float2{sum[0][i], magnitude[i]};
+            wave_sync();
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int t = quarter + 4 * i;
-                if (4 * i >= here) break;
-                const bool candidate = t < here && there && block <= (N - n + token0 + t0 + t) >> a.pages.log2;
-                float largest = candidate ? size[i] : 0.0f;
-#pragma unroll
-                for (int d = 1; d < 16; d *= 2) largest = fmaxf(largest, __shfl_xor(largest, d));
-                if (t >= here) continue;
-                const int64_t row = row0 + token0 + t0 + t;
-                a.scores[row * a.row_blocks + block] = best[i];
-                if (column == 0) a.sizes[row * (a.row_blocks / kTile) + tile] = largest;
+                const int t = quarter + 4 * i, end = min(min((t + 1) * a.G, r0 + kTile), rows);   // the token's heads among these rows
+                for (int g = max(t * a.G, r0); g < end; ++g) {
+                    const float2 x = room[g - r0][column];
+                    best[i] = fmaxf(best[i], x.x);
+                    size[i] = x.y <= size[i] ? size[i] : x.y == x.y ? x.y : INFINITY;
+                }
             }
+            wave_sync();
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int t = quarter + 4 * i;
+            if (4 * i >= here) break;
+            const bool candidate = t < here && there && block <= (first_position + t0 + t) >> a.pages.log2;
+            float largest = candidate ? size[i] : 0.0f;
+#pragma unroll
+            for (int d = 1; d < 16; d *= 2) largest = fmaxf(largest, __shfl_xor(largest, d));
+            if (t < here) emit(t0 + t, block, best[i], largest);
         }
     }
 }
 
-// 32-bit sums are off by 2^-23 of the magnitudes per addition at most, of which there are 256 with the products; twice that, as the magnitudes are
-// such a sum as well, and what is lost below the smallest numbers.
-__device__ __forceinline__ double error_of(float size) { return 0x1p-14 * (double)size + 0x1p-110; }
+template <bool BF16>
+__global__ __launch_bounds__(64 * kScoreWaves) void score_kernel(BlockArgs a) {
+    __shared__ float2 room[kScoreWaves][kTile][kTile + 1];
+    const int wave = threadIdx.x / 64, split = blockIdx.x % a.splits, unit = blockIdx.x / a.splits;
+    const int token0 = unit % a.token_groups * a.tokens_here * a.passes, h = unit / a.token_groups % a.pages.n_kv_heads, b = unit / a.token_groups / a.pages.n_kv_heads;
+    const int n = length_of(a.q_lengths, b, a.q_tokens), first_position = length_of(a.kv_lengths, b, a.kv_tokens) - n + token0;
+    const int tokens = min(a.tokens_here * a.passes, n - token0), last = first_position + tokens - 1;
+    if (tokens <= 0 || last < 0) return;
+    const int tiles = (last >> a.pages.log2) / kTile + 1;
+    const int64_t row0 = ((int64_t)b * a.pages.n_kv_heads + h) * a.q_tokens + token0;
+    for (int tile = split * kScoreWaves + wave; tile < tiles; tile += a.splits * kScoreWaves)
+        tile_scores<BF16>(a, b, h, first_position, token0, tokens, tile, room[wave], [&](int t, int block, float score, float size) {
+            a.scores[(row0 + t) * a.row_blocks + block] = score;
+            if (block % kTile == 0) a.sizes[(row0 + t) * (a.row_blocks / kTile) + tile] = size;
+        });
+}
 
+// 32-bit sums are off by 2^-23 of the magnitudes per addition at most, of which 64 and 2 make a score: 2^-16.9.  The rest to 2^-16 is more than what the magnitudes are off
+// by, as sums of 256 (2^-15 of themselves); and what is lost below the smallest numbers.
+__device__ __forceinline__ double error_of(float size) { return 0x1p-16 * (double)size + 0x1p-110; }
 // Order of whole numbers for that of scores: the larger the later, 0 below all of them.
 __device__ __forceinline__ uint32_t key_of(float x) {
     if (!(x == x)) x = -INFINITY;
@@ -139,117 +141,93 @@ __device__ __forceinline__ uint64_t key_of(double x) {
     return u >> 63 ? ~u : u | 0x8000000000000000ull;
 }
 
-// A block's score in 64 bits, by 16 lanes of 8 channels each.
+// A query head's score of a block in 64 bits, by 16 lanes of 8 channels each.
 template <bool BF16>
-__device__ __forceinline__ uint64_t exact_key(const BlockArgs& a, int b, int h, int token, int page) {
+__device__ __forceinline__ uint64_t exact_key(const BlockArgs& a, int b, int h, int token, int g, int page) {
     const int part = threadIdx.x % 16;
     const uint16_t* bounds = (const uint16_t*)a.pages.bounds.data + page * a.pages.bounds.batch + h * a.pages.bounds.head + 8 * part;
     const short8v least = *(const short8v*)bounds, most = *(const short8v*)(bounds + a.pages.bounds.token);
-    double best = -INFINITY;
-    for (int g = 0; g < a.G; ++g) {
-        const short8v q = *(const short8v*)((const uint16_t*)a.q.data + b * a.q.batch + (h * a.G + g) * a.q.head + token * a.q.token + 8 * part);
-        double sum = 0.0;
+    const short8v q = *(const short8v*)((const uint16_t*)a.q.data + b * a.q.batch + (h * a.G + g) * a.q.head + token * a.q.token + 8 * part);
+    double sum = 0.0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const double x = widen16<BF16>((uint16_t)q[e]);
-            sum += (x < 0.0 ? 0.0 : x) * (double)widen16<BF16>((uint16_t)most[e]) + (x > 0.0 ? 0.0 : x) * (double)widen16<BF16>((uint16_t)least[e]);
-        }
-#pragma unroll
-        for (int d = 1; d < 16; d *= 2) sum += __shfl_xor(sum, d);
-        best = fmax(best, sum);
+    for (int e = 0; e < 8; ++e) {
+        const double x = widen16<BF16>((uint16_t)q[e]);
+        sum += (x < 0.0 ? 0.0 : x) * (double)widen16<BF16>((uint16_t)most[e]) + (x > 0.0 ? 0.0 : x) * (double)widen16<BF16>((uint16_t)least[e]);
     }
-    return key_of(best);
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2) sum += __shfl_xor(sum, d);
+    return key_of(sum);
 }
 
-constexpr int kBand = 256;            // blocks so near to the last chosen one that are told apart in LDS
+__device__ __forceinline__ uint32_t wave_min_bits(uint32_t v) { return ~wave_max_bits(~v); }
+// the sum over the lanes up to this one
+__device__ __forceinline__ uint32_t wave_sum_to(uint32_t x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);   // lanes 1, 2, 4, 8 before in a row of 16
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);   // the last of rows 0 and 2 to rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);   // the last of row 1 to rows 2 and 3
+    return x;
+}
+
+constexpr int kBand = 256;            // blocks around the last chosen one that are told apart in LDS
 template <int THREADS>
 struct Select {
     static constexpr int kWaves = THREADS / 64, kBins = 1024;
     uint32_t bins[kBins];
-    uint32_t of_wave[kWaves];
-    uint32_t least[kWaves], most[kWaves];
-    float size[kWaves];
-    uint32_t found[2], band_n, band_index[kBand];
-    uint64_t band_key[kBand];
+    uint32_t of_wave[2][kWaves];
+    uint32_t least[kWaves], most[kWaves], size[kWaves], there[kWaves];
+    uint32_t found[3], above, band_n, band_index[kBand];
+    unsigned long long band_key[kBand];
     bool band_chosen[kBand];
 
-    // sum over the threads before this one; total: over all
-    __device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t& total) {
+    // sum over the threads before this one; total: over all (turn: 0 and 1 in turn, as what one call left is read until the next one's barrier)
+    __device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t& total, int turn) {
         const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-        uint32_t run = x;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const uint32_t y = __shfl_up(run, d);
-            if (lane >= d) run += y;
-        }
-        __syncthreads();              // (what was there has been read)
-        if (lane == 63) of_wave[wave] = run;
+        const uint32_t run = wave_sum_to(x);
+        if (lane == 63) of_wave[turn][wave] = run;
         __syncthreads();
         uint32_t before = 0;
         total = 0;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-            if (w < wave) before += of_wave[w];
-            total += of_wave[w];
+            if (w < wave) before += of_wave[turn][w];
+            total += of_wave[turn][w];
         }
         return before + run - x;
     }
-    // the least and the largest over all threads
-    __device__ __forceinline__ void extremes(uint32_t& lo, uint32_t& hi, float& sz) {
-        const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            lo = min(lo, (uint32_t)__shfl_xor(lo, d));
-            hi = max(hi, (uint32_t)__shfl_xor(hi, d));
-            sz = fmaxf(sz, __shfl_xor(sz, d));
-        }
-        __syncthreads();
-        if (lane == 0) least[wave] = lo, most[wave] = hi, size[wave] = sz;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) lo = min(lo, least[w]), hi = max(hi, most[w]), sz = fmaxf(sz, size[w]);
-    }
-    // The bin of the `left`th element, counted from the last bin (every thread has counted its elements); returns its number of elements, takes those behind it from `left`.
-    __device__ __forceinline__ uint32_t find(uint32_t& left, uint32_t& bin) {
+    // The bin of the `left`th element, counted from the last bin (every thread has counted its elements, and a barrier is behind); the number of its elements, and of those
+    // behind it.
+    __device__ __forceinline__ void find(uint32_t left, uint32_t& bin, uint32_t& here, uint32_t& behind, int turn) {
         constexpr int kOwn = kBins / THREADS;
-        __syncthreads();
         uint32_t c[kOwn], sum = 0, total;
 #pragma unroll
         for (int i = 0; i < kOwn; ++i) sum += c[i] = bins[kBins - 1 - (int)threadIdx.x * kOwn - i];
-        uint32_t before = sum_before(sum, total);
+        uint32_t before = sum_before(sum, total, turn);
         if (before < left && before + sum >= left) {
 #pragma unroll
             for (int i = 0; i < kOwn; ++i) {
-                if (before < left && before + c[i] >= left) found[0] = kBins - 1 - threadIdx.x * kOwn - i, found[1] = before;
+                if (before < left && before + c[i] >= left) found[0] = kBins - 1 - threadIdx.x * kOwn - i, found[1] = before, found[2] = c[i];
                 before += c[i];
             }
         }
         __syncthreads();
         bin = found[0];
-        left -= found[1];
-        return bins[bin];
+        behind = found[1];
+        here = found[2];
     }
     __device__ __forceinline__ void clear() {
-        __syncthreads();
         for (int i = threadIdx.x; i < kBins; i += THREADS) bins[i] = 0;
-        __syncthreads();
     }
-};
-
-// The choice by 64-bit keys in memory, where too many scores are alike: chosen(key) and, of those that match the last chosen one's bits, the first ones.
-struct Exact {
-    uint64_t edge;
-    int shift;
-    uint32_t equal;                   // of the matching ones
-    __device__ __forceinline__ bool above(uint64_t k) const { return k >> shift > edge >> shift; }
-    __device__ __forceinline__ bool matches(uint64_t k) const { return k >> shift == edge >> shift; }
 };
 
 // Thread t has the blocks t * own .. t * own + own - 1 of the row.  KEEP: their scores stay in registers (as many at most); 0: they are read again in every pass.
 template <bool BF16, int THREADS, int KEEP>
 __global__ __launch_bounds__(THREADS) void select_kernel(BlockArgs a) {
     __shared__ Select<THREADS> s;
-    const int tid = threadIdx.x, token = blockIdx.x % a.q_tokens, h = blockIdx.x / a.q_tokens % a.pages.n_kv_heads, b = blockIdx.x / a.q_tokens / a.pages.n_kv_heads;
+    const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+    const int token = blockIdx.x % a.q_tokens, h = blockIdx.x / a.q_tokens % a.pages.n_kv_heads, b = blockIdx.x / a.q_tokens / a.pages.n_kv_heads;
     const int n = length_of(a.q_lengths, b, a.q_tokens), N = length_of(a.kv_lengths, b, a.kv_tokens);
     if (token >= n) return;
     const int slots = a.first + a.top + a.recent;
@@ -276,117 +254,129 @@ __global__ __launch_bounds__(THREADS) void select_kernel(BlockArgs a) {
         }
     };
 
-    uint32_t there = 0, total, least = ~0u, most = 0;
-    float size = 0.0f;
+    // how many there are, the range of their keys and the largest sum of magnitudes
+    uint32_t there = 0, least = ~0u, most = 0, size = 0;
     if (a.top > 0)
-        for (int i = tid; i < (blocks + kTile - 1) / kTile; i += THREADS) size = fmaxf(size, a.sizes[(int64_t)blockIdx.x * (a.row_blocks / kTile) + i]);
+        for (int i = tid; i < (blocks + kTile - 1) / kTile; i += THREADS) size = max(size, __float_as_uint(a.sizes[(int64_t)blockIdx.x * (a.row_blocks / kTile) + i]));
+    s.clear();
     each([&](int, uint32_t k) {
         if (!k) return;
         ++there;
         least = min(least, k);
         most = max(most, k);
     });
-    s.sum_before(there, total);
-    s.extremes(least, most, size);
+    least = wave_min_bits(least), most = wave_max_bits(most), size = wave_max_bits(size), there = wave_sum_to(there);
+    if (lane == 63) s.least[wave] = least, s.most[wave] = most, s.size[wave] = size, s.there[wave] = there;
+    if (tid == 0) s.above = s.band_n = 0;
+    __syncthreads();
+    uint32_t total = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) least = min(least, s.least[w]), most = max(most, s.most[w]), size = max(size, s.size[w]), total += s.there[w];
 
-    // Chosen are: all of the choice; or the keys from `least + edge` on; or those above a band of scores, and the band's best.
-    enum { kAll, kNone, kAbove, kNear, kExact } how;
-    uint32_t left = min((uint32_t)a.top, total), edge = 0;
+    // Chosen are: all of the choice; none; those above a band of scores, and the band's best; or, where too many are alike, the best by 64-bit keys in memory.
+    enum { kAll, kNone, kNear, kExact } how;
+    const uint32_t wanted = min((uint32_t)a.top, total);
     float low = 0.0f, high = 0.0f;                       // the band
-    Exact exact{0, 0, 0};
+    uint64_t cut = 0;                                    // kExact: the last chosen key, of whose equals the first ones are chosen
+    uint32_t equal = 0, tie_at = 0;
     const auto is_near = [&](uint32_t k) { const float x = score_of(k); return !(x > high) && !(x < low); };
-    const uint64_t* keys = a.keys + (int64_t)blockIdx.x * a.row_blocks;
-    if (left == total) how = kAll;
-    else if (!left) how = kNone;
+    uint64_t* const keys = a.keys + (int64_t)blockIdx.x * a.row_blocks;
+    if (wanted == total) how = kAll;
+    else if (!wanted) how = kNone;
     else {
-        const uint32_t wanted = left;
-        int shift = least == most ? 0 : 32 - __builtin_clz(most - least);   // bits of the keys' distances from the least
-        uint32_t here = total;
-        while (shift > 0 && here != left) {
+        how = kNear;
+        const double error = 2.0 * error_of(__uint_as_float(size));
+        const int bits = least == most ? 1 : 32 - __builtin_clz(most - least);   // of the keys' distances from the least
+        int shift = max(0, bits - 10);
+        uint32_t edge = 0, here, bin, behind, left = wanted;   // the bin's first distance
+        each([&](int, uint32_t k) {
+            if (k) atomicAdd(&s.bins[(k - least) >> shift], 1u);
+        });
+        __syncthreads();
+        s.find(left, bin, here, behind, 0);
+        edge = bin << shift;
+        left -= behind;
+        // a bin of many is taken apart once
+        if (here > kBand / 2 && shift) {
             const int above = shift;
             shift = max(0, shift - 10);
             s.clear();
+            __syncthreads();
             each([&](int, uint32_t k) {
-                if (k && (above == 32 || ((k - least) ^ edge) >> above == 0)) atomicAdd(&s.bins[((k - least) >> shift) & ((1 << (above - shift)) - 1)], 1u);
+                if (k && ((k - least) ^ edge) >> above == 0) atomicAdd(&s.bins[((k - least) ^ edge) >> shift], 1u);
             });
-            uint32_t bin;
-            here = s.find(left, bin);
+            __syncthreads();
+            s.find(left, bin, here, behind, 1);
             edge |= bin << shift;
         }
-        // the last chosen score, and the best that is not
-        uint32_t worst = ~0u, next = 0;
-        float unused = 0.0f;
-        each([&](int, uint32_t k) {
-            if (!k) return;
-            if (k - least >= edge) worst = min(worst, k);
-            else next = max(next, k);
+        // Scores beyond twice the error of the bin that holds the last chosen one are sure (rounded away from it; where the error is infinite or NaN, none is).
+        const uint32_t last = edge + ((1u << shift) - 1);
+        low = (float)((double)score_of(least + edge) - error), high = (float)((double)score_of(min(last, most - least) + least) + error);
+        low -= fabsf(low) * 0x1p-23f, high += fabsf(high) * 0x1p-23f;
+        each([&](int i, uint32_t k) {
+            const uint64_t sure = __ballot(k && score_of(k) > high);
+            if (sure && lane == 0) atomicAdd(&s.above, (uint32_t)__builtin_popcountll(sure));
+            if (!k || !is_near(k)) return;
+            const uint32_t at = atomicAdd(&s.band_n, 1u);
+            if (at < kBand) s.band_index[at] = first + i, s.band_key[at] = 0;
         });
-        s.extremes(worst, next, unused);
-        const double error = 2.0 * error_of(size);
-        how = here == left && (double)score_of(worst) - (double)score_of(next) > error ? kAbove : kNear;
-        if (how == kNear) {
-            // (rounded away from each other; infinite or NaN, everything is near)
-            low = (float)((double)score_of(worst) - error), high = (float)((double)score_of(worst) + error);
-            low = low - fabsf(low) * 0x1p-23f, high = high + fabsf(high) * 0x1p-23f;
-            uint32_t above = 0, above_all;
-            each([&](int, uint32_t k) { above += k && score_of(k) > high; });
-            s.sum_before(above, above_all);
-            if (tid == 0) s.band_n = 0;
-            __syncthreads();
-            each([&](int i, uint32_t k) {
-                if (!k || !is_near(k)) return;
-                const uint32_t at = atomicAdd(&s.band_n, 1u);
-                if (at < kBand) s.band_index[at] = first + i;
-            });
-            __syncthreads();
-            const int band = s.band_n;
-            left = wanted - above_all;
-            if (band <= kBand) {
-                for (int e = tid / 16; e < band; e += THREADS / 16) {
-                    const uint64_t k = exact_key<BF16>(a, b, h, token, table[s.band_index[e]]);
-                    if (tid % 16 == 0) s.band_key[e] = k;
+        __syncthreads();
+        const int band = s.band_n;
+        left = wanted - s.above;
+        if (band <= kBand) {
+            if ((uint32_t)band != left) {                // (else all of it)
+                for (int x = tid / 16; x < band * a.G; x += THREADS / 16) {
+                    const uint64_t k = exact_key<BF16>(a, b, h, token, x % a.G, table[s.band_index[x / a.G]]);
+                    if (tid % 16 == 0) atomicMax(&s.band_key[x / a.G], (unsigned long long)k);
                 }
-                __syncthreads();
-                for (int e = tid; e < band; e += THREADS) {
-                    uint32_t better = 0;
-                    for (int o = 0; o < band; ++o)
-                        better += s.band_key[o] > s.band_key[e] || (s.band_key[o] == s.band_key[e] && s.band_index[o] < s.band_index[e]);
-                    s.band_chosen[e] = better < left;
-                }
-                __syncthreads();
-            } else {
-                how = kExact;
-                uint64_t* to = a.keys + (int64_t)blockIdx.x * a.row_blocks;
-                for (int c = tid / 16; c < blocks; c += THREADS / 16) {
-                    const uint64_t k = has_page(c) && !always(c) ? exact_key<BF16>(a, b, h, token, table[c]) : 0;
-                    if (tid % 16 == 0) to[c] = k;
-                }
-                left = wanted;
-                here = total;
-                int at = 64;
-                while (at > 0 && here != left) {
-                    const int above = at;
-                    at = max(0, at - 10);
-                    s.clear();
-                    for (int i = 0; i < own; ++i) {
-                        const uint64_t k = first + i < blocks ? keys[first + i] : 0;
-                        if (k && (above == 64 || (k ^ exact.edge) >> above == 0)) atomicAdd(&s.bins[(k >> at) & ((1ull << (above - at)) - 1)], 1u);
-                    }
-                    uint32_t bin;
-                    here = s.find(left, bin);
-                    exact.edge |= (uint64_t)bin << at;
-                }
-                exact.shift = at;
-                exact.equal = left;
                 __syncthreads();
             }
+            for (int e = tid; e < band; e += THREADS) {
+                uint32_t better = 0;
+                for (int o = 0; o < band; ++o)
+                    better += s.band_key[o] > s.band_key[e] || (s.band_key[o] == s.band_key[e] && s.band_index[o] < s.band_index[e]);
+                s.band_chosen[e] = better < left;
+            }
+            __syncthreads();
+        } else {
+            how = kExact;
+            for (int c = tid / 16; c < blocks; c += THREADS / 16) {
+                uint64_t best = 0;
+                if (has_page(c) && !always(c))
+                    for (int g = 0; g < a.G; ++g) {
+                        const uint64_t k = exact_key<BF16>(a, b, h, token, g, table[c]);
+                        best = k > best ? k : best;
+                    }
+                if (tid % 16 == 0) keys[c] = best;
+            }
+            left = wanted;
+            int at = 64;
+            here = total;
+            for (int turn = 0; at > 0 && here != left; turn ^= 1) {
+                const int above = at;
+                at = max(0, at - 10);
+                __syncthreads();
+                s.clear();
+                __syncthreads();
+                for (int i = 0; i < own; ++i) {
+                    const uint64_t k = first + i < blocks ? keys[first + i] : 0;
+                    if (k && (above == 64 || (k ^ cut) >> above == 0)) atomicAdd(&s.bins[(k >> at) & ((1ull << (above - at)) - 1)], 1u);
+                }
+                __syncthreads();
+                s.find(left, bin, here, behind, turn);
+                left -= behind;
+                cut |= (uint64_t)bin << at;
+            }
+            // (where all of a bin are chosen, so is all from its first key on)
+            if (here == left) equal = ~0u, cut -= cut ? 1 : 0;
+            else equal = left;
+            __syncthreads();
+            uint32_t matching = 0, unused;
+            for (int i = 0; i < own; ++i) matching += first + i < blocks && keys[first + i] && keys[first + i] == cut;
+            tie_at = s.sum_before(matching, unused, 0);
+            if (equal == ~0u) equal = 0;
+            __syncthreads();
         }
-    }
-    uint32_t tie_at = 0;
-    if (how == kExact) {
-        uint32_t matching = 0, unused;
-        for (int i = 0; i < own; ++i) matching += first + i < blocks && keys[first + i] && exact.matches(keys[first + i]);
-        tie_at = s.sum_before(matching, unused);
     }
     const auto chosen = [&](int i, uint32_t k, uint32_t& tie) {
         const int c = first + i;
@@ -394,19 +384,22 @@ __global__ __launch_bounds__(THREADS) void select_kernel(BlockArgs a) {
         if (!k) return always(c) && has_page(c);
         if (how == kAll) return true;
         if (how == kNone) return false;
-        if (how == kAbove) return k - least >= edge;
-        if (how == kExact) return exact.matches(keys[c]) ? tie++ < exact.equal : exact.above(keys[c]);
+        if (how == kExact) return keys[c] == cut ? tie++ < equal : keys[c] > cut;
         if (!is_near(k)) return score_of(k) > high;
         for (uint32_t e = 0; e < s.band_n; ++e)
             if (s.band_index[e] == (uint32_t)c) return (bool)s.band_chosen[e];
         return false;
     };
-    uint32_t number = 0, tie = tie_at;
-    each([&](int i, uint32_t k) { number += chosen(i, k, tie); });
-    uint32_t at = s.sum_before(number, total);
+    uint32_t number = 0, tie = tie_at, picked = 0;
+    each([&](int i, uint32_t k) {
+        const bool yes = chosen(i, k, tie);
+        number += yes;
+        if (KEEP) picked |= (uint32_t)yes << i;
+    });
+    uint32_t at = s.sum_before(number, total, 1);
     tie = tie_at;
     each([&](int i, uint32_t k) {
-        if (chosen(i, k, tie)) list[at++] = first + i;
+        if (KEEP ? picked >> i & 1 : chosen(i, k, tie)) list[at++] = first + i;
     });
     for (int i = total + tid; i < slots; i += THREADS) list[i] = -1;
 }
