@@ -3,7 +3,7 @@
 // score(block) = max over the KV head's query heads of  max(q, 0) . most + min(q, 0) . least, where least and most are the block's bounds: a product over 256
 // channels, [max(q, 0), min(q, 0)] by [most, least].  Which block is the last chosen depends on scores next to each other, and a sum in
 // 32 bits would choose differently from one order of additions to another, so the choice is that of sums in 64 bits.  Hardly a block needs them: score_kernel
-// makes all scores on the matrix cores in 32 bits, together with the sums of the addends' magnitudes, which bound their error; select_kernel, a workgroup to a
+// makes all scores on the matrix cores in 32 bits, together with a bound of the sums of the addends' magnitudes, which bounds their error; select_kernel, a workgroup to a
 // row, counts them in bins and makes those around the last chosen one again in 64 bits.
 #include "pages.h"
 #include "wave_ops.h"
@@ -55,55 +55,85 @@ __device__ __forceinline__ void tile_scores(const BlockArgs& a, int b, int h, in
     const bool there = (uint32_t)page < (uint32_t)a.pages.n_pages;
     if (!there) page = 0;
     const uint16_t* from = (const uint16_t*)a.pages.bounds.data + page * a.pages.bounds.batch + h * a.pages.bounds.head + 8 * quarter;
-    short8v least[4], most[4];
+    constexpr short8v kZero = {0, 0, 0, 0, 0, 0, 0, 0}, kNoSign = {0x7FFF, 0x7FFF, 0x7FFF, 0x7FFF, 0x7FFF, 0x7FFF, 0x7FFF, 0x7FFF};
+    short8v least[4], most[4], largest[4];
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
         least[s] = *(const short8v*)(from + 32 * s);
         most[s] = *(const short8v*)(from + a.pages.bounds.token + 32 * s);
     }
+    const auto query = [&](int t0, int r0, int s) {
+        const int r = min(r0 + column, min(a.tokens_here, tokens - t0) * a.G - 1);
+        return *(const short8v*)((const uint16_t*)a.q.data + b * a.q.batch + (h * a.G + r % a.G) * a.q.head + (token0 + t0 + r / a.G) * a.q.token + 8 * quarter + 32 * s);
+    };
+    short8v next[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) next[s] = query(0, 0, s);
+#pragma unroll
+    for (int s = 0; s < 4; ++s) largest[s] = __builtin_elementwise_max(most[s] & kNoSign, least[s] & kNoSign);   // (magnitudes' bits are in their order)
+    // Where heads are 1, 2, 4, 8 or whole products to a token its rows are in a lane's registers and in those of the lanes 16, 32 and 48 away: value i of a lane is token
+    // first_of + i then; else they meet in LDS, and it is token quarter + 4 i.
+    const bool even = (a.G & (a.G - 1)) == 0;
+    const int values = !even ? 4 : a.G == 1 ? 4 : a.G == 2 ? 2 : 1, step = even ? 1 : 4;
+    const int first_of = !even ? quarter : a.G == 1 ? 4 * quarter : a.G == 2 ? 2 * quarter : a.G == 4 ? quarter : a.G == 8 ? quarter / 2 : 0;
     for (int t0 = 0; t0 < tokens; t0 += a.tokens_here) {
         const int here = min(a.tokens_here, tokens - t0), rows = here * a.G;
         float best[4], size[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) best[i] = -INFINITY, size[i] = 0.0f;
+        const auto take = [](float& best, float& size, float score, float magnitude) {
+            best = fmaxf(best, score);
+            size = magnitude <= size ? size : magnitude == magnitude ? magnitude : INFINITY;
+        };
         for (int r0 = 0; r0 < rows; r0 += kTile) {
-            const int r = min(r0 + column, rows - 1);
-            const uint16_t* q = (const uint16_t*)a.q.data + b * a.q.batch + (h * a.G + r % a.G) * a.q.head + (token0 + t0 + r / a.G) * a.q.token + 8 * quarter;
             constexpr float4v kNone = {0.0f, 0.0f, 0.0f, 0.0f};
-            constexpr short8v kZero = {0, 0, 0, 0, 0, 0, 0, 0}, kNoSign = {0x7FFF, 0x7FFF, 0x7FFF, 0x7FFF, 0x7FFF, 0x7FFF, 0x7FFF, 0x7FFF};
             float4v sum[4], magnitude = kNone;
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
-                const short8v x = *(const short8v*)(q + 32 * s);
+                const short8v x = next[s];
                 const short8v plus = __builtin_elementwise_max(x, kZero), minus = __builtin_elementwise_min(x, kZero);   // (a negative number's bits are one)
                 sum[s] = mfma16<BF16>(minus, least[s], mfma16<BF16>(plus, most[s], kNone));
-                magnitude = mfma16<BF16>(plus, most[s] & kNoSign, magnitude);
-                magnitude = mfma16<BF16>(minus & kNoSign, least[s] & kNoSign, magnitude);
+                magnitude = mfma16<BF16>(x & kNoSign, largest[s], magnitude);
             }
+            // (the next rows are on their way meanwhile)
+            const bool same = r0 + kTile < rows;
+            if (same || t0 + a.tokens_here < tokens)
+#pragma unroll
+                for (int s = 0; s < 4; ++s) next[s] = query(same ? t0 : t0 + a.tokens_here, same ? r0 + kTile : 0, s);
             sum[0] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            if (even) {                                  // (rows behind the last are that one again, of whose token nothing is kept, or which adds nothing)
+                float score[4], of[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) room[4 * quarter + i][column] = float2{sum[0][i], magnitude[i]};
-            wave_sync();
+                for (int i = 0; i < 4; ++i) score[i] = sum[0][i], of[i] = magnitude[i] == magnitude[i] ? magnitude[i] : INFINITY;
+                if (a.G > 1) score[0] = fmaxf(score[0], score[1]), of[0] = fmaxf(of[0], of[1]), score[1] = fmaxf(score[2], score[3]), of[1] = fmaxf(of[2], of[3]);
+                if (a.G > 2) score[0] = fmaxf(score[0], score[1]), of[0] = fmaxf(of[0], of[1]);
+                if (a.G > 4) score[0] = fmaxf(score[0], __shfl_xor(score[0], 16)), of[0] = fmaxf(of[0], __shfl_xor(of[0], 16));
+                if (a.G > 8) score[0] = fmaxf(score[0], __shfl_xor(score[0], 32)), of[0] = fmaxf(of[0], __shfl_xor(of[0], 32));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int t = quarter + 4 * i, end = min(min((t + 1) * a.G, r0 + kTile), rows);   // the token's heads among these rows
-                for (int g = max(t * a.G, r0); g < end; ++g) {
-                    const float2 x = room[g - r0][column];
-                    best[i] = fmaxf(best[i], x.x);
-                    size[i] = x.y <= size[i] ? size[i] : x.y == x.y ? x.y : INFINITY;
+                for (int i = 0; i < 4; ++i) take(best[i], size[i], score[i], of[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) room[4 * quarter + i][column] = float2{sum[0][i], magnitude[i]};
+                wave_sync();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int t = quarter + 4 * i, end = min(min((t + 1) * a.G, r0 + kTile), rows);   // the token's heads among these rows
+                    for (int g = max(t * a.G, r0); g < end; ++g) take(best[i], size[i], room[g - r0][column].x, room[g - r0][column].y);
                 }
+                wave_sync();
             }
-            wave_sync();
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int t = quarter + 4 * i;
-            if (4 * i >= here) break;
+            if (i >= values) break;
+            const int t = first_of + step * i;
             const bool candidate = t < here && there && block <= (first_position + t0 + t) >> a.pages.log2;
-            float largest = candidate ? size[i] : 0.0f;
-#pragma unroll
-            for (int d = 1; d < 16; d *= 2) largest = fmaxf(largest, __shfl_xor(largest, d));
-            if (t < here) emit(t0 + t, block, best[i], largest);
+            float most_of = candidate ? size[i] : 0.0f;
+            most_of = fmaxf(most_of, dpp_move<kDppXor1>(most_of));
+            most_of = fmaxf(most_of, dpp_move<kDppXor2>(most_of));
+            most_of = fmaxf(most_of, dpp_move<kDppHalfMirror>(most_of));
+            most_of = fmaxf(most_of, dpp_move<kDppMirror>(most_of));
+            if (t < here) emit(t0 + t, block, best[i], most_of);   // (several lanes the same, of many heads)
         }
     }
 }

@@ -636,7 +636,7 @@ struct Plan {
 };
 
 // `units` of `rows` rows each over at most `most` positions: by waves by themselves, or (waves of a workgroup) in tiles
-Part part_of(int64_t units, int64_t rows, int64_t most, int waves, int64_t at_once = 0) {
+Part part_of(int64_t units, int64_t rows, int64_t most, int waves, bool joined, int64_t at_once = 0) {
     Part p;
     int64_t chunks = 1;
     if (!waves) {
@@ -644,7 +644,7 @@ Part part_of(int64_t units, int64_t rows, int64_t most, int waves, int64_t at_on
         p.row_tiles = (int)((rows + kWaveRows - 1) / kWaveRows);
         p.items = units * p.row_tiles;
         const int64_t tiles = (most + 31) / 32;
-        if (p.items && tiles > 4 * kStepWaves) {
+        if (p.items && tiles > (joined ? 4 : 6) * kStepWaves) {
             chunks = std::max(kStepsAtOnce / p.items, tiles / 64);
             chunks = std::min({chunks, tiles / kStepWaves, std::max<int64_t>(256, tiles / 64)});
         }
@@ -691,8 +691,8 @@ int plan_of(const specache_pages* cache, const specache_paged_config* c, Plan& p
         p.kind = kTiles;
         p.waves = std::max(p.shared, c->kv_tokens - p.shared) >= 2048 && rows > 128 ? 8 : 4;
     } else if (p.shared && c->batch * rows > kWaveRows) p.kind = kTilesAndSteps;
-    if (p.shared) p.prefix = part_of(cache->n_kv_heads, c->batch * rows, p.shared, p.kind == kSteps ? 0 : p.waves, p.kind == kTiles ? (p.waves == 8 ? 256 : 512) : 256);
-    p.own = part_of(rows ? (int64_t)c->batch * cache->n_kv_heads : 0, rows, c->kv_tokens - p.shared, p.kind == kTiles ? p.waves : 0, p.waves == 8 ? 256 : 512);
+    if (p.shared) p.prefix = part_of(cache->n_kv_heads, c->batch * rows, p.shared, p.kind == kSteps ? 0 : p.waves, true, p.kind == kTiles ? (p.waves == 8 ? 256 : 512) : 256);
+    p.own = part_of(rows ? (int64_t)c->batch * cache->n_kv_heads : 0, rows, c->kv_tokens - p.shared, p.kind == kTiles ? p.waves : 0, p.shared != 0, p.waves == 8 ? 256 : 512);
     return finish_plan(p, c->batch * rows * cache->n_kv_heads);
 }
 
@@ -714,7 +714,7 @@ int plan_of_blocks(const specache_pages* cache, const specache_block_config* c, 
     if (int rc = check_blocks(cache, c)) return rc;
     const int64_t slots = (int64_t)c->top + c->first + c->recent, blocks = (c->kv_tokens + cache->page_tokens - 1) / cache->page_tokens;
     const int64_t units = (int64_t)c->batch * c->q_tokens * cache->n_kv_heads;
-    p.own = part_of(units, c->n_q_heads / cache->n_kv_heads, std::min(slots, blocks) * cache->page_tokens, 0);
+    p.own = part_of(units, c->n_q_heads / cache->n_kv_heads, std::min(slots, blocks) * cache->page_tokens, 0, false);
     return finish_plan(p, units * (c->n_q_heads / cache->n_kv_heads));
 }
 
