@@ -44,14 +44,18 @@ __device__ __forceinline__ float4v mfma16(short8v a, short8v b, float4v c) {
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8v, a), __builtin_bit_cast(half8v, b), c, 0, 0, 0);
 }
 
+__device__ __forceinline__ int page_of(const BlockArgs& a, int b, int tile) {
+    const int block = tile * kTile + threadIdx.x % 16;
+    return block < a.pages.table_pages ? a.pages.table[b * a.pages.table_stride + block] : -1;
+}
+
 // The scores of 16 blocks for the tokens token0 .. token0 + tokens - 1 of a KV head, by a wave.  Its rows are up to 16 query heads at a time: of as many tokens as
 // fit, or of a part of one token.  It keeps the blocks' bounds and walks the rows.  Lane l has, of row and of block l % 16, the channels 32 s + 8 (l / 16) + e:
 // 16-byte accesses, four neighbouring lanes' 64 bytes for every s.  Every s has a sum of its own, so that none has more than 64 addends in a row.
-// emit(token, block, score, the largest sum of magnitudes of these blocks as far as the token's candidates go)
+// page: the lane's block's, as page_of has it.  emit(token, block, score, the largest sum of magnitudes of these blocks as far as the token's candidates go)
 template <bool BF16, typename Emit>
-__device__ __forceinline__ void tile_scores(const BlockArgs& a, int b, int h, int first_position, int token0, int tokens, int tile, float2 (*room)[kTile + 1], Emit&& emit) {
+__device__ __forceinline__ void tile_scores(const BlockArgs& a, int b, int h, int first_position, int token0, int tokens, int tile, int page, float2 (*room)[kTile + 1], Emit&& emit) {
     const int lane = threadIdx.x % 64, column = lane % 16, quarter = lane / 16, block = tile * kTile + column;
-    int page = block < a.pages.table_pages ? a.pages.table[b * a.pages.table_stride + block] : -1;
     const bool there = (uint32_t)page < (uint32_t)a.pages.n_pages;
     if (!there) page = 0;
     const uint16_t* from = (const uint16_t*)a.pages.bounds.data + page * a.pages.bounds.batch + h * a.pages.bounds.head + 8 * quarter;
@@ -143,16 +147,21 @@ __global__ __launch_bounds__(64 * kScoreWaves) void score_kernel(BlockArgs a) {
     __shared__ float2 room[kScoreWaves][kTile][kTile + 1];
     const int wave = threadIdx.x / 64, split = blockIdx.x % a.splits, unit = blockIdx.x / a.splits;
     const int token0 = unit % a.token_groups * a.tokens_here * a.passes, h = unit / a.token_groups % a.pages.n_kv_heads, b = unit / a.token_groups / a.pages.n_kv_heads;
+    const int tile0 = split * kScoreWaves + wave;
+    int page = page_of(a, b, tile0);                     // (on its way while the lengths are)
     const int n = length_of(a.q_lengths, b, a.q_tokens), first_position = length_of(a.kv_lengths, b, a.kv_tokens) - n + token0;
     const int tokens = min(a.tokens_here * a.passes, n - token0), last = first_position + tokens - 1;
     if (tokens <= 0 || last < 0) return;
     const int tiles = (last >> a.pages.log2) / kTile + 1;
     const int64_t row0 = ((int64_t)b * a.pages.n_kv_heads + h) * a.q_tokens + token0;
-    for (int tile = split * kScoreWaves + wave; tile < tiles; tile += a.splits * kScoreWaves)
-        tile_scores<BF16>(a, b, h, first_position, token0, tokens, tile, room[wave], [&](int t, int block, float score, float size) {
+    for (int tile = tile0; tile < tiles; tile += a.splits * kScoreWaves) {
+        const int here = page;
+        page = page_of(a, b, tile + a.splits * kScoreWaves);
+        tile_scores<BF16>(a, b, h, first_position, token0, tokens, tile, here, room[wave], [&](int t, int block, float score, float size) {
             a.scores[(row0 + t) * a.row_blocks + block] = score;
             if (block % kTile == 0) a.sizes[(row0 + t) * (a.row_blocks / kTile) + tile] = size;
         });
+    }
 }
 
 // 32-bit sums are off by 2^-23 of the magnitudes per addition at most, of which 64 and 2 make a score: 2^-16.9.  The rest to 2^-16 is more than what the magnitudes are off
@@ -209,6 +218,7 @@ struct Select {
     uint32_t of_wave[2][kWaves];
     uint32_t least[kWaves], most[kWaves], size[kWaves], there[kWaves];
     uint32_t found[3], above, band_n, band_index[kBand];
+    int band_page[kBand];
     unsigned long long band_key[kBand];
     bool band_chosen[kBand];
 
@@ -269,7 +279,12 @@ __global__ __launch_bounds__(THREADS) void select_kernel(BlockArgs a) {
     const auto has_page = [&](int c) { return c < blocks && (uint32_t)table[c] < (uint32_t)a.pages.n_pages; };
     const auto always = [&](int c) { return c < a.first || c > mine - a.recent; };
     // 0: not in the choice (nothing is where there is no choice, and no scores either)
-    const auto read = [&](int i) -> uint32_t { return a.top > 0 && i < own && has_page(first + i) && !always(first + i) ? key_of(scores[first + i]) : 0; };
+    const auto read = [&](int i) -> uint32_t {
+        if (a.top <= 0 || i >= own) return 0;
+        const int c = first + i, page = table[min(c, blocks - 1)];       // (both loads at once)
+        const float score = scores[min(c, blocks - 1)];
+        return c < blocks && (uint32_t)page < (uint32_t)a.pages.n_pages && !always(c) ? key_of(score) : 0;
+    };
     uint32_t kept[KEEP ? KEEP : 1];
     if constexpr (KEEP) {
 #pragma unroll
@@ -348,7 +363,7 @@ __global__ __launch_bounds__(THREADS) void select_kernel(BlockArgs a) {
             if (sure && lane == 0) atomicAdd(&s.above, (uint32_t)__builtin_popcountll(sure));
             if (!k || !is_near(k)) return;
             const uint32_t at = atomicAdd(&s.band_n, 1u);
-            if (at < kBand) s.band_index[at] = first + i, s.band_key[at] = 0;
+            if (at < kBand) s.band_index[at] = first + i, s.band_page[at] = table[first + i], s.band_key[at] = 0;
         });
         __syncthreads();
         const int band = s.band_n;
@@ -356,7 +371,7 @@ __global__ __launch_bounds__(THREADS) void select_kernel(BlockArgs a) {
         if (band <= kBand) {
             if ((uint32_t)band != left) {                // (else all of it)
                 for (int x = tid / 16; x < band * a.G; x += THREADS / 16) {
-                    const uint64_t k = exact_key<BF16>(a, b, h, token, x % a.G, table[s.band_index[x / a.G]]);
+                    const uint64_t k = exact_key<BF16>(a, b, h, token, x % a.G, s.band_page[x / a.G]);
                     if (tid % 16 == 0) atomicMax(&s.band_key[x / a.G], (unsigned long long)k);
                 }
                 __syncthreads();

@@ -104,28 +104,27 @@ __device__ __forceinline__ bool job_of(const PagedArgs& a, bool prefix, Job& j) 
         j.b = unit;
         j.n = length_of(a.q_lengths, j.b, a.q_tokens);
         j.N = length_of(a.kv_lengths, j.b, a.kv_tokens);
+        int used = 0;                                                    // of a list's entries: up to the last block that there is
+        if (LISTED) {                                                    // (asked for with the lengths)
+            const int32_t* list = a.blocks + (((int64_t)j.b * a.pages.n_kv_heads + j.h) * a.q_tokens + j.token) * a.slots;
+            const int lane = threadIdx.x % 64;
+            for (int at = (a.slots - 1) / 64 * 64; at >= 0; at -= 64) {
+                const int32_t block = list[min(at + lane, a.slots - 1)];
+                const uint64_t some = __ballot(at + lane < a.slots && block >= 0);
+                if (some) {
+                    used = at + 64 - __builtin_clzll(some);
+                    break;
+                }
+            }
+        }
         j.row0 = tile * ROWS;
         const int all = LISTED ? j.token < j.n ? a.G : 0 : j.n * a.G;
         j.rows = min(ROWS, all - j.row0);
         if (j.rows <= 0) return false;
         j.begin = LISTED ? 0 : a.shared;
         j.end = j.N;
-        if (!LISTED) {
-            const int last = j.N - j.n + (j.row0 + j.rows - 1) / a.G;
-            j.tiles = max(0, (min(j.N, last + 1) - j.begin + TILE - 1) / TILE);
-        } else {
-            const int32_t* list = a.blocks + (((int64_t)j.b * a.pages.n_kv_heads + j.h) * a.q_tokens + j.token) * a.slots;
-            const int lane = threadIdx.x % 64;
-            int used = 0;                                                // of its entries: up to the last block that there is
-            for (int at = (a.slots - 1) / 64 * 64; at >= 0; at -= 64) {
-                const uint64_t some = __ballot(at + lane < a.slots && list[min(at + lane, a.slots - 1)] >= 0);
-                if (some) {
-                    used = at + 64 - __builtin_clzll(some);
-                    break;
-                }
-            }
-            j.tiles = (int)((((int64_t)used << a.pages.log2) + TILE - 1) / TILE);
-        }
+        if (LISTED) j.tiles = (int)((((int64_t)used << a.pages.log2) + TILE - 1) / TILE);
+        else j.tiles = max(0, (min(j.N, j.N - j.n + (j.row0 + j.rows - 1) / a.G + 1) - j.begin + TILE - 1) / TILE);
     }
     j.i_begin = (int)((int64_t)j.tiles * chunk / chunks);
     j.i_end = (int)((int64_t)j.tiles * (chunk + 1) / chunks);
@@ -307,7 +306,7 @@ __device__ __forceinline__ int least_of_wave(int v) {
 }
 
 constexpr int kTileBytes = 64 * kRowBytes16;   // of keys, or of values
-constexpr int kLds = 4 * kTileBytes;
+constexpr int kWaveBytes = kTileBytes;         // of a wave by itself: 32 positions, keys and values, or the sums of 32 rows
 
 __device__ __forceinline__ uint32_t lds_address(const char* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }
 
@@ -425,7 +424,7 @@ __device__ __forceinline__ void tile_job(const PagedArgs& a, bool prefix, char* 
 // The waves of a workgroup take a chunk's tiles in turn and join their results in LDS at its end.
 template <bool BF16, bool LISTED, int WAVES>
 __device__ __forceinline__ void step_job(const PagedArgs& a, bool prefix, char* lds, float2 (*joined)[kWaveRows]) {
-    constexpr int TILE = 32, HALF = TILE / 2 * kRowBytes16, OWN = kLds / WAVES;
+    constexpr int TILE = 32, HALF = TILE / 2 * kRowBytes16, OWN = kWaveBytes;
     static_assert(OWN >= 2 * TILE * kRowBytes16 && OWN >= kWaveRows * kD * 4, "a wave's part of LDS holds a tile, and its sums");
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     Job j;
@@ -530,7 +529,7 @@ __device__ __forceinline__ void step_job(const PagedArgs& a, bool prefix, char* 
 enum { kSteps, kTilesAndSteps, kTiles };      // of the prefix and the own positions
 template <bool BF16, bool LISTED, int KIND, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void paged_kernel(PagedArgs a) {
-    __shared__ __align__(1024) char lds[kLds];
+    __shared__ __align__(1024) char lds[KIND == kTiles ? 4 * kTileBytes : WAVES * kWaveBytes];
     __shared__ union {
         float2 joined[WAVES][kWaveRows];
         struct {
@@ -554,8 +553,6 @@ __global__ __launch_bounds__(64 * kMergeWaves) void paged_merge_kernel(PagedArgs
     if (WAVES < kMergeWaves && r >= a.merge_rows) return;
     const int Hkv = a.pages.n_kv_heads, head = r % (Hkv * a.G), token = r / (Hkv * a.G) % a.q_tokens, b = r / (Hkv * a.G) / a.q_tokens;
     const int h = head / a.G, g = head % a.G;
-    const int n = length_of(a.q_lengths, b, a.q_tokens);
-    if (token >= n) return;
     const int n_prefix = a.prefix_chunks, parts = n_prefix + a.own_chunks;
     const int prefix_row = (b * a.q_tokens + token) * a.G + g, own_row = LISTED ? g : token * a.G + g;
     const int64_t unit = LISTED ? ((int64_t)b * a.q_tokens + token) * Hkv + h : (int64_t)b * Hkv + h;
@@ -574,6 +571,7 @@ __global__ __launch_bounds__(64 * kMergeWaves) void paged_merge_kernel(PagedArgs
             one[i] = ((const float2*)(shared ? a.prefix_ml : a.own_ml))[at];
             oc[i] = *(const float2*)((shared ? a.prefix_o : a.own_o) + at * kD + 2 * lane);
         }
+        if (token >= length_of(a.q_lengths, b, a.q_tokens)) return;      // (no row: nothing was stored, and nothing is asked of what was loaded)
         float most = m;
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
@@ -617,9 +615,7 @@ __global__ __launch_bounds__(64 * kMergeWaves) void paged_merge_kernel(PagedArgs
     *(uint32_t*)(to + 2 * lane) = pack16<BF16>(x * by, y * by);
 }
 
-constexpr int kStepWaves = 4;
 constexpr int64_t kMostGroups = INT32_MAX / 512;   // a launch's threads are counted in 32 bits
-constexpr int64_t kStepsAtOnce = 512;
 // how a kind of work (the prefix's, the sequences' own) is laid out
 struct Part {
     int row_tiles = 1, item_rows = 1, chunks = 0;
@@ -630,33 +626,39 @@ struct Part {
 constexpr int kMostWaves = 8;
 struct Plan {
     Part prefix, own;
-    int shared = 0, kind = kSteps, waves = kStepWaves;
+    int shared = 0, kind = kSteps, waves = 4;
     bool parts = false;
     int64_t scratch = 0;
 };
 
-// `units` of `rows` rows each over at most `most` positions: by waves by themselves, or (waves of a workgroup) in tiles
-Part part_of(int64_t units, int64_t rows, int64_t most, int waves, bool joined, int64_t at_once = 0) {
+// `units` of `rows` rows each over at most `most` positions, in tiles of 64 by workgroups of `waves` waves
+Part tiles_of(int64_t units, int64_t rows, int64_t most, int waves, int64_t at_once) {
     Part p;
+    p.item_rows = waves * kWaveRows;
+    p.row_tiles = (int)((rows + p.item_rows - 1) / p.item_rows);
+    p.items = units * p.row_tiles;
+    p.chunks = p.items ? (int)std::max<int64_t>(std::min<int64_t>(at_once / p.items, (most + 63) / 64 / 4), 1) : 1;
+    return p;
+}
+// the same by `waves` waves by themselves; joined: the results are joined by a merge anyway
+Part steps_of(int64_t units, int64_t rows, int64_t most, int waves, bool joined) {
+    Part p;
+    p.item_rows = (int)std::min<int64_t>(std::max<int64_t>(rows, 1), kWaveRows);
+    p.row_tiles = (int)((rows + kWaveRows - 1) / kWaveRows);
+    p.items = units * p.row_tiles;
+    const int64_t tiles = (most + 31) / 32, at_once = waves == 8 ? 256 : 512;
     int64_t chunks = 1;
-    if (!waves) {
-        p.item_rows = (int)std::min<int64_t>(std::max<int64_t>(rows, 1), kWaveRows);
-        p.row_tiles = (int)((rows + kWaveRows - 1) / kWaveRows);
-        p.items = units * p.row_tiles;
-        const int64_t tiles = (most + 31) / 32;
-        if (p.items && tiles > (joined ? 4 : 6) * kStepWaves) {
-            chunks = std::max(kStepsAtOnce / p.items, tiles / 64);
-            chunks = std::min({chunks, tiles / kStepWaves, std::max<int64_t>(256, tiles / 64)});
-        }
-    } else {
-        p.item_rows = waves * kWaveRows;
-        p.row_tiles = (int)((rows + p.item_rows - 1) / p.item_rows);
-        p.items = units * p.row_tiles;
-        if (p.items) chunks = std::min<int64_t>(at_once / p.items, (most + 63) / 64 / 4);
+    if (p.items && tiles > (joined ? 4 : 6) * waves) {
+        chunks = std::max(at_once / p.items, tiles / 64);
+        chunks = std::min({chunks, (tiles + waves - 1) / waves, std::max<int64_t>(256, tiles / 64)});
     }
     p.chunks = (int)std::max<int64_t>(chunks, 1);
     return p;
 }
+// Waves of a workgroup of steps: 8 where the rows' workgroups can have a compute unit each.  us, 4 / 8: 64 rows of 19 tiles 11.0 / 9.8, 32 heads of 4 over 5000 positions
+// 13.0 / 11.7, 16 ragged sequences of 8 heads up to 32768 220 / 213; but what is joined with a prefix is better off with more workgroups (three sequences of 32 heads behind 1000
+// shared positions 12.5 / 14.0).
+int step_waves(int64_t units, int64_t rows) { return units * ((rows + kWaveRows - 1) / kWaveRows) <= 256 ? 8 : 4; }
 
 int finish_plan(Plan& p, int64_t merge_rows) {
     if (!p.shared && merge_rows >= kMostGroups) p.own.chunks = 1;
@@ -687,12 +689,22 @@ int plan_of(const specache_pages* cache, const specache_paged_config* c, Plan& p
     if (c->batch > 1 && rows) p.shared = std::min(c->shared_tokens, c->kv_tokens) / cache->page_tokens * cache->page_tokens;
     const int64_t tile = kMostWaves * kWaveRows;
     if (c->batch * ((rows + tile - 1) / tile) * 10 <= (c->batch * rows + tile - 1) / tile * 11) p.shared = 0;
+    const int64_t units = rows ? (int64_t)c->batch * cache->n_kv_heads : 0, own = c->kv_tokens - p.shared;
     if (rows > kWaveRows) {
         p.kind = kTiles;
-        p.waves = std::max(p.shared, c->kv_tokens - p.shared) >= 2048 && rows > 128 ? 8 : 4;
-    } else if (p.shared && c->batch * rows > kWaveRows) p.kind = kTilesAndSteps;
-    if (p.shared) p.prefix = part_of(cache->n_kv_heads, c->batch * rows, p.shared, p.kind == kSteps ? 0 : p.waves, true, p.kind == kTiles ? (p.waves == 8 ? 256 : 512) : 256);
-    p.own = part_of(rows ? (int64_t)c->batch * cache->n_kv_heads : 0, rows, c->kv_tokens - p.shared, p.kind == kTiles ? p.waves : 0, p.shared != 0, p.waves == 8 ? 256 : 512);
+        p.waves = std::max<int64_t>(p.shared, own) >= 2048 && rows > 128 ? 8 : 4;
+        const int64_t at_once = p.waves == 8 ? 256 : 512;
+        if (p.shared) p.prefix = tiles_of(cache->n_kv_heads, c->batch * rows, p.shared, p.waves, at_once);
+        p.own = tiles_of(units, rows, own, p.waves, at_once);
+    } else if (p.shared && c->batch * rows > kWaveRows) {
+        p.kind = kTilesAndSteps;
+        p.prefix = tiles_of(cache->n_kv_heads, c->batch * rows, p.shared, p.waves, 256);
+        p.own = steps_of(units, rows, own, p.waves, true);
+    } else {
+        p.waves = p.shared ? 4 : step_waves(units, rows);
+        if (p.shared) p.prefix = steps_of(cache->n_kv_heads, c->batch * rows, p.shared, p.waves, true);
+        p.own = steps_of(units, rows, own, p.waves, p.shared != 0);
+    }
     return finish_plan(p, c->batch * rows * cache->n_kv_heads);
 }
 
@@ -714,8 +726,10 @@ int plan_of_blocks(const specache_pages* cache, const specache_block_config* c, 
     if (int rc = check_blocks(cache, c)) return rc;
     const int64_t slots = (int64_t)c->top + c->first + c->recent, blocks = (c->kv_tokens + cache->page_tokens - 1) / cache->page_tokens;
     const int64_t units = (int64_t)c->batch * c->q_tokens * cache->n_kv_heads;
-    p.own = part_of(units, c->n_q_heads / cache->n_kv_heads, std::min(slots, blocks) * cache->page_tokens, 0, false);
-    return finish_plan(p, units * (c->n_q_heads / cache->n_kv_heads));
+    const int G = c->n_q_heads / cache->n_kv_heads;
+    p.waves = step_waves(units, G);
+    p.own = steps_of(units, G, std::min(slots, blocks) * cache->page_tokens, p.waves, false);
+    return finish_plan(p, units * G);
 }
 
 }  // namespace
@@ -770,8 +784,8 @@ void launch_merge(const Plan& p, const PagedArgs& a, hipStream_t stream) {
 template <bool BF16, bool LISTED>
 void launch(const Plan& p, const PagedArgs& a, hipStream_t stream) {
     const dim3 grid((unsigned)(p.prefix.groups() + p.own.groups()));
-    const auto kernel = LISTED || p.kind == kSteps ? paged_kernel<BF16, LISTED, kSteps, kStepWaves>
-                        : p.kind == kTilesAndSteps ? paged_kernel<BF16, false, kTilesAndSteps, kStepWaves>
+    const auto kernel = LISTED || p.kind == kSteps ? (p.waves == 8 ? paged_kernel<BF16, LISTED, kSteps, 8> : paged_kernel<BF16, LISTED, kSteps, 4>)
+                        : p.kind == kTilesAndSteps ? paged_kernel<BF16, false, kTilesAndSteps, 4>
                         : p.waves == 8             ? paged_kernel<BF16, false, kTiles, 8>
                                                    : paged_kernel<BF16, false, kTiles, 4>;
     hipLaunchKernelGGL(kernel, grid, dim3(64 * p.waves), 0, stream, a);
