@@ -133,13 +133,13 @@ def lib():
         L.specache_window_attend.argtypes = [C.POINTER(WindowConfig), view, view, view, view, vp, vp, vp, i64, vp]
         L.specache_sample_scratch.argtypes = [C.POINTER(SampleConfig), C.POINTER(i64)]
         L.specache_sample.argtypes = [C.POINTER(SampleConfig), vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
-        pages = C.POINTER(PagesConfig)
+        pages, cfg = vp, vp            # (addresses of PagesConfig, PagedConfig and BlockConfig structures)
         L.specache_paged_append.argtypes = [pages, C.POINTER(Rotary), i32, i32, i32, view, view, view, view, vp, vp, vp, vp]
-        L.specache_paged_scratch.argtypes = [pages, C.POINTER(PagedConfig), C.POINTER(i64)]
-        L.specache_paged_attend.argtypes = [pages, C.POINTER(PagedConfig), view, view, vp, vp, vp, i64, vp]
-        L.specache_block_scratch.argtypes = [pages, C.POINTER(BlockConfig), C.POINTER(i64)]
-        L.specache_block_select.argtypes = [pages, C.POINTER(BlockConfig), view, vp, vp, vp, vp, i64, vp]
-        L.specache_block_attend.argtypes = [pages, C.POINTER(BlockConfig), view, view, vp, vp, vp, vp, i64, vp]
+        L.specache_paged_scratch.argtypes = [pages, cfg, C.POINTER(i64)]
+        L.specache_paged_attend.argtypes = [pages, cfg, view, view, vp, vp, vp, i64, vp]
+        L.specache_block_scratch.argtypes = [pages, cfg, C.POINTER(i64)]
+        L.specache_block_select.argtypes = [pages, cfg, view, vp, vp, vp, vp, i64, vp]
+        L.specache_block_attend.argtypes = [pages, cfg, view, view, vp, vp, vp, vp, i64, vp]
         for name in EXPORTS:
             if name != "specache_last_error":
                 getattr(L, name).restype = C.c_int
@@ -265,7 +265,7 @@ class _Views(threading.local):
 
 
 _room = _Views()
-_PACK = {n: struct.Struct(f"{4 * n}q").pack_into for n in (1, 2, 3, 4, 6)}
+_PACK = {n: struct.Struct(f"{4 * n}q").pack_into for n in (3, 4, 6)}
 
 
 def _views(device, dtype, names, tensors, shapes):
@@ -301,7 +301,7 @@ def _scratch(t, device):
         return None, 0
     if t.get_device() != device or not t.is_contiguous():
         _refuse("scratch must be contiguous and on the current device")
-    return t.data_ptr(), t.numel() * t.element_size()
+    return t.data_ptr(), t.nbytes
 
 
 def rotary_plan(rotary_dim=128, base=10000.0, layout=ROTARY_HALF, scaling=ROTARY_UNSCALED, factor=1.0, original_tokens=0,
@@ -378,6 +378,31 @@ def sample(logits, u, tokens, temperature=None, top_k=None, top_p=None, min_p=No
                                 _flat(tokens, shape, i32, device, "tokens"), address, size, _current(stream)))
 
 
+class _Room(threading.local):
+    """Room for two specache_views and a configuration behind them, packed at once."""
+
+    def __init__(self):
+        self.room = (C.c_int64 * 12)()
+        self.q = C.addressof(self.room)
+        self.out, self.cfg = self.q + 32, self.q + 64
+
+
+_call = _Room()
+_PACK_PAGED = struct.Struct("8q5if").pack_into
+_PACK_BLOCKS = struct.Struct("8q7if").pack_into
+_WIDE = "counts must be whole numbers of 32 bits, sm_scale a finite one"
+
+
+def _rows(t, shape, kind, device, name):
+    """The fields of a [B, H, n, 128] tensor's specache_view."""
+    if t.shape != shape or t.dtype is not kind or t.get_device() != device:
+        _refuse(f"{name} must be a {tuple(shape)} tensor of the cache's type on the current device")
+    b, h, n, c = t.stride()
+    if c != 1:
+        _refuse(f"{name}: the channels must lie side by side")
+    return t.data_ptr(), b if shape[0] > 1 else 0, h if shape[1] > 1 else 0, n if shape[2] > 1 else 0
+
+
 class Pages:
     """A layer's paged cache for the calls below: k, v [pages, Hkv, page_tokens, 128] and bounds [pages, Hkv, 2, 128] (views as they are), table [B, table_pages]
     int32 (a row's entries side by side).  It keeps the tensors; what is in them may change between calls."""
@@ -390,34 +415,38 @@ class Pages:
         views = _views(self.device, k.dtype, ("k", "v", "bounds"), (k, v, bounds), (k.shape, k.shape, (P, H, 2, 128)))
         if table.dim() != 2 or table.dtype is not _torch.int32 or table.get_device() != self.device or (table.shape[1] > 1 and table.stride(1) != 1):
             _refuse("table must be a [batch, pages] tensor of int32 on the current device, a row's entries side by side")
-        self.batch, self.places = table.shape[0], table.shape[1] * T
+        self.batch, self.kv_heads, self.places = table.shape[0], H, table.shape[1] * T
         self.config = PagesConfig(*(View.from_address(at) for at in views[:3]), table.data_ptr(), table.stride(0) if table.shape[0] > 1 else table.shape[1],
                                   P, H, T, table.shape[1], 128, _type_of(k))
-        self.at = C.byref(self.config)
+        self.at = C.addressof(self.config)
 
-    def _take(self, q, *others):
-        """Addresses of q's and the others' views, which have q's shape [B, Hq, n, 128]; and the counts."""
+    def _shape(self, q):
+        """q's shape and the device, checked against the cache's."""
         shape, device = q.shape, _here()
         if device != self.device:
             _refuse("the cache is not on the current device")
         if len(shape) != 4 or shape[3] != 128 or shape[0] != self.batch:
             _refuse("q is [B, Hq, n, 128], with as many sequences as the table has")
-        tensors = (q,) + others
-        return device, shape, _views(device, self.kind, ("q", "out")[:len(tensors)], tensors, (shape,) * len(tensors))
+        return shape, device
 
 
 def paged_append(cache, plan, k, v, q=None, q_out=None, starts=None, lengths=None, positions=None, stream=None):
     """k, v [B, Hkv, n, 128] to positions starts[b] .. of the cache, k turned by plan (None: as it is); q [B, Hq, n, 128] turned into q_out."""
     B, _, n, _ = k.shape
-    H = cache.config.n_kv_heads
-    device = _here()
+    device, H, kind = _here(), cache.kv_heads, cache.kind
     if device != cache.device or B != cache.batch:
         _refuse("the cache is not on the current device, or has other sequences")
     if (q is None) != (q_out is None):
         _refuse("a tensor and its output are given or left out together")
-    heads = 0 if q is None else q.shape[1]
-    a = _views(device, cache.kind, ("q", "q_out", "k", "v"), (q, q_out, k, v), ((B, heads, n, 128), (B, heads, n, 128), (B, H, n, 128), (B, H, n, 128)))
-    i32 = _torch.int32
+    if q is None:
+        heads, rows, out = 0, (0, 0, 0, 0), (0, 0, 0, 0)
+    else:
+        heads = q.shape[1]
+        shape = (B, heads, n, 128)
+        rows, out = _rows(q, shape, kind, device, "q"), _rows(q_out, shape, kind, device, "q_out")
+    shape = (B, H, n, 128)
+    _PACK[4](_room.room, 0, *rows, *out, *_rows(k, shape, kind, device, "k"), *_rows(v, shape, kind, device, "v"))
+    a, i32 = _room.at, _torch.int32
     _done(lib().specache_paged_append(cache.at, None if plan is None else C.byref(plan), B, n, heads, a[0], a[1], a[2], a[3],
                                       _flat(starts, (B,), i32, device, "starts"), _flat(lengths, (B,), i32, device, "lengths"),
                                       _flat(positions, (B, n), i32, device, "positions"), _current(stream)))
@@ -433,11 +462,17 @@ def paged_scratch(cache, batch, n_q_heads, q_tokens, kv_tokens, shared_tokens=0)
 def paged_attend(cache, q, out, kv_tokens=None, shared_tokens=0, q_lengths=None, kv_lengths=None, sm_scale=0.0, scratch=None, stream=None):
     """Attention of q [B, Hq, n, 128] over the cache's positions (kv_tokens at most; None: what the table holds), whose first shared_tokens the sequences
     share, into out (q's shape)."""
-    device, (B, Hq, n, _), a = cache._take(q, out)
-    cfg = PagedConfig(B, Hq, n, cache.places if kv_tokens is None else kv_tokens, shared_tokens, sm_scale)
+    shape, device = cache._shape(q)
+    B, Hq, n, _ = shape
+    kind, i32, c = cache.kind, _torch.int32, _call
+    try:
+        _PACK_PAGED(c.room, 0, *_rows(q, shape, kind, device, "q"), *_rows(out, shape, kind, device, "out"),
+                    B, Hq, n, cache.places if kv_tokens is None else kv_tokens, shared_tokens, sm_scale)
+    except (struct.error, OverflowError):
+        _refuse(_WIDE)
     address, size = _scratch(scratch, device)
-    _done(lib().specache_paged_attend(cache.at, C.byref(cfg), a[0], a[1], _flat(q_lengths, (B,), _torch.int32, device, "q_lengths"),
-                                      _flat(kv_lengths, (B,), _torch.int32, device, "kv_lengths"), address, size, _current(stream)))
+    _done(lib().specache_paged_attend(cache.at, c.cfg, c.q, c.out, _flat(q_lengths, (B,), i32, device, "q_lengths"),
+                                      _flat(kv_lengths, (B,), i32, device, "kv_lengths"), address, size, _current(stream)))
 
 
 def block_scratch(cache, batch, n_q_heads, q_tokens, kv_tokens, top, first=0, recent=0):
@@ -449,27 +484,39 @@ def block_scratch(cache, batch, n_q_heads, q_tokens, kv_tokens, top, first=0, re
 
 def block_select(cache, q, blocks, kv_tokens=None, top=0, first=0, recent=0, q_lengths=None, kv_lengths=None, scratch=None, stream=None):
     """blocks [B, Hkv, n, first + top + recent] of int32: the blocks of the cache (its pages) that the rows of q [B, Hq, n, 128] see."""
-    device, (B, Hq, n, _), a = cache._take(q)
-    cfg = BlockConfig(B, Hq, n, cache.places if kv_tokens is None else kv_tokens, top, first, recent)
-    address, size = _scratch(scratch, device)
-    lists = _flat(blocks, (B, cache.config.n_kv_heads, n, first + top + recent), _torch.int32, device, "blocks")
+    shape, device = cache._shape(q)
+    B, Hq, n, _ = shape
+    i32, c = _torch.int32, _call
     if cache.bounds is None and top > 0:
         _refuse("the cache keeps no bounds")
-    _done(lib().specache_block_select(cache.at, C.byref(cfg), a[0], lists, _flat(q_lengths, (B,), _torch.int32, device, "q_lengths"),
-                                      _flat(kv_lengths, (B,), _torch.int32, device, "kv_lengths"), address, size, _current(stream)))
+    lists = _flat(blocks, (B, cache.kv_heads, n, first + top + recent), i32, device, "blocks")
+    try:
+        _PACK_BLOCKS(c.room, 0, *_rows(q, shape, cache.kind, device, "q"), 0, 0, 0, 0,
+                     B, Hq, n, cache.places if kv_tokens is None else kv_tokens, top, first, recent, 0.0)
+    except (struct.error, OverflowError):
+        _refuse(_WIDE)
+    address, size = _scratch(scratch, device)
+    _done(lib().specache_block_select(cache.at, c.cfg, c.q, lists, _flat(q_lengths, (B,), i32, device, "q_lengths"),
+                                      _flat(kv_lengths, (B,), i32, device, "kv_lengths"), address, size, _current(stream)))
 
 
 def block_attend(cache, q, out, blocks, kv_tokens=None, q_lengths=None, kv_lengths=None, sm_scale=0.0, scratch=None, stream=None):
     """Attention of q [B, Hq, n, 128] over the listed blocks [B, Hkv, n, entries] of the cache, into out (q's shape)."""
-    device, (B, Hq, n, _), a = cache._take(q, out)
+    shape, device = cache._shape(q)
+    B, Hq, n, _ = shape
+    kind, i32, c = cache.kind, _torch.int32, _call
     if blocks.dim() != 4:
         _refuse("blocks is [B, Hkv, n, entries]")
     slots = blocks.shape[3]
-    cfg = BlockConfig(B, Hq, n, cache.places if kv_tokens is None else kv_tokens, slots, 0, 0, sm_scale)
+    lists = _flat(blocks, (B, cache.kv_heads, n, slots), i32, device, "blocks")
+    try:
+        _PACK_BLOCKS(c.room, 0, *_rows(q, shape, kind, device, "q"), *_rows(out, shape, kind, device, "out"),
+                     B, Hq, n, cache.places if kv_tokens is None else kv_tokens, slots, 0, 0, sm_scale)
+    except (struct.error, OverflowError):
+        _refuse(_WIDE)
     address, size = _scratch(scratch, device)
-    lists = _flat(blocks, (B, cache.config.n_kv_heads, n, slots), _torch.int32, device, "blocks")
-    _done(lib().specache_block_attend(cache.at, C.byref(cfg), a[0], a[1], lists, _flat(q_lengths, (B,), _torch.int32, device, "q_lengths"),
-                                      _flat(kv_lengths, (B,), _torch.int32, device, "kv_lengths"), address, size, _current(stream)))
+    _done(lib().specache_block_attend(cache.at, c.cfg, c.q, c.out, lists, _flat(q_lengths, (B,), i32, device, "q_lengths"),
+                                      _flat(kv_lengths, (B,), i32, device, "kv_lengths"), address, size, _current(stream)))
 
 
 class SpeCache:

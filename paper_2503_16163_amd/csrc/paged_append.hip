@@ -2,17 +2,18 @@
 //
 // The first workgroups take the keys and values, the others the queries.  A workgroup of keys holds what one call brings to one page (a segment), so that
 // the page's bounds need no atomics: it walks the segment's tokens head by head, keeps the running minimum and maximum of its lanes' channels in registers,
-// and joins them in LDS.  Memory is what bounds it; a step's tokens, one to a page, are spread over heads instead.
+// and joins them across rows in the waves and between waves in LDS.  Memory is what bounds it; a step's tokens, one to a page, are spread over heads instead.
 #include <cmath>
 
 #include "pages.h"
 #include "rotate16.h"
+#include "wave_ops.h"
 
 namespace specache {
 namespace {
 
 constexpr int kThreads = 256, kSlots = kThreads / kParts;   // rows that a workgroup has in hand at a time
-constexpr int kAhead = 4;
+constexpr int kAhead = 4, kAheadPairs = 2;   // rows whose loads a lane has in flight: queries, and keys with their values
 constexpr int64_t kMostGroups = (1ll << 32) / kThreads - 1;
 
 struct AppendArgs {
@@ -28,27 +29,70 @@ struct AppendArgs {
     int q_splits;
 };
 
-// kThreads lanes; the least and the largest of what the lanes of a part (and of a head, where HEADS share the workgroup) hold
+// The least and the largest of what a lane has had of a head, channels 8 part and 64 + 8 part on: as signed whole numbers of 16 bits that are in order as the numbers are (all
+// bits but the sign's turned over where that is set), which a register has two of.
+typedef short short8v __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ short8v in_order(short8v x) { return x ^ ((x >> (short)15) & (short)0x7FFF); }   // (and back)
+template <bool BF16>
 struct Bounds {
-    float least[16], most[16];
+    static constexpr short kInfinity = BF16 ? 0x7F80 : 0x7C00;
+    short8v least[2], most[2];         // of the two accesses
+    static __device__ __forceinline__ short8v numbers(const uint4& x) { return __builtin_bit_cast(short8v, x); }
     __device__ __forceinline__ void clear() {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) least[i] = INFINITY, most[i] = -INFINITY;
+        for (int i = 0; i < 2; ++i) least[i] = kInfinity, most[i] = (short)~kInfinity;
     }
-    template <bool BF16>
-    __device__ __forceinline__ void take(const uint4& u0, const uint4& u1) {
-        float x[2][8];
-        unpack8<BF16>(u0, x[0]);
-        unpack8<BF16>(u1, x[1]);
+    __device__ __forceinline__ void take(const uint4 (&u)[2]) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            least[i] = fminf(least[i], x[i / 8][i % 8]);
-            most[i] = fmaxf(most[i], x[i / 8][i % 8]);
+        for (int i = 0; i < 2; ++i) {
+            const short8v x = numbers(u[i]), y = in_order(x), odd = (x & (short)0x7FFF) > kInfinity;   // a NaN (all ones there) is passed over
+            least[i] = __builtin_elementwise_min(least[i], (y & ~odd) | (kInfinity & odd));
+            most[i] = __builtin_elementwise_max(most[i], (y & ~odd) | ((short)~kInfinity & odd));
         }
+    }
+    // by the bounds that were: the least's two accesses, the most's
+    __device__ __forceinline__ void widen(const uint4 (&old)[4]) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            least[i] = __builtin_elementwise_min(least[i], in_order(numbers(old[i])));
+            most[i] = __builtin_elementwise_max(most[i], in_order(numbers(old[2 + i])));
+        }
+    }
+    // with those of the lanes 8 ROWS away
+    template <int ROWS>
+    __device__ __forceinline__ void meet() {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint4v l = __builtin_bit_cast(uint4v, least[i]), m = __builtin_bit_cast(uint4v, most[i]);
+            uint4v a[2], b[2];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                both<ROWS>(l[c], a, c);
+                both<ROWS>(m[c], b, c);
+            }
+            least[i] = __builtin_elementwise_min(__builtin_bit_cast(short8v, a[0]), __builtin_bit_cast(short8v, a[1]));
+            most[i] = __builtin_elementwise_max(__builtin_bit_cast(short8v, b[0]), __builtin_bit_cast(short8v, b[1]));
+        }
+    }
+    // a lane's own and the other's, in some order
+    template <int ROWS, typename V>
+    static __device__ __forceinline__ void both(uint32_t x, V (&y)[2], int c) {
+        if constexpr (ROWS == 1) {
+            y[0][c] = x, y[1][c] = dpp_move_u32<kDppRowRor8>(x);
+        } else {
+            const auto p = ROWS == 2 ? __builtin_amdgcn_permlane16_swap(x, x, false, false) : __builtin_amdgcn_permlane32_swap(x, x, false, false);
+            y[0][c] = p[0], y[1][c] = p[1];
+        }
+    }
+    // of `rows` neighbouring rows of a wave: 1, 2, 4 or 8
+    __device__ __forceinline__ void meet_rows(int rows) {
+        if (rows > 1) meet<1>();
+        if (rows > 2) meet<2>();
+        if (rows > 4) meet<4>();
     }
 };
 
-template <bool BF16, bool HALF, bool STREAM>
+template <bool BF16, bool HALF, bool PART, bool STREAM>
 __device__ __forceinline__ void append_queries(const AppendArgs& a, int group) {
     const int part = threadIdx.x % kParts, slot = threadIdx.x / kParts;
     const int tile = 1 << a.q_tile_log2, tiles = (a.tokens + tile - 1) >> a.q_tile_log2;
@@ -67,24 +111,26 @@ __device__ __forceinline__ void append_queries(const AppendArgs& a, int group) {
         uint4 u[kAhead][2];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            const int h = h0 + i * step;
-            if (h >= a.n_q_heads) continue;
+            const int h = min(h0 + i * step, a.n_q_heads - 1);           // (of the last one again nothing is kept)
             u[i][0] = *(const uint4*)(from + h * a.q.head + parts.c0);
             u[i][1] = *(const uint4*)(from + h * a.q.head + parts.c1);
         }
 #pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (turns) turn.apply(u[i][0], u[i][1], parts.turns[1]);
+        if constexpr (PART) deal_lines(u, part, a.plan.rotary_dim);
+#pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             const int h = h0 + i * step;
             if (h >= a.n_q_heads) continue;
-            if (turns) turn.apply(u[i][0], u[i][1], parts.turns[1]);
-            store16<STREAM>(to + h * a.q_out.head + parts.c0, u[i][0]);
-            store16<STREAM>(to + h * a.q_out.head + parts.c1, u[i][1]);
+            store16<STREAM>(to + h * a.q_out.head + 8 * part, u[i][0]);
+            store16<STREAM>(to + h * a.q_out.head + kD / 2 + 8 * part, u[i][1]);
         }
     }
 }
 
-template <bool BF16, bool HALF, bool STREAM, bool BOUNDS>
-__device__ __forceinline__ void append_pairs(const AppendArgs& a, int group, float (*joined)[kParts][2][16]) {
+template <bool BF16, bool HALF, bool PART, bool STREAM, bool BOUNDS>
+__device__ __forceinline__ void append_pairs(const AppendArgs& a, int group, uint4v (*joined)[BOUNDS ? kThreads / 64 : 1][2][2][kParts]) {
     const int part = threadIdx.x % kParts, slot = threadIdx.x / kParts, tile = 1 << a.key_tile_log2;
     const int split = group % a.key_splits, segment = group / a.key_splits % a.segments, b = group / a.key_splits / a.segments;
     const int n = length_of(a.lengths, b, a.tokens);
@@ -105,71 +151,137 @@ __device__ __forceinline__ void append_pairs(const AppendArgs& a, int group, flo
     const uint16_t* from_v = (const uint16_t*)a.v.data + b * a.v.batch + t0 * a.v.token;
     uint16_t* to_k = (uint16_t*)a.pages.k.data + page * a.pages.k.batch + place0 * a.pages.k.token;
     uint16_t* to_v = (uint16_t*)a.pages.v.data + page * a.pages.v.batch + place0 * a.pages.v.token;
-    int turned = -1;
-    for (int hh = split * heads_here; hh < a.pages.n_kv_heads; hh += step) {
-        const int h = hh + (slot >> a.key_tile_log2);
-        Bounds bounds;
-        bounds.clear();
-        for (int pass = 0; pass < passes; ++pass) {
-            const int i = pass * tile + (slot & (tile - 1));
-            if (i >= tokens || h >= a.pages.n_kv_heads) continue;
-            uint4 u[2], w[2];
-            u[0] = *(const uint4*)(from_k + h * a.k.head + i * a.k.token + parts.c0);
-            u[1] = *(const uint4*)(from_k + h * a.k.head + i * a.k.token + parts.c1);
-            w[0] = *(const uint4*)(from_v + h * a.v.head + i * a.v.token + parts.c0);
-            w[1] = *(const uint4*)(from_v + h * a.v.head + i * a.v.token + parts.c1);
+    int turned = -1, turn_of_heads = 0;
+    // The rows of up to 8 tokens are in one wave: their bounds meet there, and the page's own ones travel with the rows (a step's 16 tokens 4.4 us against 5.9 through LDS).
+    const bool few = tile <= 8;
+    const int heads = (a.pages.n_kv_heads - split * heads_here + step - 1) / step;    // of these lanes
+    Bounds<BF16> bounds;
+    uint16_t* kept = nullptr;
+    // kAheadPairs rows at a time, head by head and in them pass by pass: all loads, then all stores, as a load behind a store waits for that as well
+    for (int f0 = 0; f0 < heads * passes; f0 += kAheadPairs) {
+        uint4 u[kAheadPairs][2], w[kAheadPairs][2];
+#pragma unroll
+        for (int x = 0; x < kAheadPairs; ++x) {
+            const int f = min(f0 + x, heads * passes - 1), i = min(f % passes * tile + (slot & (tile - 1)), tokens - 1);
+            const int h = min(split * heads_here + f / passes * step + (slot >> a.key_tile_log2), a.pages.n_kv_heads - 1);
+            u[x][0] = *(const uint4*)(from_k + h * a.k.head + i * a.k.token + parts.c0);
+            u[x][1] = *(const uint4*)(from_k + h * a.k.head + i * a.k.token + parts.c1);
+            w[x][0] = *(const uint4*)(from_v + h * a.v.head + i * a.v.token + 8 * part);
+            w[x][1] = *(const uint4*)(from_v + h * a.v.head + i * a.v.token + kD / 2 + 8 * part);
+        }
+        uint4 old[4] = {};
+        if (BOUNDS && few && place0) {                   // (kAheadPairs heads at most: one by one)
+            const int h = min(split * heads_here + f0 * step + (slot >> a.key_tile_log2), a.pages.n_kv_heads - 1);
+            const uint16_t* from = (const uint16_t*)a.pages.bounds.data + page * a.pages.bounds.batch + h * a.pages.bounds.head + 8 * part;
+            old[0] = *(const uint4*)from;
+            old[1] = *(const uint4*)(from + kD / 2);
+            old[2] = *(const uint4*)(from + a.pages.bounds.token);
+            old[3] = *(const uint4*)(from + a.pages.bounds.token + kD / 2);
+        }
+#pragma unroll
+        for (int x = 0; x < kAheadPairs; ++x) {
+            const int pass = (f0 + x) % passes;
             if (turns) {
+                const int i = min(pass * tile + (slot & (tile - 1)), tokens - 1);
                 if (turned != pass) turn.set(a.plan, part, a.positions ? a.positions[(int64_t)b * a.tokens + t0 + i] : low + i);
                 turned = pass;
-                turn.apply(u[0], u[1], parts.turns[1]);
+                turn.apply(u[x][0], u[x][1], parts.turns[1]);
             }
-            store16<STREAM>(to_k + h * a.pages.k.head + i * a.pages.k.token + parts.c0, u[0]);
-            store16<STREAM>(to_k + h * a.pages.k.head + i * a.pages.k.token + parts.c1, u[1]);
-            store16<STREAM>(to_v + h * a.pages.v.head + i * a.pages.v.token + parts.c0, w[0]);
-            store16<STREAM>(to_v + h * a.pages.v.head + i * a.pages.v.token + parts.c1, w[1]);
-            if constexpr (BOUNDS) bounds.take<BF16>(u[0], u[1]);
+        }
+        if constexpr (PART) deal_lines(u, part, a.plan.rotary_dim);
+#pragma unroll
+        for (int x = 0; x < kAheadPairs; ++x) {
+            const int f = f0 + x, i = f % passes * tile + (slot & (tile - 1)), h = split * heads_here + f / passes * step + (slot >> a.key_tile_log2);
+            if (f >= heads * passes || i >= tokens || h >= a.pages.n_kv_heads) continue;
+            uint16_t* k = to_k + h * a.pages.k.head + i * a.pages.k.token + 8 * part;
+            uint16_t* v = to_v + h * a.pages.v.head + i * a.pages.v.token + 8 * part;
+            store16<STREAM>(k, u[x][0]);
+            store16<STREAM>(k + kD / 2, u[x][1]);
+            store16<STREAM>(v, w[x][0]);
+            store16<STREAM>(v + kD / 2, w[x][1]);
         }
         if constexpr (BOUNDS) {
-            __syncthreads();           // (what the head before left there has been read)
 #pragma unroll
-            for (int c = 0; c < 16; ++c) joined[slot][part][0][c] = bounds.least[c], joined[slot][part][1][c] = bounds.most[c];
-            __syncthreads();
-            // one thread to a head, part and bound's access of 8 channels
-            for (int x = threadIdx.x; x < heads_here * kParts * 4; x += kThreads) {
-                const int p = x % kParts, which = x / kParts % 2, access = x / kParts / 2 % 2, head = hh + x / kParts / 4;
-                if (head >= a.pages.n_kv_heads) continue;
-                const RowParts<HALF> places(p, a.plan.rotary_dim);
-                uint16_t* to = (uint16_t*)a.pages.bounds.data + page * a.pages.bounds.batch + head * a.pages.bounds.head + which * a.pages.bounds.token + (access ? places.c1 : places.c0);
-                float y[8];
-                if (place0 == 0) {
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) y[c] = which ? -INFINITY : INFINITY;
-                } else unpack8<BF16>(*(const uint4*)to, y);
-                const int slot0 = (x / kParts / 4) << a.key_tile_log2;
-                for (int s = 0; s < min(tile, tokens); ++s)
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        const float v = joined[slot0 + s][p][which][8 * access + c];
-                        y[c] = which ? fmaxf(y[c], v) : fminf(y[c], v);
+            for (int x = 0; x < kAheadPairs; ++x) {
+                const int f = f0 + x, pass = f % passes, i = pass * tile + (slot & (tile - 1)), hh = split * heads_here + f / passes * step;
+                const int h = hh + (slot >> a.key_tile_log2);
+                if (f >= heads * passes) break;
+                if (pass == 0) bounds.clear();
+                if (i < tokens && h < a.pages.n_kv_heads) bounds.take(u[x]);
+                if (pass + 1 < passes) continue;
+                if (few) {
+                    kept = (uint16_t*)a.pages.bounds.data + page * a.pages.bounds.batch + h * a.pages.bounds.head + 8 * part;
+                    const bool writes = (slot & (tile - 1)) == 0 && h < a.pages.n_kv_heads;
+                    if (place0 && writes) {
+                        if (x) {                         // (only the first head's were asked for ahead)
+                            old[0] = *(const uint4*)kept;
+                            old[1] = *(const uint4*)(kept + kD / 2);
+                            old[2] = *(const uint4*)(kept + a.pages.bounds.token);
+                            old[3] = *(const uint4*)(kept + a.pages.bounds.token + kD / 2);
+                        }
+                        bounds.widen(old);
                     }
-                *(uint4*)to = pack8<BF16>(y);
+                    bounds.meet_rows(tile);
+                    if (writes) {
+                        *(short8v*)kept = in_order(bounds.least[0]);
+                        *(short8v*)(kept + kD / 2) = in_order(bounds.least[1]);
+                        *(short8v*)(kept + a.pages.bounds.token) = in_order(bounds.most[0]);
+                        *(short8v*)(kept + a.pages.bounds.token + kD / 2) = in_order(bounds.most[1]);
+                    }
+                    continue;
+                }
+                // a wave's 8 rows meet in it, the waves of a head in LDS (by turns in one of two places: a barrier is between a place's reads and its next writes)
+                bounds.meet_rows(8);
+                auto place = joined[turn_of_heads];
+                turn_of_heads ^= 1;
+                if (slot % 8 == 0) {
+#pragma unroll
+                    for (int access = 0; access < 2; ++access) {
+                        place[slot / 8][0][access][part] = __builtin_bit_cast(uint4v, bounds.least[access]);
+                        place[slot / 8][1][access][part] = __builtin_bit_cast(uint4v, bounds.most[access]);
+                    }
+                }
+                __syncthreads();
+                // one thread to a head, part and bound's access of 8 channels
+                const int waves = tile / 8, y = threadIdx.x, p = y % kParts, which = y / kParts % 2, access = y / kParts / 2 % 2, head = hh + y / kParts / 4;
+                if (y < heads_here * kParts * 4 && head < a.pages.n_kv_heads) {
+                    uint4v* const to = (uint4v*)((uint16_t*)a.pages.bounds.data + page * a.pages.bounds.batch + head * a.pages.bounds.head + which * a.pages.bounds.token + access * (kD / 2) + 8 * p);
+                    const int wave0 = y / kParts / 4 * waves;
+                    short8v z = __builtin_bit_cast(short8v, place[wave0][which][access][p]);
+                    for (int s = 1; s < waves; ++s) {
+                        const short8v v = __builtin_bit_cast(short8v, place[wave0 + s][which][access][p]);
+                        z = which ? __builtin_elementwise_max(z, v) : __builtin_elementwise_min(z, v);
+                    }
+                    if (place0) {
+                        const short8v v = in_order(__builtin_bit_cast(short8v, *to));
+                        z = which ? __builtin_elementwise_max(z, v) : __builtin_elementwise_min(z, v);
+                    }
+                    *to = __builtin_bit_cast(uint4v, in_order(z));
+                }
             }
         }
     }
 }
 
-template <bool BF16, bool HALF, bool STREAM, bool BOUNDS>
-__global__ __launch_bounds__(kThreads) void paged_append_kernel(AppendArgs a) {
-    __shared__ float joined[BOUNDS ? kSlots : 1][kParts][2][16];
-    if ((int)blockIdx.x < a.key_groups) append_pairs<BF16, HALF, STREAM, BOUNDS>(a, blockIdx.x, joined);
-    else append_queries<BF16, HALF, STREAM>(a, blockIdx.x - a.key_groups);
+// HALF: pairs of channels are halves of what is turned; PART: which is less than the head
+template <bool BF16, bool HALF, bool PART, bool STREAM, bool BOUNDS>
+__global__ __launch_bounds__(kThreads, 4) void paged_append_kernel(AppendArgs a) {
+    __shared__ uint4v joined[2][BOUNDS ? kThreads / 64 : 1][2][2][kParts];   // [turn][wave][least, most][access][part]
+    if ((int)blockIdx.x < a.key_groups) append_pairs<BF16, HALF, PART, STREAM, BOUNDS>(a, blockIdx.x, joined);
+    else append_queries<BF16, HALF, PART, STREAM>(a, blockIdx.x - a.key_groups);
 }
 
-template <bool BF16, bool HALF>
+template <bool BF16, bool HALF, bool PART>
 void launch(const AppendArgs& a, int64_t groups, bool stream_out, bool bounds, hipStream_t stream) {
-    const auto kernel = stream_out ? (bounds ? paged_append_kernel<BF16, HALF, true, true> : paged_append_kernel<BF16, HALF, true, false>)
-                                   : (bounds ? paged_append_kernel<BF16, HALF, false, true> : paged_append_kernel<BF16, HALF, false, false>);
+    const auto kernel = stream_out ? (bounds ? paged_append_kernel<BF16, HALF, PART, true, true> : paged_append_kernel<BF16, HALF, PART, true, false>)
+                                   : (bounds ? paged_append_kernel<BF16, HALF, PART, false, true> : paged_append_kernel<BF16, HALF, PART, false, false>);
     hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kThreads), 0, stream, a);
+}
+template <bool BF16>
+void launch(const AppendArgs& a, int64_t groups, bool stream_out, bool bounds, hipStream_t stream) {
+    if (a.turns && a.plan.layout == SPECACHE_ROTARY_INTERLEAVED) launch<BF16, false, false>(a, groups, stream_out, bounds, stream);
+    else if (a.plan.rotary_dim == kD) launch<BF16, true, false>(a, groups, stream_out, bounds, stream);
+    else launch<BF16, true, true>(a, groups, stream_out, bounds, stream);
 }
 
 }  // namespace
@@ -234,9 +346,8 @@ extern "C" int specache_paged_append(const specache_pages* cache, const specache
     if (!groups) return SPECACHE_OK;
     if (groups >= kMostGroups) return fail_without_context(SPECACHE_EINVAL, "too many tokens");
     a.key_groups = (int)key_groups;
-    const bool half = !plan || plan->layout == SPECACHE_ROTARY_HALF;
-    const bool stream_out = (int64_t)batch * tokens * (n_q_heads + 2 * cache->n_kv_heads) * kD * 2 > kCached && (!half || a.plan.rotary_dim == kD);
-    if (cache->dtype == SPECACHE_BF16) half ? launch<true, true>(a, groups, stream_out, bounds, (hipStream_t)stream) : launch<true, false>(a, groups, stream_out, bounds, (hipStream_t)stream);
-    else half ? launch<false, true>(a, groups, stream_out, bounds, (hipStream_t)stream) : launch<false, false>(a, groups, stream_out, bounds, (hipStream_t)stream);
+    const bool stream_out = (int64_t)batch * tokens * (n_q_heads + 2 * cache->n_kv_heads) * kD * 2 > kCached;
+    if (cache->dtype == SPECACHE_BF16) launch<true>(a, groups, stream_out, bounds, (hipStream_t)stream);
+    else launch<false>(a, groups, stream_out, bounds, (hipStream_t)stream);
     return launched();
 }

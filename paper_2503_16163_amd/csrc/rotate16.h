@@ -12,7 +12,7 @@ typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 template <bool STREAM>
 __device__ __forceinline__ void store16(uint16_t* to, const uint4& v) {
     if constexpr (STREAM) __builtin_nontemporal_store(__builtin_bit_cast(uint4v, v), (uint4v*)to);
-    else *(uint4*)to = v;
+    else *(uint4v*)to = __builtin_bit_cast(uint4v, v);
 }
 template <bool BF16>
 __device__ __forceinline__ void unpack8(const uint4& u, float (&x)[8]) {
@@ -69,6 +69,40 @@ struct Turn {
         if (second) u1 = pack8<BF16>(y[1]);
     }
 };
+
+// Where a head's halves of less than all of it are turned, either of a lane's accesses shares its lines with the other.  This deals the 8 lanes' channels of ROWS rows
+// anew, 8 part and 64 + 8 part on, so that a row is two whole lines: of the 16 pieces of 8 channels lane p has p and p + e where it turns them (p < e = d / 16),
+// else p + e and p + 8.
+template <int E>
+__device__ __forceinline__ void deal_piece(uint32_t& u0, uint32_t& u1, int part) {
+    const uint32_t gone = part < E ? u1 : u0;
+    const uint32_t lower = __builtin_amdgcn_update_dpp(0, gone, 0x110 + E, 0xF, 0xF, false);       // of lane - E, in a row of 16
+    const uint32_t upper = __builtin_amdgcn_update_dpp(0, gone, 0x100 + 8 - E, 0xF, 0xF, false);   // of lane + 8 - E
+    if (part < E) u1 = upper;
+    else u0 = lower;
+}
+template <int E, int ROWS>
+__device__ __forceinline__ void deal_rows(uint4 (&u)[ROWS][2], int part) {
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        deal_piece<E>(u[i][0].x, u[i][1].x, part);
+        deal_piece<E>(u[i][0].y, u[i][1].y, part);
+        deal_piece<E>(u[i][0].z, u[i][1].z, part);
+        deal_piece<E>(u[i][0].w, u[i][1].w, part);
+    }
+}
+template <int ROWS>
+__device__ __forceinline__ void deal_lines(uint4 (&u)[ROWS][2], int part, int d) {
+    switch (d / 16) {
+        case 1: return deal_rows<1>(u, part);
+        case 2: return deal_rows<2>(u, part);
+        case 3: return deal_rows<3>(u, part);
+        case 4: return deal_rows<4>(u, part);
+        case 5: return deal_rows<5>(u, part);
+        case 6: return deal_rows<6>(u, part);
+        case 7: return deal_rows<7>(u, part);
+    }
+}
 
 inline bool in_place_or_apart(const specache_view& in, const specache_view& out) { return in.data != out.data || same_view(in, out); }
 
