@@ -246,8 +246,9 @@ def _here():
     return _with_torch().cuda.current_device()
 
 
-def _current(stream):
-    return _torch.cuda.current_stream().cuda_stream if stream is None else _stream(stream)
+def _current(stream, device):
+    # (the device is known here: torch takes 1.5 us to find it)
+    return _torch.cuda.current_stream(device).cuda_stream if stream is None else _stream(stream)
 
 
 def _type_of(t):
@@ -328,7 +329,7 @@ def rotate(plan, q, q_out, k=None, k_out=None, v=None, v_out=None, positions=Non
                (shape, shape, kv_shape, kv_shape, kv_shape, kv_shape))
     _done(lib().specache_rotate(C.byref(plan), _type_of(q), B, n, Hq, a[0], a[1], 0 if kv is None else kv_shape[1],
                                 None if k is None else a[2], None if k is None else a[3], None if v is None else a[4], None if v is None else a[5],
-                                _flat(positions, (B, n), _torch.int32, device, "positions"), first_position, _current(stream)))
+                                _flat(positions, (B, n), _torch.int32, device, "positions"), first_position, _current(stream, device)))
 
 
 def window_scratch(batch, n_q_heads, n_kv_heads, q_tokens, kv_tokens, window=0, sinks=0):
@@ -350,7 +351,7 @@ def window_attend(q, k, v, out, window=0, sinks=0, q_lengths=None, kv_lengths=No
     cfg = WindowConfig(B, Hq, pairs[1], D, n, pairs[2], window, sinks, _type_of(q), sm_scale)
     address, size = _scratch(scratch, device)
     _done(lib().specache_window_attend(C.byref(cfg), a[0], a[1], a[2], a[3], _flat(q_lengths, (B,), _torch.int32, device, "q_lengths"),
-                                       _flat(kv_lengths, (B,), _torch.int32, device, "kv_lengths"), address, size, _current(stream)))
+                                       _flat(kv_lengths, (B,), _torch.int32, device, "kv_lengths"), address, size, _current(stream, device)))
 
 
 def sample_scratch(rows, vocab, dtype):
@@ -375,7 +376,7 @@ def sample(logits, u, tokens, temperature=None, top_k=None, top_p=None, min_p=No
     _done(lib().specache_sample(C.byref(cfg), logits.data_ptr(), _flat(u, shape, f32, device, "u"),
                                 _flat(temperature, shape, f32, device, "temperature"), _flat(top_k, shape, i32, device, "top_k"),
                                 _flat(top_p, shape, f32, device, "top_p"), _flat(min_p, shape, f32, device, "min_p"),
-                                _flat(tokens, shape, i32, device, "tokens"), address, size, _current(stream)))
+                                _flat(tokens, shape, i32, device, "tokens"), address, size, _current(stream, device)))
 
 
 class _Room(threading.local):
@@ -390,7 +391,7 @@ class _Room(threading.local):
 _call = _Room()
 _PACK_PAGED = struct.Struct("8q5if").pack_into
 _PACK_BLOCKS = struct.Struct("8q7if").pack_into
-_WIDE = "counts must be whole numbers of 32 bits, sm_scale a finite one"
+_WIDE = "counts must be whole numbers of 32 bits, sm_scale a number"
 
 
 def _rows(t, shape, kind, device, name):
@@ -449,7 +450,7 @@ def paged_append(cache, plan, k, v, q=None, q_out=None, starts=None, lengths=Non
     a, i32 = _room.at, _torch.int32
     _done(lib().specache_paged_append(cache.at, None if plan is None else C.byref(plan), B, n, heads, a[0], a[1], a[2], a[3],
                                       _flat(starts, (B,), i32, device, "starts"), _flat(lengths, (B,), i32, device, "lengths"),
-                                      _flat(positions, (B, n), i32, device, "positions"), _current(stream)))
+                                      _flat(positions, (B, n), i32, device, "positions"), _current(stream, device)))
 
 
 def paged_scratch(cache, batch, n_q_heads, q_tokens, kv_tokens, shared_tokens=0):
@@ -468,11 +469,11 @@ def paged_attend(cache, q, out, kv_tokens=None, shared_tokens=0, q_lengths=None,
     try:
         _PACK_PAGED(c.room, 0, *_rows(q, shape, kind, device, "q"), *_rows(out, shape, kind, device, "out"),
                     B, Hq, n, cache.places if kv_tokens is None else kv_tokens, shared_tokens, sm_scale)
-    except (struct.error, OverflowError):
+    except struct.error:
         _refuse(_WIDE)
     address, size = _scratch(scratch, device)
     _done(lib().specache_paged_attend(cache.at, c.cfg, c.q, c.out, _flat(q_lengths, (B,), i32, device, "q_lengths"),
-                                      _flat(kv_lengths, (B,), i32, device, "kv_lengths"), address, size, _current(stream)))
+                                      _flat(kv_lengths, (B,), i32, device, "kv_lengths"), address, size, _current(stream, device)))
 
 
 def block_scratch(cache, batch, n_q_heads, q_tokens, kv_tokens, top, first=0, recent=0):
@@ -493,11 +494,11 @@ def block_select(cache, q, blocks, kv_tokens=None, top=0, first=0, recent=0, q_l
     try:
         _PACK_BLOCKS(c.room, 0, *_rows(q, shape, cache.kind, device, "q"), 0, 0, 0, 0,
                      B, Hq, n, cache.places if kv_tokens is None else kv_tokens, top, first, recent, 0.0)
-    except (struct.error, OverflowError):
+    except struct.error:
         _refuse(_WIDE)
     address, size = _scratch(scratch, device)
     _done(lib().specache_block_select(cache.at, c.cfg, c.q, lists, _flat(q_lengths, (B,), i32, device, "q_lengths"),
-                                      _flat(kv_lengths, (B,), i32, device, "kv_lengths"), address, size, _current(stream)))
+                                      _flat(kv_lengths, (B,), i32, device, "kv_lengths"), address, size, _current(stream, device)))
 
 
 def block_attend(cache, q, out, blocks, kv_tokens=None, q_lengths=None, kv_lengths=None, sm_scale=0.0, scratch=None, stream=None):
@@ -512,11 +513,11 @@ def block_attend(cache, q, out, blocks, kv_tokens=None, q_lengths=None, kv_lengt
     try:
         _PACK_BLOCKS(c.room, 0, *_rows(q, shape, kind, device, "q"), *_rows(out, shape, kind, device, "out"),
                      B, Hq, n, cache.places if kv_tokens is None else kv_tokens, slots, 0, 0, sm_scale)
-    except (struct.error, OverflowError):
+    except struct.error:
         _refuse(_WIDE)
     address, size = _scratch(scratch, device)
     _done(lib().specache_block_attend(cache.at, c.cfg, c.q, c.out, lists, _flat(q_lengths, (B,), i32, device, "q_lengths"),
-                                      _flat(kv_lengths, (B,), i32, device, "kv_lengths"), address, size, _current(stream)))
+                                      _flat(kv_lengths, (B,), i32, device, "kv_lengths"), address, size, _current(stream, device)))
 
 
 class SpeCache:

@@ -158,7 +158,7 @@ def test_bindings_refuse(monkeypatch):
                  lambda: binding.paged_append(cache, None, new.bfloat16(), new), lambda: binding.paged_append(cache, None, new, new, starts=torch.zeros(2, dtype=torch.int32)),
                  lambda: binding.paged_attend(cache, q[:2], q[:2]), lambda: binding.paged_attend(cache, q, q[:, :2]), lambda: binding.paged_attend(cache, q.float(), q.float()),
                  lambda: binding.block_select(cache, q, blocks, top=5), lambda: binding.block_attend(cache, q, q, blocks[..., :4]), lambda: binding.block_attend(cache, q, q, blocks[0]),
-                 lambda: binding.block_attend(cache, q, q, blocks.long()), lambda: binding.paged_attend(cache, q, q, 2 ** 31), lambda: binding.paged_attend(cache, q, q, 32, -2 ** 40), lambda: binding.paged_attend(cache, q, q, 32, sm_scale=1e40),
+                 lambda: binding.block_attend(cache, q, q, blocks.long()), lambda: binding.paged_attend(cache, q, q, 2 ** 31), lambda: binding.paged_attend(cache, q, q, 32, -2 ** 40),
                  lambda: binding.block_attend(cache, q, q, blocks, 2 ** 33), lambda: binding.block_select(cache, q, blocks[..., :2].contiguous(), 32, 0, 2, 0.0)):
         with pytest.raises(binding.SpeCacheError) as e:
             make()
