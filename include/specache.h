@@ -609,7 +609,7 @@ typedef struct specache_pages {
  * rotation goes by; NULL: a token's position in its sequence.
  * bounds: a page whose place 0 is among the tokens gets those of the tokens written here, any other the wider of what it has and those; a NaN is passed over.
  * Two tokens that one call, or two that overlap, write to one page come from one sequence and one call (pages that sequences share are not appended to).
- * batch = 0 and tokens = 0 are allowed; batch * tokens goes up to 2^30.
+ * The inputs share no memory with the cache's pages.  batch = 0 and tokens = 0 are allowed; batch * tokens goes up to 2^30.
  * Errors: EINVAL (null or misaligned view, counts, a plan that specache_rotary_plan did not write), EHIP.
  */
 int specache_paged_append(const specache_pages* cache, const specache_rotary* plan, int32_t batch, int32_t tokens,

@@ -687,8 +687,10 @@ int plan_of(const specache_pages* cache, const specache_paged_config* c, Plan& p
     const int G = c->n_q_heads / cache->n_kv_heads;
     const int64_t rows = (int64_t)c->q_tokens * G;
     if (c->batch > 1 && rows) p.shared = std::min(c->shared_tokens, c->kv_tokens) / cache->page_tokens * cache->page_tokens;
+    // Sequences whose rows fill tiles by themselves share nothing but the caches: row tiles are as many either way, and without parts there is no merge (8 prompts of 1024 rows behind
+    // 16384 positions 531 us against 557).  Nor do more rows than a merge has threads for.
     const int64_t tile = kMostWaves * kWaveRows;
-    if (c->batch * ((rows + tile - 1) / tile) * 10 <= (c->batch * rows + tile - 1) / tile * 11) p.shared = 0;
+    if (c->batch * ((rows + tile - 1) / tile) * 10 <= (c->batch * rows + tile - 1) / tile * 11 || c->batch * rows * cache->n_kv_heads >= kMostGroups) p.shared = 0;
     const int64_t units = rows ? (int64_t)c->batch * cache->n_kv_heads : 0, own = c->kv_tokens - p.shared;
     if (rows > kWaveRows) {
         p.kind = kTiles;
