@@ -8,6 +8,7 @@
 // rows as a workgroup holds.  Its partial results, and those of the sequences' own positions, are joined by merge_kernel.
 #include "pages.h"
 #include "rows16.h"
+#include "wave_ops.h"
 
 #include <algorithm>
 #include <cmath>
@@ -291,6 +292,31 @@ struct PagedRows : Rows<BF16, BLOCKS> {
             }
         }
     }
+    // A wave's sums to their places by way of its kSumsBytes of LDS, so that a row's lines are written whole.  us, straight / by way of LDS: a prefix of 3234 positions
+    // for 32 sequences of 27 tokens and 8 heads 61.8 / 58.4, 6517 for 64 of 2 and 32 heads 44.5 / 43.6.  (Results in 16 bits gain nothing from it: 17.1 / 18.9 for 5 sequences
+    // of 169 tokens and 64 heads, and go straight.)  place(row) is where a row goes.
+    template <typename Place>
+    __device__ __forceinline__ void store_sums(char* room, int rows, Place&& place) {
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {               // 64 channels at a time (a row's turned by 4 per row: no two rows of a group of lanes meet in a bank)
+            wait_reads();
+#pragma unroll
+            for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float16v& o = Base::o[2 * part + dt];
+                    *(float4*)(room + (Base::lane % 32 * 64 + (32 * dt + 8 * i + 4 * Base::half + 4 * Base::lane) % 64) * 4) = float4{o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]};
+                }
+            wave_sync();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int r = 4 * i + Base::lane / 16, c = Base::lane % 16 * 4;
+                const float4 x = *(const float4*)(room + (r * 64 + (c + 4 * r) % 64) * 4);
+                if (r < rows) *(float4*)(place(r) + 64 * part + c) = x;
+            }
+            wave_sync();
+        }
+    }
     // the two halves' sums and what they saw, together
     __device__ __forceinline__ void finish() {
         Base::l += other_half(Base::l);
@@ -306,6 +332,7 @@ __device__ __forceinline__ int least_of_wave(int v) {
 }
 
 constexpr int kTileBytes = 64 * kRowBytes16;   // of keys, or of values
+constexpr int kSumsBytes = 32 * 64 * 4;         // of a wave's sums, 64 channels at a time
 constexpr int kWaveBytes = kTileBytes;         // of a wave by itself: 32 positions, keys and values, or the sums of 32 rows
 
 __device__ __forceinline__ uint32_t lds_address(const char* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }
@@ -318,6 +345,7 @@ __device__ __forceinline__ const uint16_t* query_of(const PagedArgs& a, const Ro
 // Rows of more than a wave: the waves of a workgroup have rows of their own and share tiles of 64 positions, which travel to LDS while the one before is worked on.
 template <bool BF16, int WAVES>
 __device__ __forceinline__ void tile_job(const PagedArgs& a, bool prefix, char* lds, int* least, int* any_dropped) {
+    static_assert(WAVES * kSumsBytes <= 4 * kTileBytes, "every wave has a part of the buffers for its sums");
     constexpr int TILE = 64, ROWS = WAVES * kWaveRows, LOADS = 16 / WAVES, PARTS = 4 / LOADS;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     Job j;
@@ -412,16 +440,20 @@ __device__ __forceinline__ void tile_job(const PagedArgs& a, bool prefix, char* 
     __syncthreads();
     if (*any_dropped) rs.give_odd_values(directory, fetch_values, n, j.end);
     rs.finish();
-    if (i_row >= j.rows) return;
-    if (prefix || a.parts) rs.store_part(prefix ? a.prefix_o : a.own_o, prefix ? a.prefix_ml : a.own_ml, j.place + i_row, n > 0);
-    else {
+    if (prefix || a.parts) {
+        __syncthreads();                   // (the buffers have been read)
+        const int rows = min(kWaveRows, j.rows - wave * kWaveRows);
+        if (rows <= 0) return;
+        const int64_t place = j.place + wave * kWaveRows;
+        if (lane < rows) *(float2*)((prefix ? a.prefix_ml : a.own_ml) + 2 * (place + lane)) = float2{rs.m, rs.l};
+        float* const sums = (prefix ? a.prefix_o : a.own_o) + place * kD;
+        if (n > 0) rs.store_sums(lds + wave * kSumsBytes, rows, [&](int r) { return sums + r * kD; });
+    } else if (i_row < j.rows) {
         rs.seen.last = rs.m != -INFINITY ? 0 : -1;   // (whether the row saw anything)
         rs.store((uint16_t*)a.out.data + row.b * a.out.batch + row.head * a.out.head + row.token * a.out.token);
     }
 }
 
-// Waves by themselves: up to 32 rows, 32 positions at a time; as soon as a tile's keys have been read the next ones travel to their place, and so do the values.
-// The waves of a workgroup take a chunk's tiles in turn and join their results in LDS at its end.
 template <bool BF16, bool LISTED, int WAVES>
 __device__ __forceinline__ void step_job(const PagedArgs& a, bool prefix, char* lds, float2 (*joined)[kWaveRows]) {
     constexpr int TILE = 32, HALF = TILE / 2 * kRowBytes16, OWN = kWaveBytes;
@@ -537,8 +569,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_kernel(PagedArgs a) {
         };
     } more;
     const bool prefix = !LISTED && (int)blockIdx.x < a.prefix_groups;
-    if (KIND == kTiles || (KIND == kTilesAndSteps && prefix)) tile_job<BF16, WAVES>(a, prefix, lds, more.least, &more.any_dropped);
-    else if constexpr (KIND != kTiles) step_job<BF16, LISTED, WAVES>(a, prefix, lds, more.joined);
+    if constexpr (KIND != kSteps) {
+        if (KIND == kTiles || prefix) return tile_job<BF16, WAVES>(a, prefix, lds, more.least, &more.any_dropped);
+    }
+    if constexpr (KIND != kTiles) step_job<BF16, LISTED, WAVES>(a, prefix, lds, more.joined);
 }
 
 // The partial results of a row, joined: those of the prefix, then those of its own positions; two channels per lane, the parts dealt to the waves of a
@@ -623,7 +657,6 @@ struct Part {
     int64_t groups() const { return items * chunks; }
     int64_t places() const { return items * chunks * item_rows; }
 };
-constexpr int kMostWaves = 8;
 struct Plan {
     Part prefix, own;
     int shared = 0, kind = kSteps, waves = 4;
@@ -646,7 +679,7 @@ Part steps_of(int64_t units, int64_t rows, int64_t most, int waves, bool joined)
     p.item_rows = (int)std::min<int64_t>(std::max<int64_t>(rows, 1), kWaveRows);
     p.row_tiles = (int)((rows + kWaveRows - 1) / kWaveRows);
     p.items = units * p.row_tiles;
-    const int64_t tiles = (most + 31) / 32, at_once = waves == 8 ? 256 : 512;
+    const int64_t tiles = (most + 31) / 32, at_once = 2048 / waves;
     int64_t chunks = 1;
     if (p.items && tiles > (joined ? 4 : 6) * waves) {
         chunks = std::max(at_once / p.items, tiles / 64);
@@ -655,10 +688,59 @@ Part steps_of(int64_t units, int64_t rows, int64_t most, int waves, bool joined)
     p.chunks = (int)std::max<int64_t>(chunks, 1);
     return p;
 }
-// Waves of a workgroup of steps: 8 where the rows' workgroups can have a compute unit each.  us, 4 / 8: 64 rows of 19 tiles 11.0 / 9.8, 32 heads of 4 over 5000 positions
-// 13.0 / 11.7, 16 ragged sequences of 8 heads up to 32768 220 / 213; but what is joined with a prefix is better off with more workgroups (three sequences of 32 heads behind 1000
-// shared positions 12.5 / 14.0).
-int step_waves(int64_t units, int64_t rows) { return units * ((rows + kWaveRows - 1) / kWaveRows) <= 256 ? 8 : 4; }
+// Waves of a workgroup of steps: 2048 waves are what the chip holds, 10 tiles what one has at most where that can be (256 tokens of 8 heads over 19 blocks of 64, 2 waves / 4: 113 / 108).  us, 4 / 8: 64 rows of 19 tiles 11.0 / 9.8, 32 heads of 4
+// over 5000 positions 13.0 / 11.7, 16 ragged sequences of 8 heads up to 32768 220 / 213; 4 / 1: 64 sequences of 32 heads up to 2 positions 22.3 / 8.8, 32 of 20 tokens and
+// 32 heads 15.6 / 10.5
+int step_waves(int64_t units, int64_t rows, int64_t most) {
+    const int64_t items = units * ((rows + kWaveRows - 1) / kWaveRows), tiles = (most + 31) / 32;
+    int waves = 1;
+    while (waves < 8 && waves < tiles && (items * waves < 2048 || tiles > 10 * waves)) waves *= 2;
+    return waves;
+}
+
+// Attention of `batch` sequences of `rows` rows to a KV head over `most` positions, of which `shared` are worked on for all of them together.
+struct Work {
+    int64_t heads, batch, rows, shared, most;
+    // lays it out, and says about how many us it takes
+    double plan(Plan& p) const {
+        const int64_t units = rows ? batch * heads : 0, own = most - shared;
+        p.shared = (int)shared;
+        p.prefix = Part();
+        if (rows > kWaveRows) {
+            p.kind = kTiles;
+            p.waves = std::max(shared, own) >= 2048 && rows > 128 ? 8 : 4;
+            const int64_t at_once = p.waves == 8 ? 256 : 512;
+            if (shared) p.prefix = tiles_of(heads, batch * rows, shared, p.waves, at_once);
+            p.own = tiles_of(units, rows, own, p.waves, at_once);
+        } else if (shared && batch * rows > kWaveRows) {
+            p.kind = kTilesAndSteps;
+            p.waves = 4;
+            // Two workgroups of the prefix to a compute unit where it is most of the work and their chunks stay long, one beside the sequences' own else.  us, 1 / 2: 31583
+            // positions for 64 sequences of 3 tokens and 32 heads 183 / 151, but 6517 for 64 of 2 44 / 47, 15597 for 32 of 2 and 16 heads 30 / 33,
+            // and 46783 for 32 of 2 and 64 heads that have 4675 of their own each 234 / 256
+            p.prefix = tiles_of(heads, batch * rows, shared, 4, 512);
+            if (shared < 2048 * (int64_t)p.prefix.chunks || tile_us(heads, batch * rows, shared, 4) < 2 * step_us(units, own, kOnceRate))
+                p.prefix = tiles_of(heads, batch * rows, shared, 4, 256);
+            p.own = steps_of(units, rows, own, 4, true);
+        } else {
+            p.kind = kSteps;
+            p.waves = shared ? 4 : step_waves(units, rows, most);   // (joined, us of 4 / 8: 12220 shared by 32 sequences of 32 heads 58.7 / 66.8, 501 21.8 / 30.5)
+            if (shared) p.prefix = steps_of(heads, batch * rows, shared, p.waves, true);
+            p.own = steps_of(units, rows, own, p.waves, shared != 0);
+        }
+        const bool parts = shared || p.own.chunks > 1;
+        double us = rows > kWaveRows ? tile_us(units, rows, own, p.waves) : step_us(units, own, kAgainRate);
+        if (shared) us += kJoinUs + (p.kind == kSteps ? step_us(heads, shared, kOnceRate) : tile_us(heads, batch * rows, shared, p.waves));
+        return us + (parts ? 2 * 520 * (double)(p.prefix.places() + p.own.places()) / 3e6 : 0.0);
+    }
+    // bytes per us: of positions that one sequence reads after another (largely from the caches), and of those read once; us that a prefix by itself costs beside its work
+    static constexpr double kAgainRate = 12e6, kOnceRate = 6e6, kJoinUs = 8;
+    static double tile_us(int64_t units, int64_t rows, int64_t most, int waves) {   // (whole items of rows, at 0.9 PFLOP/s)
+        const int64_t item = waves * kWaveRows;
+        return (double)units * ((rows + item - 1) / item * item) * most * 4 * kD / 0.9e9;
+    }
+    static double step_us(int64_t units, int64_t most, double rate) { return (double)units * ((most + 31) / 32) * 2 * 32 * kRowBytes16 / rate; }
+};
 
 int finish_plan(Plan& p, int64_t merge_rows) {
     if (!p.shared && merge_rows >= kMostGroups) p.own.chunks = 1;
@@ -686,26 +768,17 @@ int plan_of(const specache_pages* cache, const specache_paged_config* c, Plan& p
     if (c->shared_tokens < 0) return fail_without_context(SPECACHE_EINVAL, "shared_tokens must not be negative");
     const int G = c->n_q_heads / cache->n_kv_heads;
     const int64_t rows = (int64_t)c->q_tokens * G;
-    if (c->batch > 1 && rows) p.shared = std::min(c->shared_tokens, c->kv_tokens) / cache->page_tokens * cache->page_tokens;
-    // Sequences whose rows fill tiles by themselves share nothing but the caches: row tiles are as many either way, and without parts there is no merge (8 prompts of 1024 rows behind
-    // 16384 positions 531 us against 557).  Nor do more rows than a merge has threads for.
-    const int64_t tile = kMostWaves * kWaveRows;
-    if (c->batch * ((rows + tile - 1) / tile) * 10 <= (c->batch * rows + tile - 1) / tile * 11 || c->batch * rows * cache->n_kv_heads >= kMostGroups) p.shared = 0;
-    const int64_t units = rows ? (int64_t)c->batch * cache->n_kv_heads : 0, own = c->kv_tokens - p.shared;
-    if (rows > kWaveRows) {
-        p.kind = kTiles;
-        p.waves = std::max<int64_t>(p.shared, own) >= 2048 && rows > 128 ? 8 : 4;
-        const int64_t at_once = p.waves == 8 ? 256 : 512;
-        if (p.shared) p.prefix = tiles_of(cache->n_kv_heads, c->batch * rows, p.shared, p.waves, at_once);
-        p.own = tiles_of(units, rows, own, p.waves, at_once);
-    } else if (p.shared && c->batch * rows > kWaveRows) {
-        p.kind = kTilesAndSteps;
-        p.prefix = tiles_of(cache->n_kv_heads, c->batch * rows, p.shared, p.waves, 256);
-        p.own = steps_of(units, rows, own, p.waves, true);
-    } else {
-        p.waves = p.shared ? 4 : step_waves(units, rows);
-        if (p.shared) p.prefix = steps_of(cache->n_kv_heads, c->batch * rows, p.shared, p.waves, true);
-        p.own = steps_of(units, rows, own, p.waves, p.shared != 0);
+    const int64_t units = rows ? (int64_t)c->batch * cache->n_kv_heads : 0;
+    // Shared where that takes less time by the estimate.  us, shared / not: 16 sequences of 69 tokens behind 323 positions 33 / 19, 3 steps behind 13424 25 / 20, 64 of one head
+    // behind 13559 with 116 tokens 517 / 453; 32 steps of 32 heads behind 12220 59 / 880, 64 of 3 tokens behind 31583 151 / 580.  Over 110 drawn calls 26.6 (all that can be
+    // shared) / 23.7 (geometric means, the choice of waves included); near the border it is off by up to a tenth (one KV head behind 9313 for 32 of 2 23.3 / 25.7).
+    Work alone{cache->n_kv_heads, c->batch, rows, 0, c->kv_tokens};
+    const double us = alone.plan(p);
+    if (c->batch > 1 && units && units * rows < kMostGroups) {
+        Work joined = alone;
+        joined.shared = std::min(c->shared_tokens, c->kv_tokens) / cache->page_tokens * cache->page_tokens;
+        Plan q;
+        if (joined.shared && joined.plan(q) < us) p = q;
     }
     return finish_plan(p, c->batch * rows * cache->n_kv_heads);
 }
@@ -729,7 +802,7 @@ int plan_of_blocks(const specache_pages* cache, const specache_block_config* c, 
     const int64_t slots = (int64_t)c->top + c->first + c->recent, blocks = (c->kv_tokens + cache->page_tokens - 1) / cache->page_tokens;
     const int64_t units = (int64_t)c->batch * c->q_tokens * cache->n_kv_heads;
     const int G = c->n_q_heads / cache->n_kv_heads;
-    p.waves = step_waves(units, G);
+    p.waves = step_waves(units, G, std::min(slots, blocks) * cache->page_tokens);
     p.own = steps_of(units, G, std::min(slots, blocks) * cache->page_tokens, p.waves, false);
     return finish_plan(p, units * G);
 }
@@ -786,7 +859,9 @@ void launch_merge(const Plan& p, const PagedArgs& a, hipStream_t stream) {
 template <bool BF16, bool LISTED>
 void launch(const Plan& p, const PagedArgs& a, hipStream_t stream) {
     const dim3 grid((unsigned)(p.prefix.groups() + p.own.groups()));
-    const auto kernel = LISTED || p.kind == kSteps ? (p.waves == 8 ? paged_kernel<BF16, LISTED, kSteps, 8> : paged_kernel<BF16, LISTED, kSteps, 4>)
+    const auto steps = p.waves == 8 ? paged_kernel<BF16, LISTED, kSteps, 8> : p.waves == 4 ? paged_kernel<BF16, LISTED, kSteps, 4>
+                       : p.waves == 2 ? paged_kernel<BF16, LISTED, kSteps, 2> : paged_kernel<BF16, LISTED, kSteps, 1>;
+    const auto kernel = LISTED || p.kind == kSteps ? steps
                         : p.kind == kTilesAndSteps ? paged_kernel<BF16, false, kTilesAndSteps, 4>
                         : p.waves == 8             ? paged_kernel<BF16, false, kTiles, 8>
                                                    : paged_kernel<BF16, false, kTiles, 4>;

@@ -94,12 +94,12 @@ def test_attend_refuses():
 
 def test_attend_wants_its_scratch_memory():
     size = C.c_int64()
-    for cache, cfg in ((_pages(table_pages=10000), _paged(kv_tokens=100000)), (_pages(), _paged(shared_tokens=32))):
+    for cache, cfg in ((_pages(table_pages=10000), _paged(kv_tokens=100000)), (_pages(n_kv_heads=4, table_pages=2000), _paged(batch=32, kv_tokens=20000, shared_tokens=16384))):
         assert binding.lib().specache_paged_scratch(_ref(cache), _ref(cfg), C.byref(size)) == binding.OK and size.value > 0
         assert _attend(cache, cfg) == _attend(cache, cfg, scratch=A + 8, size=size.value) == binding.EINVAL
         assert _attend(cache, cfg, scratch=A, size=size.value - 1) == binding.ECAPACITY
-    # what is shared counts in whole pages, and for more than one sequence
-    for cfg in (_paged(), _paged(shared_tokens=15), _paged(batch=1, shared_tokens=160)):
+    # what is shared counts in whole pages, for more than one sequence, and where it pays
+    for cfg in (_paged(), _paged(shared_tokens=15), _paged(shared_tokens=32), _paged(batch=1, shared_tokens=160)):
         assert binding.lib().specache_paged_scratch(_ref(_pages()), _ref(cfg), C.byref(size)) == binding.OK and size.value == 0
 
 
