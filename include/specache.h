@@ -620,7 +620,7 @@ int specache_paged_append(const specache_pages* cache, const specache_rotary* pl
 /*
  * Attention over a paged cache: of a sequence with n queries and N cached tokens, query row i stands at position p = N - n + i and sees the
  * positions j <= p that have a page.  A row that sees nothing gives zeros.
- * shared_tokens: the table's rows agree over the first shared_tokens / page_tokens pages (those of row 0 are read).  Their keys and values are then read
+ * shared_tokens: the table's rows agree over the first shared_tokens / page_tokens pages (those of row 0 may be read for all).  Their keys and values are then read
  * once for all sequences where the counts promise that this takes less time; it changes the time and the rounding alone.  0: nothing is shared.
  */
 typedef struct specache_paged_config {
