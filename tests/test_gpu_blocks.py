@@ -267,3 +267,19 @@ def test_captured_overlapping_and_the_same_every_time(B, Hq, Hkv, n, N, page, to
         torch.cuda.synchronize()
         for s, (blocks, out) in zip(sets, want):
             assert torch.equal(s["blocks"], blocks) and torch.equal(s["out"], out)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("B,Hq,Hkv,n,N_of,page,top,first,recent", [
+    # units for one, two and four waves to a workgroup; few chunks, which one wave joins
+    (2, 16, 8, 150, [700, 333], 32, 3, 1, 1), (2, 16, 8, 80, [700, 333], 32, 3, 1, 1), (2, 8, 4, 100, [900, 640], 32, 20, 1, 1), (16, 16, 8, 1, [2600 - 17 * i for i in range(16)], 64, 32, 1, 2)])
+def test_waves_and_chunks(B, Hq, Hkv, n, N_of, page, top, first, recent, dtype):
+    q, k, v, bounds, table = _make(n, B, Hq, Hkv, n, N_of, page, dtype)
+    cache = binding.Pages(k, v, table, bounds)
+    blocks = select(cache, q, max(N_of), top, first, recent, None, N_of)
+    out = attend(cache, q, blocks, max(N_of), None, N_of)
+    for i in sorted({0, n // 2, n - 1}):               # (a row's list is its own)
+        one = blocks[:, :, i:i + 1]
+        N_then = [N - n + 1 + i for N in N_of]
+        exact, tol = reference(q[:, :, i:i + 1], k, v, table, [1] * B, N_then, SCALE, _seen(one, page, N_then))
+        compare(out[:, :, i:i + 1], exact, tol, [1] * B)

@@ -196,3 +196,21 @@ def test_captured_while_positions_move():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(x, y) and all(torch.equal(a, b) for a, b in zip(mine, want))
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("with_bounds", [False, True])
+@pytest.mark.parametrize("layout,d", [(0, 128), (0, 96), (1, 128), (1, 64)])
+def test_more_than_the_caches_hold(layout, d, with_bounds, dtype):
+    """Prompts whose stores go past the caches (from 32 MiB on), ragged, from inside a page on."""
+    plan = binding.rotary_plan(d, 1.0e4, layout)
+    starts, lengths = [37, 300], [6000, 5555]
+    case = _case(d + layout, 2, 6000, 8, 2, 128, dtype, "places" if layout else "heads", starts, lengths)
+    _check(case, plan, starts, lengths, with_bounds=with_bounds, f=_frequencies(d, 1.0e4, 0, 1.0, 0, 0, 0))
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("layout,d", [(0, 128), (0, 96), (1, 128)])
+def test_small_calls_without_bounds(layout, d, dtype):
+    case = _case(d, 3, 9, 4, 2, 16, dtype, "heads", [3, 15, 16])
+    _check(case, binding.rotary_plan(d, 1.0e4, layout), [3, 15, 16], with_bounds=False, f=_frequencies(d, 1.0e4, 0, 1.0, 0, 0, 0))

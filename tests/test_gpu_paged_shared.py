@@ -92,3 +92,15 @@ def test_captured_and_the_same_every_time(kind):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("kind", FEW)
+def test_nothing_but_what_is_shared(kind):
+    """The longest sequence ends where the shared pages do (their queries then see less of them than all), and the others before."""
+    B, Hq, Hkv, n, most, page, shared = KINDS[kind]
+    q, k, v, table, cache = _make(kind, 5, torch.bfloat16)
+    whole = shared // page * page
+    N_of = [whole - b for b in range(B)]
+    assert binding.paged_scratch(cache, B, Hq, n, whole, shared) != binding.paged_scratch(cache, B, Hq, n, whole, 0), "this size does not share"
+    exact, tol = reference(q, k, v, table, [n] * B, N_of, SCALE)
+    compare(attend(cache, q, whole, shared, None, N_of), exact, tol, [n] * B)
