@@ -688,9 +688,9 @@ Part steps_of(int64_t units, int64_t rows, int64_t most, int waves, bool joined)
     p.chunks = (int)std::max<int64_t>(chunks, 1);
     return p;
 }
-// Waves of a workgroup of steps: 2048 waves are what the chip holds, 10 tiles what one has at most where that can be.  us, 2 / 4: 256 tokens of
-// 8 heads over 19 blocks of 64 113 / 108; 4 / 8: 64 rows of 19 tiles 11.0 / 9.8, 32 heads of 4 over 5000 positions 13.0 / 11.7, 16 ragged sequences of 8 heads up to 32768 220 / 213; 4 / 1: 64 sequences of 32 heads up to 2 positions 22.3 / 8.8, 32 of 20 tokens and
-// 32 heads 15.6 / 10.5
+// Waves of a workgroup of steps: 2048 waves are what the chip holds, 10 tiles what one has at most where that can be.  us, 2 / 4: 256 tokens of 8 heads over 19 blocks
+// of 64 113 / 108; 4 / 8: 64 rows of 19 tiles 11.0 / 9.8, 32 heads of 4 over 5000 positions 13.0 / 11.7, 16 ragged sequences of 8 heads up to 32768 220 / 213;
+// 4 / 1: 64 sequences of 32 heads up to 2 positions 22.3 / 8.8, 32 of 20 tokens and 32 heads 15.6 / 10.5
 int step_waves(int64_t units, int64_t rows, int64_t most) {
     const int64_t items = units * ((rows + kWaveRows - 1) / kWaveRows), tiles = (most + 31) / 32;
     int waves = 1;
