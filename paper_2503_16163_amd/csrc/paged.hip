@@ -124,7 +124,8 @@ __device__ __forceinline__ bool job_of(const PagedArgs& a, bool prefix, Job& j) 
         if (j.rows <= 0) return false;
         j.begin = LISTED ? 0 : a.shared;
         j.end = j.N;
-        if (LISTED) j.tiles = (int)((((int64_t)used << a.pages.log2) + TILE - 1) / TILE);
+        // (of a sequence without tokens no entry is a block, and there need not be a page whose memory a tile could be taken from)
+        if (LISTED) j.tiles = j.N > 0 ? (int)((((int64_t)used << a.pages.log2) + TILE - 1) / TILE) : 0;
         else j.tiles = max(0, (min(j.N, j.N - j.n + (j.row0 + j.rows - 1) / a.G + 1) - j.begin + TILE - 1) / TILE);
     }
     j.i_begin = (int)((int64_t)j.tiles * chunk / chunks);
