@@ -321,7 +321,8 @@ struct PagedRows : Rows<BF16, BLOCKS> {
     // the two halves' sums and what they saw, together
     __device__ __forceinline__ void finish() {
         Base::l += other_half(Base::l);
-        if (!saw && other_half(saw ? 1.0f : 0.0f) == 0.0f) Base::m = -INFINITY;
+        const float other = other_half(saw ? 1.0f : 0.0f);   // (by all lanes: a lane that saw nothing asks one that may have)
+        if (!saw && other == 0.0f) Base::m = -INFINITY;
     }
 };
 
