@@ -391,7 +391,10 @@ class _Room(threading.local):
 _call = _Room()
 _PACK_PAGED = struct.Struct("8q5if").pack_into
 _PACK_BLOCKS = struct.Struct("8q7if").pack_into
+_PACK_PAGED_COUNTS = struct.Struct("5if").pack_into
+_PACK_BLOCK_COUNTS = struct.Struct("7if").pack_into
 _WIDE = "counts must be whole numbers of 32 bits, sm_scale a number"
+_MOST = 2 ** 31 - 1    # (ctypes would cut a longer count off without a word)
 
 
 def _rows(t, shape, kind, device, name):
@@ -416,6 +419,8 @@ class Pages:
         views = _views(self.device, k.dtype, ("k", "v", "bounds"), (k, v, bounds), (k.shape, k.shape, (P, H, 2, 128)))
         if table.dim() != 2 or table.dtype is not _torch.int32 or table.get_device() != self.device or (table.shape[1] > 1 and table.stride(1) != 1):
             _refuse("table must be a [batch, pages] tensor of int32 on the current device, a row's entries side by side")
+        if max(P, H, T, table.shape[1]) > _MOST:
+            _refuse(_WIDE)
         self.batch, self.kv_heads, self.places = table.shape[0], H, table.shape[1] * T
         self.config = PagesConfig(*(View.from_address(at) for at in views[:3]), table.data_ptr(), table.stride(0) if table.shape[0] > 1 else table.shape[1],
                                   P, H, T, table.shape[1], 128, _type_of(k))
@@ -437,6 +442,8 @@ def paged_append(cache, plan, k, v, q=None, q_out=None, starts=None, lengths=Non
     device, H, kind = _here(), cache.kv_heads, cache.kind
     if device != cache.device or B != cache.batch:
         _refuse("the cache is not on the current device, or has other sequences")
+    if n > _MOST or B > _MOST or (q is not None and q.shape[1] > _MOST):
+        _refuse(_WIDE)
     if (q is None) != (q_out is None):
         _refuse("a tensor and its output are given or left out together")
     if q is None:
@@ -455,8 +462,12 @@ def paged_append(cache, plan, k, v, q=None, q_out=None, starts=None, lengths=Non
 
 def paged_scratch(cache, batch, n_q_heads, q_tokens, kv_tokens, shared_tokens=0):
     """Bytes of scratch memory that paged_attend needs for these counts (0: none)."""
-    out = C.c_int64()
-    _done(lib().specache_paged_scratch(cache.at, C.byref(PagedConfig(batch, n_q_heads, q_tokens, kv_tokens, shared_tokens)), C.byref(out)))
+    out, c = C.c_int64(), _call
+    try:
+        _PACK_PAGED_COUNTS(c.room, 64, batch, n_q_heads, q_tokens, kv_tokens, shared_tokens, 0.0)
+    except struct.error:
+        _refuse(_WIDE)
+    _done(lib().specache_paged_scratch(cache.at, c.cfg, C.byref(out)))
     return out.value
 
 
@@ -478,8 +489,12 @@ def paged_attend(cache, q, out, kv_tokens=None, shared_tokens=0, q_lengths=None,
 
 def block_scratch(cache, batch, n_q_heads, q_tokens, kv_tokens, top, first=0, recent=0):
     """Bytes of scratch memory that block_select and block_attend need for these counts (0: none)."""
-    out = C.c_int64()
-    _done(lib().specache_block_scratch(cache.at, C.byref(BlockConfig(batch, n_q_heads, q_tokens, kv_tokens, top, first, recent)), C.byref(out)))
+    out, c = C.c_int64(), _call
+    try:
+        _PACK_BLOCK_COUNTS(c.room, 64, batch, n_q_heads, q_tokens, kv_tokens, top, first, recent, 0.0)
+    except struct.error:
+        _refuse(_WIDE)
+    _done(lib().specache_block_scratch(cache.at, c.cfg, C.byref(out)))
     return out.value
 
 
