@@ -652,6 +652,7 @@ __global__ __launch_bounds__(64 * kMergeWaves) void paged_merge_kernel(PagedArgs
 }
 
 constexpr int64_t kMostGroups = INT32_MAX / 512;   // a launch's threads are counted in 32 bits
+constexpr int64_t kMostParts = (1 << 30) / (4 * (kD + 2));   // rows of partial results of split walks: of more there is enough to do without (less than kMostGroups / 2)
 // how a kind of work (the prefix's, the sequences' own) is laid out
 struct Part {
     int row_tiles = 1, item_rows = 1, chunks = 0;
@@ -685,7 +686,7 @@ Part steps_of(int64_t units, int64_t rows, int64_t most, int waves, bool joined)
     int64_t chunks = 1;
     if (p.items && tiles > (joined ? 4 : 6) * waves) {
         chunks = std::max(at_once / p.items, tiles / 64);
-        chunks = std::min({chunks, (tiles + waves - 1) / waves, std::max<int64_t>(256, tiles / 64)});
+        chunks = std::min({chunks, (tiles + waves - 1) / waves, std::max<int64_t>(256, tiles / 64), kMostParts / (p.items * p.item_rows)});
     }
     p.chunks = (int)std::max<int64_t>(chunks, 1);
     return p;
@@ -776,7 +777,7 @@ int plan_of(const specache_pages* cache, const specache_paged_config* c, Plan& p
     // shared) / 23.7 (geometric means, the choice of waves included); near the border it is off by up to a tenth (one KV head behind 9313 for 32 of 2 23.3 / 25.7).
     Work alone{cache->n_kv_heads, c->batch, rows, 0, c->kv_tokens};
     const double us = alone.plan(p);
-    if (c->batch > 1 && units && units * rows < kMostGroups) {
+    if (c->batch > 1 && units && units * rows < kMostGroups / 2) {   // (the prefix's workgroups and the others' are one launch)
         Work joined = alone;
         joined.shared = std::min(c->shared_tokens, c->kv_tokens) / cache->page_tokens * cache->page_tokens;
         Plan q;
