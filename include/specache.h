@@ -654,6 +654,7 @@ int specache_paged_attend(const specache_pages* cache, const specache_paged_conf
  * sum that is NaN counts as -infinity.
  * specache_block_attend: as specache_paged_attend, but a row sees the positions j <= p of its listed blocks alone.  An entry
  * that is negative or no block of the sequence's N tokens is passed over; one that is listed twice counts twice.
+ * The lists, batch * q_tokens * n_kv_heads, are up to 2^22 - 1.
  */
 typedef struct specache_block_config {
     int32_t batch, n_q_heads, q_tokens, kv_tokens;   /* as in specache_paged_config                */
@@ -663,7 +664,10 @@ typedef struct specache_block_config {
     float sm_scale;          /* specache_block_attend's; <= 0 selects 1/sqrt(head_dim)             */
 } specache_block_config;
 
-/* Host only: the bytes of scratch memory that either call needs (0: none).  Errors: EINVAL. */
+/*
+ * Host only: the bytes of scratch memory that either call needs (0: none).  The choice takes 12.25 for each block of a row, for as many rows as 256 MiB hold at a time (or the
+ * up to 16 tokens of a sequence whose heads make one matrix product, where those need more); partial results of split walks take up to 1 GiB.  Errors: EINVAL.
+ */
 int specache_block_scratch(const specache_pages* cache, const specache_block_config* cfg, int64_t* bytes);
 
 /*

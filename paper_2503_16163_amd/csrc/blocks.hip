@@ -28,9 +28,10 @@ struct BlockArgs {
     const int32_t* q_lengths;
     const int32_t* kv_lengths;
     int32_t* blocks;
-    float* scores;                    // [batch][KV head][token][row_blocks]
-    float* sizes;                     // [batch][KV head][token][row_blocks / 16]: the largest sum of magnitudes of 16 blocks
-    uint64_t* keys;                   // [batch][KV head][token][row_blocks]: where a row's scores are all made again
+    int unit0, row0;                  // a launch's first unit (what the workgroups of a token group make) and its first row [batch][KV head][token]
+    float* scores;                    // [row of the launch][row_blocks]
+    float* sizes;                     // [row of the launch][row_blocks / 16]: the largest sum of magnitudes of 16 blocks
+    uint64_t* keys;                   // [row of the launch][row_blocks]: where a row's scores are all made again
     int batch, G, q_tokens, kv_tokens, top, first, recent;
     int row_blocks;                   // whole tiles
     int tokens_here;                  // tokens whose heads make a product's rows
@@ -145,7 +146,7 @@ __device__ __forceinline__ void tile_scores(const BlockArgs& a, int b, int h, in
 template <bool BF16>
 __global__ __launch_bounds__(64 * kScoreWaves) void score_kernel(BlockArgs a) {
     __shared__ float2 room[kScoreWaves][kTile][kTile + 1];
-    const int wave = threadIdx.x / 64, split = blockIdx.x % a.splits, unit = blockIdx.x / a.splits;
+    const int wave = threadIdx.x / 64, split = blockIdx.x % a.splits, unit = a.unit0 + blockIdx.x / a.splits;
     const int token0 = unit % a.token_groups * a.tokens_here * a.passes, h = unit / a.token_groups % a.pages.n_kv_heads, b = unit / a.token_groups / a.pages.n_kv_heads;
     const int tile0 = split * kScoreWaves + wave;
     int page = page_of(a, b, tile0);                     // (on its way while the lengths are)
@@ -153,7 +154,7 @@ __global__ __launch_bounds__(64 * kScoreWaves) void score_kernel(BlockArgs a) {
     const int tokens = min(a.tokens_here * a.passes, n - token0), last = first_position + tokens - 1;
     if (tokens <= 0 || last < 0) return;
     const int tiles = (last >> a.pages.log2) / kTile + 1;
-    const int64_t row0 = ((int64_t)b * a.pages.n_kv_heads + h) * a.q_tokens + token0;
+    const int64_t row0 = ((int64_t)b * a.pages.n_kv_heads + h) * a.q_tokens + token0 - a.row0;
     for (int tile = tile0; tile < tiles; tile += a.splits * kScoreWaves) {
         const int here = page;
         page = page_of(a, b, tile + a.splits * kScoreWaves);
@@ -267,11 +268,11 @@ template <bool BF16, int THREADS, int KEEP>
 __global__ __launch_bounds__(THREADS) void select_kernel(BlockArgs a) {
     __shared__ Select<THREADS> s;
     const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-    const int token = blockIdx.x % a.q_tokens, h = blockIdx.x / a.q_tokens % a.pages.n_kv_heads, b = blockIdx.x / a.q_tokens / a.pages.n_kv_heads;
+    const int row = a.row0 + blockIdx.x, token = row % a.q_tokens, h = row / a.q_tokens % a.pages.n_kv_heads, b = row / a.q_tokens / a.pages.n_kv_heads;
     const int n = length_of(a.q_lengths, b, a.q_tokens), N = length_of(a.kv_lengths, b, a.kv_tokens);
     if (token >= n) return;
     const int slots = a.first + a.top + a.recent;
-    int32_t* list = a.blocks + (int64_t)blockIdx.x * slots;
+    int32_t* list = a.blocks + (int64_t)row * slots;
     const int position = N - n + token, mine = position >= 0 ? position >> a.pages.log2 : -1;
     const int blocks = mine + 1, own = (blocks + THREADS - 1) / THREADS, first = tid * own;
     const int32_t* table = a.pages.table + b * a.pages.table_stride;
@@ -450,39 +451,54 @@ __global__ __launch_bounds__(THREADS) void select_kernel(BlockArgs a) {
 }
 
 constexpr int64_t kMostGroups = INT32_MAX / 1024;
+// What the scores of a launch take at most, so that a long prompt's choice does not ask for its tokens times its blocks (32768 tokens of 8 KV heads behind 8192 blocks: 26 GB);
+// the units go in slices.  It is more than a thousand rows of 16384 blocks, and what the memory-side cache holds.
+constexpr int64_t kSliceBytes = 256 << 20;
 
 struct Plan {
     BlockArgs a{};
-    int64_t groups = 0, rows = 0, bytes = 0;
+    int64_t rows = 0, units = 0, slice_units = 0, slice_rows = 0, bytes = 0;
+    int64_t first_row(int64_t unit) const { return unit == units ? rows : unit / a.token_groups * a.q_tokens + unit % a.token_groups * a.tokens_here * a.passes; }
 };
 
 int plan_of(const specache_pages* cache, const specache_block_config* c, Plan& p) {
     if (int rc = check_blocks(cache, c)) return rc;
     BlockArgs& a = p.a;
     a.G = c->n_q_heads / cache->n_kv_heads;
+    a.q_tokens = c->q_tokens;
     const int64_t blocks = ((int64_t)c->kv_tokens + cache->page_tokens - 1) / cache->page_tokens, tiles = (blocks + kTile - 1) / kTile;
     a.row_blocks = (int)(tiles * kTile);
     a.tokens_here = std::max(1, kTile / a.G);
     p.rows = (int64_t)c->batch * cache->n_kv_heads * c->q_tokens;
     const int64_t heads = (int64_t)c->batch * cache->n_kv_heads, groups = (c->q_tokens + a.tokens_here - 1) / a.tokens_here;
+    const int64_t row_bytes = c->top > 0 ? a.row_blocks * (int64_t)(sizeof(uint64_t) + sizeof(float)) + tiles * (int64_t)sizeof(float) : 0;
     // a wave's bounds are read for up to 8 products' rows, where there are rows enough for 4096 waves all the same
     a.passes = (int)std::max<int64_t>(1, std::min<int64_t>(8, heads * groups * tiles / 4096));
+    while (a.passes > 1 && a.tokens_here * a.passes * row_bytes > kSliceBytes) --a.passes;
     a.token_groups = (int)((groups + a.passes - 1) / a.passes);
-    const int64_t units = heads * a.token_groups;
-    a.splits = units ? (int)std::max<int64_t>(1, std::min<int64_t>((tiles + kScoreWaves - 1) / kScoreWaves, (1024 + units - 1) / units)) : 1;
-    p.groups = a.row_blocks ? units * a.splits : 0;
-    if (p.rows > kMostGroups || p.groups > kMostGroups) return fail_without_context(SPECACHE_EINVAL, "too many rows");
-    p.bytes = c->top > 0 ? p.rows * (a.row_blocks * (int64_t)(sizeof(uint64_t) + sizeof(float)) + tiles * (int64_t)sizeof(float)) : 0;
+    p.units = heads * a.token_groups;
+    const int64_t unit_rows = std::max<int64_t>(1, std::min<int64_t>(c->q_tokens, a.tokens_here * a.passes));
+    p.slice_units = std::min(p.units, kMostGroups / unit_rows);
+    if (row_bytes) p.slice_units = std::min(p.slice_units, std::max<int64_t>(1, kSliceBytes / (unit_rows * row_bytes)));
+    p.slice_rows = std::min(p.rows, p.slice_units * unit_rows);
+    a.splits = p.units ? (int)std::max<int64_t>(1, std::min<int64_t>((tiles + kScoreWaves - 1) / kScoreWaves, (1024 + p.slice_units - 1) / p.slice_units)) : 1;
+    p.bytes = p.slice_rows * row_bytes;
     return SPECACHE_OK;
 }
 
 template <bool BF16>
-void launch(const Plan& p, const BlockArgs& a, hipStream_t stream) {
-    if (a.top > 0 && p.groups && a.pages.n_pages) hipLaunchKernelGGL((score_kernel<BF16>), dim3((unsigned)p.groups), dim3(64 * kScoreWaves), 0, stream, a);
+void launch(const Plan& p, BlockArgs& a, hipStream_t stream) {
     const int threads = a.row_blocks > 1024 ? 1024 : 256;
     const auto kernel = a.row_blocks <= 512 ? select_kernel<BF16, 256, 2> : a.row_blocks <= 1024 ? select_kernel<BF16, 256, 4> : a.row_blocks <= 4096 ? select_kernel<BF16, 1024, 4>
                         : a.row_blocks <= 16384 ? select_kernel<BF16, 1024, 16> : select_kernel<BF16, 1024, 0>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)p.rows), dim3(threads), 0, stream, a);
+    for (int64_t unit = 0; unit < p.units; unit += p.slice_units) {
+        const int64_t units = std::min(p.slice_units, p.units - unit);
+        a.unit0 = (int)unit;
+        a.row0 = (int)p.first_row(unit);
+        if (a.top > 0 && a.row_blocks && a.pages.n_pages)
+            hipLaunchKernelGGL((score_kernel<BF16>), dim3((unsigned)(units * a.splits)), dim3(64 * kScoreWaves), 0, stream, a);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(p.first_row(unit + units) - a.row0)), dim3(threads), 0, stream, a);
+    }
 }
 
 }  // namespace
@@ -523,10 +539,9 @@ int specache_block_select(const specache_pages* cache, const specache_block_conf
     a.kv_lengths = kv_lengths;
     a.blocks = blocks;
     a.keys = (uint64_t*)scratch;
-    a.scores = (float*)(a.keys + p.rows * a.row_blocks);
-    a.sizes = a.scores + p.rows * a.row_blocks;
+    a.scores = (float*)(a.keys + p.slice_rows * a.row_blocks);
+    a.sizes = a.scores + p.slice_rows * a.row_blocks;
     a.batch = cfg->batch;
-    a.q_tokens = cfg->q_tokens;
     a.kv_tokens = cfg->kv_tokens;
     a.top = cfg->top;
     a.first = cfg->first;

@@ -795,6 +795,7 @@ int check_blocks(const specache_pages* cache, const specache_block_config* c) {
     const int64_t slots = (int64_t)c->top + c->first + c->recent;
     if (c->top < 0 || c->first < 0 || c->recent < 0 || slots < 1 || slots > (1 << 20))
         return fail_without_context(SPECACHE_EINVAL, "top, first and recent must not be negative, and make up from 1 to 2^20 entries");
+    if ((int64_t)c->batch * c->q_tokens * cache->n_kv_heads > kMostGroups) return fail_without_context(SPECACHE_EINVAL, "too many lists");
     return SPECACHE_OK;
 }
 
