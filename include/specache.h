@@ -600,7 +600,7 @@ typedef struct specache_pages {
 } specache_pages;
 
 /*
- * Appends to a paged cache with the rotation on the way, in one launch: token t < n of sequence b goes to position starts[b] + t, its key
+ * Appends to a paged cache with the rotation on the way, in one launch (of more than 2^23 workgroups of up to 32 tokens: several): token t < n of sequence b goes to position starts[b] + t, its key
  * (of k [batch, n_kv_heads, tokens]) turned by plan, its value (of v, alike) as it is; q [batch, n_q_heads, tokens] is turned into q_out, which
  * may be q itself.  Arithmetic as in specache_rotate; plan NULL: nothing is turned.  q and q_out may be NULL with n_q_heads = 0.
  * starts: device int32 [batch], the positions that the sequences hold already; NULL: 0.  lengths: device int32 [batch], n, held to

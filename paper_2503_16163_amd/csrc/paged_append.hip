@@ -14,7 +14,7 @@ namespace {
 
 constexpr int kThreads = 256, kSlots = kThreads / kParts;   // rows that a workgroup has in hand at a time
 constexpr int kAhead = 4, kAheadPairs = 2;   // rows whose loads a lane has in flight: queries, and keys with their values
-constexpr int64_t kMostGroups = (1ll << 32) / kThreads - 1;
+constexpr int64_t kMostGroups = INT32_MAX / kThreads;   // of a launch, whose threads are counted in 32 bits
 
 struct AppendArgs {
     specache_rotary plan;
@@ -24,6 +24,7 @@ struct AppendArgs {
     int turns;                         // there is a plan
     int batch, tokens, n_q_heads;
     int segments;                      // of a sequence, at most
+    int64_t first_group;               // of this launch
     int key_groups, key_splits;        // workgroups of keys and values; of them to a segment
     int key_tile_log2, q_tile_log2;    // tokens among the rows in hand
     int q_splits;
@@ -267,18 +268,20 @@ __device__ __forceinline__ void append_pairs(const AppendArgs& a, int group, uin
 template <bool BF16, bool HALF, bool PART, bool STREAM, bool BOUNDS>
 __global__ __launch_bounds__(kThreads, 4) void paged_append_kernel(AppendArgs a) {
     __shared__ uint4v joined[2][BOUNDS ? kThreads / 64 : 1][2][2][kParts];   // [turn][wave][least, most][access][part]
-    if ((int)blockIdx.x < a.key_groups) append_pairs<BF16, HALF, PART, STREAM, BOUNDS>(a, blockIdx.x, joined);
-    else append_queries<BF16, HALF, PART, STREAM>(a, blockIdx.x - a.key_groups);
+    const int64_t group = a.first_group + blockIdx.x;
+    if (group < a.key_groups) append_pairs<BF16, HALF, PART, STREAM, BOUNDS>(a, (int)group, joined);
+    else append_queries<BF16, HALF, PART, STREAM>(a, (int)(group - a.key_groups));
 }
 
 template <bool BF16, bool HALF, bool PART>
-void launch(const AppendArgs& a, int64_t groups, bool stream_out, bool bounds, hipStream_t stream) {
+void launch(AppendArgs& a, int64_t groups, bool stream_out, bool bounds, hipStream_t stream) {
     const auto kernel = stream_out ? (bounds ? paged_append_kernel<BF16, HALF, PART, true, true> : paged_append_kernel<BF16, HALF, PART, true, false>)
                                    : (bounds ? paged_append_kernel<BF16, HALF, PART, false, true> : paged_append_kernel<BF16, HALF, PART, false, false>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kThreads), 0, stream, a);
+    for (a.first_group = 0; a.first_group < groups; a.first_group += kMostGroups)
+        hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(groups - a.first_group, kMostGroups)), dim3(kThreads), 0, stream, a);
 }
 template <bool BF16>
-void launch(const AppendArgs& a, int64_t groups, bool stream_out, bool bounds, hipStream_t stream) {
+void launch(AppendArgs& a, int64_t groups, bool stream_out, bool bounds, hipStream_t stream) {
     if (a.turns && a.plan.layout == SPECACHE_ROTARY_INTERLEAVED) launch<BF16, false, false>(a, groups, stream_out, bounds, stream);
     else if (a.plan.rotary_dim == kD) launch<BF16, true, false>(a, groups, stream_out, bounds, stream);
     else launch<BF16, true, true>(a, groups, stream_out, bounds, stream);
@@ -331,20 +334,17 @@ extern "C" int specache_paged_append(const specache_pages* cache, const specache
     a.segments = starts ? (tokens + page - 2) / page + 1 : (tokens + page - 1) / page;
     while (a.key_tile_log2 < 5 && (1 << a.key_tile_log2) < std::min(tokens, page)) ++a.key_tile_log2;
     while (a.q_tile_log2 < 2 && (1 << a.q_tile_log2) < tokens) ++a.q_tile_log2;
-    const auto q_tiles = [&] { return (int64_t)batch * (((int64_t)tokens + (1 << a.q_tile_log2) - 1) >> a.q_tile_log2); };
-    while (n_q_heads && a.q_tile_log2 < 5 && q_tiles() >= kMostGroups / 4) ++a.q_tile_log2;
+    const int64_t q_tiles = (int64_t)batch * (((int64_t)tokens + (1 << a.q_tile_log2) - 1) >> a.q_tile_log2);   // (2^30 of these and of segments at most)
     // 16 workgroups per compute unit, if there are heads to split
     const auto splits = [](int64_t groups, int heads, int tile_log2) {
         const int64_t most = (heads + (kSlots >> tile_log2) - 1) / (kSlots >> tile_log2);
         return (int)std::min(std::max<int64_t>((4096 + groups - 1) / groups, 1), std::max<int64_t>(most, 1));
     };
-    const int64_t key_tiles = cache->n_pages ? (int64_t)batch * a.segments : 0, q_tiles_n = n_q_heads ? q_tiles() : 0;
-    if (key_tiles >= kMostGroups / 2 || q_tiles_n >= kMostGroups / 2) return fail_without_context(SPECACHE_EINVAL, "too many tokens");
+    const int64_t key_tiles = cache->n_pages ? (int64_t)batch * a.segments : 0, q_tiles_n = n_q_heads ? q_tiles : 0;
     a.key_splits = key_tiles ? splits(key_tiles, cache->n_kv_heads, a.key_tile_log2) : 1;
     a.q_splits = q_tiles_n ? splits(q_tiles_n, n_q_heads, a.q_tile_log2) : 1;
     const int64_t key_groups = key_tiles * a.key_splits, groups = key_groups + q_tiles_n * a.q_splits;
     if (!groups) return SPECACHE_OK;
-    if (groups >= kMostGroups) return fail_without_context(SPECACHE_EINVAL, "too many tokens");
     a.key_groups = (int)key_groups;
     const bool stream_out = (int64_t)batch * tokens * (n_q_heads + 2 * cache->n_kv_heads) * kD * 2 > kCached;
     if (cache->dtype == SPECACHE_BF16) launch<true>(a, groups, stream_out, bounds, (hipStream_t)stream);
