@@ -608,7 +608,7 @@ typedef struct specache_pages {
  * (or is negative, or not in the table) is not written.  positions: device int32 [batch, tokens], contiguous: what the
  * rotation goes by; NULL: a token's position in its sequence.
  * bounds: a page whose place 0 is among the tokens gets those of the tokens written here, any other the wider of what it has and those; a NaN is passed over.
- * Two tokens that one call, or two that overlap, write to one page come from one sequence and one call (pages that sequences share are not appended to).
+ * Two tokens that one call, or two that overlap, write to one page come from one sequence and one call, by way of one entry of the table (pages that sequences share are not appended to).
  * The inputs share no memory with the cache's pages.  batch = 0 and tokens = 0 are allowed; batch * tokens goes up to 2^30.
  * Errors: EINVAL (null or misaligned view, counts, a plan that specache_rotary_plan did not write), EHIP.
  */
@@ -622,6 +622,7 @@ int specache_paged_append(const specache_pages* cache, const specache_rotary* pl
  * positions j <= p that have a page.  A row that sees nothing gives zeros.
  * shared_tokens: the table's rows agree over the first shared_tokens / page_tokens pages (those of row 0 may be read for all).  Their keys and values are then read
  * once for all sequences where the counts promise that this takes less time; it changes the time and the rounding alone.  0: nothing is shared.
+ * batch * n_kv_heads * ceil(q_tokens * (n_q_heads / n_kv_heads) / 128) goes up to 2^22 - 1, batch * q_tokens * n_q_heads up to 2^28.
  */
 typedef struct specache_paged_config {
     int32_t batch;           /* >= 0                                                               */
@@ -632,12 +633,16 @@ typedef struct specache_paged_config {
     float sm_scale;          /* logit scale; <= 0 selects 1/sqrt(head_dim)                         */
 } specache_paged_config;
 
-/* Host only: the bytes of scratch memory that specache_paged_attend needs (0: none); it depends on the counts alone.  Errors: EINVAL. */
+/*
+ * Host only: the bytes of scratch memory that specache_paged_attend needs (0: none; up to 1 GiB, with a prefix that is shared up to 4); it depends on the counts alone.
+ * Errors: EINVAL.
+ */
 int specache_paged_scratch(const specache_pages* cache, const specache_paged_config* cfg, int64_t* bytes);
 
 /*
  * q, out: [batch, n_q_heads, q_tokens] rows of the cache's type (they may have the same view).  q_lengths, kv_lengths: device int32 [batch], n and N, held to
- * 0 .. q_tokens and 0 .. kv_tokens; NULL: those.  Rows from n on and places from N on are neither read nor written.
+ * 0 .. q_tokens and 0 .. kv_tokens; NULL: those.  Rows from n on and places from N on are neither read nor written
+ * (but where a prefix is shared all of its places may be read, and row 0 of a sequence without queries: they count for nothing).
  * Numerics, values that are not finite, scratch and errors: as for specache_window_attend.
  */
 int specache_paged_attend(const specache_pages* cache, const specache_paged_config* cfg, const specache_view* q,

@@ -33,6 +33,23 @@ def test_many_long_lists(tokens, heads, entries):
         assert size.value <= GIB
 
 
+@pytest.mark.parametrize("heads,group,tokens", [(1, 1, 1), (8, 4, 8), (1, 4, 16), (32, 1, 1), (1, 1, 64), (2, 8, 16)])
+def test_the_counts_that_specache_h_names(heads, group, tokens):
+    """The most sequences that it promises are taken, one more than a launch has workgroups or than 2^28 rows is refused; partial results fit 4 GiB with a prefix that is shared."""
+    size = C.c_int64()
+    cache = _pages(n_kv_heads=heads, table_pages=1 << 16)
+    most = min(((1 << 22) - 1) // (heads * -(-tokens * group // 128)), (1 << 28) // (heads * group * tokens))
+    for batch, want in ((most, binding.OK), (most + 1, binding.EINVAL)):
+        for kv_tokens, shared in ((1, 0), (1 << 20, 0), (1 << 20, 1 << 19), (1 << 20, 1 << 20)):
+            size.value = 0
+            assert binding.lib().specache_paged_scratch(_ref(cache), _ref(PagedConfig(batch, heads * group, tokens, kv_tokens, shared, 0.0)), C.byref(size)) == want, (batch, shared)
+            assert size.value <= (4 * GIB if shared else GIB)
+    for batch in (1000, 22705, 47727):
+        if batch <= most:
+            assert binding.lib().specache_paged_scratch(_ref(cache), _ref(PagedConfig(batch, heads * group, tokens, 1 << 20, 1 << 19, 0.0)), C.byref(size)) == binding.OK
+            assert size.value <= 4 * GIB
+
+
 @pytest.mark.gpu
 def test_many_steps_of_few_pages():
     """2100 sequences and 32 heads of up to 131072 positions; most have a few, and all have their pages of one row of the table."""
