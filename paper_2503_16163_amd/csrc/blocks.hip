@@ -166,7 +166,7 @@ __global__ __launch_bounds__(64 * kScoreWaves) void score_kernel(BlockArgs a) {
 }
 
 // 32-bit sums are off by 2^-23 of the magnitudes per addition at most, of which 64 and 2 make a score: 2^-16.9.  The rest to 2^-16 is more than what the magnitudes are off
-// by, as sums of 256 (2^-15 of themselves); and what is lost below the smallest numbers.
+// by, as sums of 128 (2^-16 of themselves); and what is lost below the smallest numbers.
 __device__ __forceinline__ double error_of(float size) { return 0x1p-16 * (double)size + 0x1p-110; }
 // Order of whole numbers for that of scores: the larger the later, 0 below all of them.
 __device__ __forceinline__ uint32_t key_of(float x) {

@@ -773,8 +773,9 @@ int plan_of(const specache_pages* cache, const specache_paged_config* c, Plan& p
     const int64_t rows = (int64_t)c->q_tokens * G;
     const int64_t units = rows ? (int64_t)c->batch * cache->n_kv_heads : 0;
     // Shared where that takes less time by the estimate.  us, shared / not: 16 sequences of 69 tokens behind 323 positions 33 / 19, 3 steps behind 13424 25 / 20, 64 of one head
-    // behind 13559 with 116 tokens 517 / 453; 32 steps of 32 heads behind 12220 59 / 880, 64 of 3 tokens behind 31583 151 / 580.  Over 110 drawn calls 26.6 (all that can be
-    // shared) / 23.7 (geometric means, the choice of waves included); near the border it is off by up to a tenth (one KV head behind 9313 for 32 of 2 23.3 / 25.7).
+    // behind 13559 with 116 tokens 517 / 453; 32 steps of 32 heads behind 12220 59 / 880, 64 of 3 tokens behind 31583 151 / 580.  The 60 calls of several
+    // sequences behind a prefix that random.Random(1) to (250) draw in perf/more_operators.py take 36.1 so, 41.2 always shared, 49.3 never (geometric means), 35.2 at best: 6 are off
+    // by more than 5 % (one KV head behind 9313 for 32 of 2 23.2 / 25.7; furthest, 64 steps of 32 heads behind 156 with 6 of their own 30.4 / 16.2).
     Work alone{cache->n_kv_heads, c->batch, rows, 0, c->kv_tokens};
     const double us = alone.plan(p);
     if (c->batch > 1 && units && units * rows < kMostGroups / 2) {   // (the prefix's workgroups and the others' are one launch)

@@ -265,6 +265,8 @@ __device__ __forceinline__ void append_pairs(const AppendArgs& a, int group, uin
 }
 
 // HALF: pairs of channels are halves of what is turned; PART: which is less than the head
+// (With both and bounds it spills 3 registers, which costs nothing that shows: 32768 tokens of 32 and 8 heads to pages of 64 take 156.5 us with 64 channels turned, without bounds
+// 157.0, all 128 turned 154.6.)
 template <bool BF16, bool HALF, bool PART, bool STREAM, bool BOUNDS>
 __global__ __launch_bounds__(kThreads, 4) void paged_append_kernel(AppendArgs a) {
     __shared__ uint4v joined[2][BOUNDS ? kThreads / 64 : 1][2][2][kParts];   // [turn][wave][least, most][access][part]
