@@ -670,7 +670,7 @@ typedef struct specache_block_config {
 } specache_block_config;
 
 /*
- * Host only: the bytes of scratch memory that either call needs (0: none).  The choice takes 12.25 for each block of a row, for as many rows as 256 MiB hold at a time (or the
+ * Host only: the bytes of scratch memory that either call needs (0: none).  The choice takes 12.25 for each block of a row, for as many rows as 1 GiB holds at a time (or the
  * up to 16 tokens of a sequence whose heads make one matrix product, where those need more); partial results of split walks take up to 1 GiB.  Errors: EINVAL.
  */
 int specache_block_scratch(const specache_pages* cache, const specache_block_config* cfg, int64_t* bytes);

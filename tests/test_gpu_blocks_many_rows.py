@@ -10,7 +10,7 @@ from tests.paged import generator
 from tests.test_gpu_blocks import lists, select
 from tests.test_paged import _pages, _ref
 
-MIB = 1 << 20
+GIB = 1 << 30
 
 
 @pytest.mark.parametrize("batch,heads,group,tokens,kv_tokens,page", [
@@ -19,7 +19,7 @@ def test_scratch_memory_is_bounded(batch, heads, group, tokens, kv_tokens, page)
     size = C.c_int64()
     cache = _pages(n_kv_heads=heads, page_tokens=page, table_pages=kv_tokens // page)
     assert binding.lib().specache_block_scratch(_ref(cache), _ref(BlockConfig(batch, heads * group, tokens, kv_tokens, 16, 1, 1, 0.0)), C.byref(size)) == binding.OK
-    assert 0 < size.value <= 256 * MIB
+    assert 0 < size.value <= GIB
 
 
 def test_one_launch_s_rows_of_the_longest_context():
@@ -42,8 +42,8 @@ def test_most_lists():
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
 @pytest.mark.parametrize("Hq,Hkv,n,n_of,N_of,page,alike", [
-    (32, 8, 1500, [1500, 700], [131072, 100001], 16, False), (9, 3, 2999, [2999, 2998], [131072, 131071], 16, False), (8, 8, 2500, [2500, 2500], [70000, 131072], 16, False),
-    (8, 2, 1800, [1800, 1800], [131072, 100000], 16, True)])     # (all scores alike: told apart in 64 bits in the scratch memory)
+    (32, 8, 1500, [1500, 700], [131072, 100001], 16, False), (9, 3, 4999, [4999, 4998], [131072, 131071], 16, False), (8, 8, 2500, [2500, 2500], [70000, 131072], 16, False),
+    (8, 2, 6500, [6500, 6400], [131072, 100000], 16, True)])     # (all scores alike: told apart in 64 bits in the scratch memory)
 def test_slices(Hq, Hkv, n, n_of, N_of, page, alike, dtype):
     B, most, top, first, recent = 2, 131072, 20, 1, 2
     gen = generator(n)
